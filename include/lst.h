@@ -383,6 +383,105 @@ int lst_input_sync(lst_input* s);
 /* lst_input_free -- synchronise and release the layer (NULL ok). */
 void lst_input_free(lst_input* s);
 
+/*
+ * What stands between the two layers, and what follows the output layer.
+ *
+ * The sparse input layer and the output layer leave the rows between them (m x d
+ * activations and their gradients) to the caller.  The calls below work on such
+ * rows: dropout, a gated linear recurrence over packed sequences, outputs of a
+ * layer whose weights are held in 8 bits, and the choice of a token from them.
+ *
+ * They hold no state.  Shared by all of them:
+ *   - Matrices are row-major with unit stride along a row and any row stride ld
+ *     (in elements, at least the number of columns), at any address that an
+ *     element may have: the halves of one product's rows can be passed as they are.
+ *   - dtype names the element type of the matrices passed as void*; every sum and
+ *     state is float32 or wider, rounded once on its way out.
+ *   - hip_stream is the stream the work is enqueued on; the device of the pointers
+ *     must be the calling thread's current one.  No call allocates, synchronises
+ *     or keeps a pointer, so every one can be captured into a graph.
+ *   - workspace (device) is memory of the caller of at least the bytes that the
+ *     matching lst_*_workspace returns, 16-byte aligned.  Its contents need not be
+ *     kept between calls; two calls that may overlap need one each.
+ *   - status (device, may be NULL) is a word of the caller, zero to begin with:
+ *     an error that only the device can see is stored there when it still is zero.
+ */
+enum { LST_F32 = 0, LST_BF16 = 1, LST_F16 = 2 };
+
+/*
+ * lst_dropout -- y = residual + x * keep / (1 - p), the mask drawn by a
+ * counter-based generator and never stored.
+ *   rows, cols      0 <= rows <= 2^32, cols >= 1.
+ *   x, residual, y  rows x cols; residual may be NULL; y may be x or residual.
+ *   p               probability that an element is dropped, in [0, 1], rounded to a
+ *                   multiple of 2^-16; the factor is that of the rounded p.  A
+ *                   dropped element counts as zero whatever it holds.
+ *   seed, offset    tell masks apart: a program keeps one seed and gives every mask
+ *                   of a step an offset of its own.
+ *   counter (device, may be NULL) is added to offset when the kernel runs, so that
+ *                   the replays of a captured graph draw new masks.
+ * The mask is a function of (seed, offset, row, column) alone: the backward pass is
+ * the same call on the gradient without a residual.  Element (i, j) is kept when the
+ * 16 bits of half j % 2 of word (j % 8) / 2 of Philox4x32-10 with the counter
+ * (j / 8, i, offset's low word, its high word) and the key (seed's low word, its
+ * high word) are at least 65536 p.
+ */
+int lst_dropout(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t ldx,
+                const void* residual, int64_t ldr, void* y, int64_t ldy, double p, uint64_t seed,
+                uint64_t offset, const uint64_t* counter, void* hip_stream);
+
+/*
+ * lst_recur_forward -- a gated linear recurrence over packed sequences:
+ *   f_t = sigmoid(g_t),  h_t = f_t h_{t-1} + (1 - f_t) x_t,  y_t = h_t,
+ * for each of the d channels (1..4096) by itself.
+ *   x, g, y          rows x d, the sequences' rows one after another.
+ *   offsets (device) n_seq + 1 ints, ascending: sequence s has the rows offsets[s] ..
+ *                    offsets[s + 1] - 1, possibly none.  NULL: n_seq sequences of
+ *                    rows / n_seq rows each.  Rows of y in no sequence are left as
+ *                    they were.  Offsets that descend or leave [0, rows] set the
+ *                    status LST_EINDEX; the outputs of that call are unspecified.
+ *   h0     (device)  n_seq x d floats, the states before the first rows; NULL: zeros.
+ *   h_last (device)  n_seq x d floats, receives the last states (that of h0 for a
+ *                    sequence without rows); may be NULL, and may be h0.
+ *   saved  (device)  receives what lst_recur_backward needs: lst_recur_saved(rows, d)
+ *                    floats; NULL when there will be no backward pass.
+ */
+#define LST_RECUR_CHUNK 128 /* rows of y between two states in saved */
+int lst_recur_forward(int32_t dtype, int32_t rows, int32_t n_seq, int32_t d, const void* x,
+                      int64_t ldx, const void* g, int64_t ldg, const int32_t* offsets,
+                      const float* h0, void* y, int64_t ldy, float* h_last, float* saved,
+                      void* workspace, int32_t* status, void* hip_stream);
+
+/*
+ * lst_recur_backward -- gradients of lst_recur_forward.  x, g, offsets and h0 as
+ * there, saved from that call; grad_y (rows x d) and grad_last (n_seq x d floats, or
+ * NULL) are dL/dy and dL/dh_last.  grad_x and grad_g receive dL/dx and dL/dg (rows in
+ * no sequence are left as they were), grad_h0 (or NULL) dL/dh0.
+ */
+int lst_recur_backward(int32_t dtype, int32_t rows, int32_t n_seq, int32_t d, const void* x,
+                       int64_t ldx, const void* g, int64_t ldg, const int32_t* offsets,
+                       const float* h0, const void* grad_y, int64_t ldgy, const float* grad_last,
+                       const float* saved, void* grad_x, int64_t ldgx, void* grad_g,
+                       int64_t ldgg, float* grad_h0, void* workspace, int32_t* status,
+                       void* hip_stream);
+
+/* Floats of saved, and bytes of workspace, for rows x d (-1 for a bad size). */
+int64_t lst_recur_saved(int32_t rows, int32_t d);
+int64_t lst_recur_workspace(int32_t rows, int32_t d);
+
+/*
+ * lst_recur_step -- one token of the same recurrence for each row (generation):
+ * h[slots[i]] <- f h[slots[i]] + (1 - f) x_i, y_i = the new state.
+ *   h     (device)  n_slots x d floats, the states of the sequences in progress.
+ *   slots (device)  rows ints: the state that row i continues; -1: none, its row of y
+ *                   is left as it was.  NULL: row i continues state i.  An index
+ *                   outside [-1, n_slots), and one that an earlier row names already,
+ *                   sets the status LST_EINDEX and counts as -1.
+ */
+int lst_recur_step(int32_t dtype, int32_t rows, int32_t n_slots, int32_t d, const void* x,
+                   int64_t ldx, const void* g, int64_t ldg, const int32_t* slots, float* h,
+                   void* y, int64_t ldy, int32_t* status, void* hip_stream);
+
 /* lst_strerror -- static description of a status code. */
 const char* lst_strerror(int status);
 

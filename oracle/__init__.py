@@ -21,6 +21,8 @@ Modules
             and the recomputation of U^{-T}.
   input_layer  the sparse input layer of section 2.2 (forward A = X W_in and
             the update of the rows of W_in the inputs refer to).
+  between   dropout's generator and mask, and the gated linear recurrence with its
+            gradients.
 
 Pin status (what fixes each function other than itself) is listed in each
 function's docstring; the only function without a pin by the paper is the
@@ -28,4 +30,4 @@ minibatch forms of the two spherical-softmax factored steps, which are pinned
 by the explicit definition (itself pinned by closed forms, finite differences
 and the normalisation of the class probabilities) instead.
 """
-from . import explicit, factored, input_layer, stabilize  # noqa: F401
+from . import between, explicit, factored, input_layer, stabilize  # noqa: F401

@@ -7,7 +7,10 @@ becomes the library's stream.  Every step of the computation runs in the HIP
 kernels of liblst.so; there is no other code path.  If the library has not been
 built, load_library() raises instead of falling back to anything.
 
-Classes FactoredOutputLayer and NaiveOutputLayer wrap a state handle.
+Classes FactoredOutputLayer and NaiveOutputLayer wrap a state handle.  The
+operators around the layers (dropout, the gated recurrence, ...) hold no handle:
+they run on torch's current stream of their tensors' device, and their workspaces
+are tensors of their own for each call.
 """
 from __future__ import annotations
 
@@ -31,6 +34,12 @@ LST_ENOSCRATCH = -8
 LST_LOSS_SQUARED = 0
 LST_LOSS_SPHERICAL = 1
 LST_LOSS_SPHERICAL_SHIFTED = 2
+
+LST_F32 = 0
+LST_BF16 = 1
+LST_F16 = 2
+
+LST_RECUR_CHUNK = 128
 
 _LOSS = {"squared": LST_LOSS_SQUARED, "spherical": LST_LOSS_SPHERICAL,
          "spherical_shifted": LST_LOSS_SPHERICAL_SHIFTED}
@@ -122,6 +131,18 @@ _SIGS = {
     "lst_input_get_W": (ctypes.c_int, [_P, _P]),
     "lst_input_sync": (ctypes.c_int, [_P]),
     "lst_input_free": (None, [_P]),
+    "lst_dropout": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, _P,
+                                   ctypes.c_int64, _P, ctypes.c_int64, _P, ctypes.c_int64,
+                                   ctypes.c_double, ctypes.c_uint64, ctypes.c_uint64, _P, _P]),
+    "lst_recur_forward": (ctypes.c_int, [ctypes.c_int32] * 4 + [
+        _P, ctypes.c_int64, _P, ctypes.c_int64, _P, _P, _P, ctypes.c_int64, _P, _P, _P, _P, _P]),
+    "lst_recur_backward": (ctypes.c_int, [ctypes.c_int32] * 4 + [
+        _P, ctypes.c_int64, _P, ctypes.c_int64, _P, _P, _P, ctypes.c_int64, _P, _P, _P,
+        ctypes.c_int64, _P, ctypes.c_int64, _P, _P, _P, _P]),
+    "lst_recur_saved": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32]),
+    "lst_recur_workspace": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32]),
+    "lst_recur_step": (ctypes.c_int, [ctypes.c_int32] * 4 + [
+        _P, ctypes.c_int64, _P, ctypes.c_int64, _P, _P, _P, ctypes.c_int64, _P, _P]),
     "lst_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "lst_free": (None, [_P]),
 }
@@ -359,6 +380,194 @@ def lst_free(h) -> None:
         load_library().lst_free(h)
 
 
+# ------------------------------------------- the operators around the layers
+def _dtype_code(t, what: str) -> int:
+    import torch
+
+    code = {torch.float32: LST_F32, torch.bfloat16: LST_BF16, torch.float16: LST_F16}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what} must be float32, bfloat16 or float16, got {t.dtype}")
+    return code
+
+
+def _matrix(t, what: str, like=None, shape=None):
+    """Address and row stride of a device matrix with unit stride along its rows (None -> NULL);
+    like: a tensor whose type and device it must have."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda:
+        raise TypeError(f"{what} must be a device tensor")
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{what} must be a matrix" + (f" of {tuple(shape)}" if shape else ""))
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise TypeError(f"{what} must be {like.dtype} on {like.device}, got {t.dtype} on {t.device}")
+    rows, cols = t.shape
+    ld = t.stride(0)
+    if rows > 0x7FFFFFFF or cols > 0x7FFFFFFF:
+        raise ValueError(f"{what} is too large")
+    if rows <= 1:
+        ld = cols
+    if (cols > 1 and t.stride(1) != 1) or ld < cols:
+        raise ValueError(f"{what} must have unit stride along its rows, and rows that do not overlap")
+    return t.data_ptr(), ld
+
+
+def _vector(t, dtype, what: str, device, count=None):
+    """Address of a contiguous device tensor of the given type and number of elements."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.device != device:
+        raise TypeError(f"{what} must be a tensor on {device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, got {t.dtype}")
+    if not t.is_contiguous() or (count is not None and t.numel() != count):
+        raise ValueError(f"{what} must be contiguous" +
+                         (f" and hold {count} elements" if count is not None else ""))
+    return t.data_ptr()
+
+
+def _enqueue(name: str, device, *args) -> None:
+    """Call an entry point with torch's current stream of the device as its last argument."""
+    import torch
+
+    fn = getattr(load_library(), name)
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if device.index == torch.cuda.current_device():
+        code = fn(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            code = fn(*args, stream)
+    if code != LST_OK:
+        raise LstError(code, name)
+
+
+def _word(v, what: str) -> int:
+    v = int(v)
+    if not 0 <= v < 1 << 64:
+        raise ValueError(f"{what} must be in [0, 2^64)")
+    return v
+
+
+def lst_dropout(x, p, seed, offset=0, *, residual=None, counter=None, out=None):
+    """y = residual + x * keep / (1 - p); the mask is that of (seed, offset, row, column)."""
+    import torch
+
+    px, ldx = _matrix(x, "x")
+    code = _dtype_code(x, "x")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    pr, ldr = _matrix(residual, "residual", x, x.shape)
+    py, ldy = _matrix(out, "out", x, x.shape)
+    _enqueue("lst_dropout", x.device, code, x.shape[0], x.shape[1], px, ldx, pr, ldr, py, ldy,
+             float(p), _word(seed, "seed"), _word(offset, "offset"),
+             _vector(counter, torch.int64, "counter", x.device, 1))
+    return out
+
+
+def lst_recur_saved(rows: int, d: int) -> int:
+    return int(load_library().lst_recur_saved(rows, d))
+
+
+def lst_recur_workspace(rows: int, d: int) -> int:
+    return int(load_library().lst_recur_workspace(rows, d))
+
+
+def _recur_inputs(x, g, offsets, h0, n_seq):
+    """Checked arguments that the forward and the backward pass share."""
+    import torch
+
+    px, ldx = _matrix(x, "x")
+    code = _dtype_code(x, "x")
+    pg, ldg = _matrix(g, "g", x, x.shape)
+    if offsets is not None:
+        if offsets.numel() < 1:
+            raise ValueError("offsets must hold at least one element")
+        have = offsets.numel() - 1
+    elif n_seq is not None:
+        have = int(n_seq)
+    else:
+        have = h0.shape[0] if h0 is not None else 1
+    if n_seq is not None and n_seq != have:
+        raise ValueError("n_seq and offsets disagree")
+    rows, d = x.shape
+    if h0 is not None and tuple(h0.shape) != (have, d):
+        raise ValueError("h0 must be (n_seq, d)")
+    if offsets is None and (have < 1 or rows % have):
+        raise ValueError("without offsets, the rows must divide into n_seq equal sequences")
+    return (have, (code, rows, have, d, px, ldx, pg, ldg,
+                   _vector(offsets, torch.int32, "offsets", x.device),
+                   _vector(h0, torch.float32, "h0", x.device)))
+
+
+def _recur_work(rows, d, device):
+    import torch
+
+    n = lst_recur_workspace(rows, d)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n > 0 else None
+
+
+def lst_recur_forward(x, g, offsets=None, h0=None, *, n_seq=None, out=None, h_last=None,
+                      save=False, status=None):
+    """(y, h_last, saved) of the gated recurrence; saved is None unless save."""
+    import torch
+
+    have, args = _recur_inputs(x, g, offsets, h0, n_seq)
+    rows, d, dev = x.shape[0], x.shape[1], x.device
+    if out is None:
+        out = torch.empty((rows, d), dtype=x.dtype, device=dev)
+    if h_last is None:
+        h_last = torch.empty((have, d), dtype=torch.float32, device=dev)
+    saved = None
+    if save:
+        saved = torch.empty((lst_recur_saved(rows, d) // d, d), dtype=torch.float32, device=dev)
+    work = _recur_work(rows, d, dev)
+    _enqueue("lst_recur_forward", dev, *args, *_matrix(out, "out", x, x.shape),
+             _vector(h_last, torch.float32, "h_last", dev, have * d),
+             None if saved is None else saved.data_ptr(),
+             None if work is None else work.data_ptr(),
+             _vector(status, torch.int32, "status", dev, 1))
+    return out, h_last, saved
+
+
+def lst_recur_backward(x, g, grad_y, saved, offsets=None, h0=None, grad_last=None, *, n_seq=None,
+                       out=None, status=None):
+    """(grad_x, grad_g, grad_h0) from the forward pass' inputs and saved; out: the first two."""
+    import torch
+
+    have, args = _recur_inputs(x, g, offsets, h0, n_seq)
+    rows, d, dev = x.shape[0], x.shape[1], x.device
+    if out is None:
+        out = tuple(torch.empty((rows, d), dtype=x.dtype, device=dev) for _ in range(2))
+    grad_h0 = torch.empty((have, d), dtype=torch.float32, device=dev)
+    work = _recur_work(rows, d, dev)
+    _enqueue("lst_recur_backward", dev, *args, *_matrix(grad_y, "grad_y", x, x.shape),
+             _vector(grad_last, torch.float32, "grad_last", dev, have * d),
+             _vector(saved, torch.float32, "saved", dev, lst_recur_saved(rows, d)),
+             *_matrix(out[0], "grad_x", x, x.shape), *_matrix(out[1], "grad_g", x, x.shape),
+             grad_h0.data_ptr(), None if work is None else work.data_ptr(),
+             _vector(status, torch.int32, "status", dev, 1))
+    return out[0], out[1], grad_h0
+
+
+def lst_recur_step(x, g, h, slots=None, *, out=None, status=None):
+    """One token for each row: h[slots[i]] moves on in place; returns the new states as y."""
+    import torch
+
+    px, ldx = _matrix(x, "x")
+    code = _dtype_code(x, "x")
+    pg, ldg = _matrix(g, "g", x, x.shape)
+    rows, d, dev = x.shape[0], x.shape[1], x.device
+    if h.dim() != 2 or h.shape[1] != d:
+        raise ValueError("h must be (n_slots, d)")
+    if out is None:
+        out = torch.empty((rows, d), dtype=x.dtype, device=dev)
+    _enqueue("lst_recur_step", dev, code, rows, h.shape[0], d, px, ldx, pg, ldg,
+             _vector(slots, torch.int32, "slots", dev, rows),
+             _vector(h, torch.float32, "h", dev), *_matrix(out, "out", x, x.shape),
+             _vector(status, torch.int32, "status", dev, 1))
+    return out
+
+
 # ------------------------------------------------------------------- classes
 class _Layer:
     def __init__(self, handle, D: int, d: int, m_max: int, K_max: int, device):
@@ -541,3 +750,61 @@ class NaiveOutputLayer(_Layer):
         loss, grad = out if out is not None else self._alloc_outputs(H.shape[0])
         lst_naive_step(self._h, H, Y_idx, Y_val, lr, loss, grad)
         return loss, grad
+
+
+class Dropout:
+    """Dropout whose mask is drawn from (seed, offset, row, column) and never stored: the
+    backward pass takes the offset of its forward pass."""
+
+    def __init__(self, p: float, seed: int = 0):
+        if not 0.0 <= p <= 1.0:
+            raise ValueError("p must be in [0, 1]")
+        self.p, self.seed = float(p), _word(seed, "seed")
+
+    def forward(self, x, offset=0, *, residual=None, counter=None, out=None):
+        return lst_dropout(x, self.p, self.seed, offset, residual=residual, counter=counter,
+                           out=out)
+
+    def backward(self, grad_y, offset=0, *, counter=None, out=None):
+        return lst_dropout(grad_y, self.p, self.seed, offset, counter=counter, out=out)
+
+
+class GatedRecurrence:
+    """h_t = f_t h_{t-1} + (1 - f_t) x_t with f = sigmoid(g), over packed sequences."""
+
+    def __init__(self, d: int, device="cuda"):
+        import torch
+
+        load_library()
+        self.d = int(d)
+        self._status = torch.zeros(1, dtype=torch.int32, device=device)
+
+    def _width(self, x):
+        if x.dim() != 2 or x.shape[1] != self.d:
+            raise ValueError(f"rows must have {self.d} columns")
+
+    def forward(self, x, g, offsets=None, h0=None, *, n_seq=None, out=None, h_last=None,
+                save=False):
+        self._width(x)
+        return lst_recur_forward(x, g, offsets, h0, n_seq=n_seq, out=out, h_last=h_last,
+                                 save=save, status=self._status)
+
+    def backward(self, x, g, grad_y, saved, offsets=None, h0=None, grad_last=None, *, n_seq=None,
+                 out=None):
+        self._width(x)
+        return lst_recur_backward(x, g, grad_y, saved, offsets, h0, grad_last, n_seq=n_seq,
+                                  out=out, status=self._status)
+
+    def step(self, x, g, h, slots=None, *, out=None):
+        self._width(x)
+        return lst_recur_step(x, g, h, slots, out=out, status=self._status)
+
+    def sync(self) -> int:
+        """Wait for the device; returns (and clears) the sticky status code."""
+        import torch
+
+        torch.cuda.synchronize(self._status.device)
+        code = int(self._status.item())
+        if code:
+            self._status.zero_()
+        return code

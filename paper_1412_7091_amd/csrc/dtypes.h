@@ -1,0 +1,67 @@
+// Element types of the operators around the output layer: float32, bfloat16 and
+// float16 in memory, float32 in registers.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "lst.h"
+
+namespace lst {
+
+// N elements at any address that an element may have: one access of up to 16
+// bytes each, which global memory takes without further alignment.
+template <class T, int N>
+struct VecOf {
+  typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
+template <class T>
+struct VecOf<T, 1> {
+  typedef T type;
+};
+template <class T, int N>
+using vec_t = typename VecOf<T, N>::type;
+
+template <class T, int N>
+__device__ inline void load_vec(const T* p, T (&v)[N]) {
+  if constexpr (N == 1) {
+    v[0] = *p;
+  } else {
+    const vec_t<T, N> w = *reinterpret_cast<const vec_t<T, N>*>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = w[i];
+  }
+}
+
+template <class T, int N>
+__device__ inline void store_vec(T* p, const T (&v)[N]) {
+  if constexpr (N == 1) {
+    *p = v[0];
+  } else {
+    vec_t<T, N> w;
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = v[i];
+    *reinterpret_cast<vec_t<T, N>*>(p) = w;
+  }
+}
+
+// Calls f with a value of the element type that dtype names.
+template <class F>
+inline int with_dtype(int dtype, F f) {
+  switch (dtype) {
+    case LST_F32: return f(float{});
+    case LST_BF16: return f(__bf16{});
+    case LST_F16: return f(_Float16{});
+    default: return LST_EINVAL;
+  }
+}
+
+inline bool known_dtype(int dtype) {
+  return dtype == LST_F32 || dtype == LST_BF16 || dtype == LST_F16;
+}
+
+inline int launched() { return hipGetLastError() == hipSuccess ? LST_OK : LST_EHIP; }
+
+}  // namespace lst
