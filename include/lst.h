@@ -482,6 +482,33 @@ int lst_recur_step(int32_t dtype, int32_t rows, int32_t n_slots, int32_t d, cons
                    int64_t ldx, const void* g, int64_t ldg, const int32_t* slots, float* h,
                    void* y, int64_t ldy, int32_t* status, void* hip_stream);
 
+/*
+ * lst_quantize -- a matrix (the weights of a trained layer: lst_materialize_W) into
+ * 8 bits, with one scale for each block of 128 columns of a row.
+ *   x       rows x cols, 1 <= cols <= 4096.
+ *   codes  (device)  rows x 128 b bytes, b = (cols + 127) / 128, 16-byte aligned:
+ *                    receives e4m3 values, zeros behind the last column.
+ *   scales (device)  rows x b bytes: receives biased exponents; a value of the block
+ *                    is its code times 2^(scale - 127), the smallest power of two
+ *                    with no value of the block above 448 times it (at least 2^-127).
+ * Codes are rounded to nearest, ties to even.  A value that is not finite gives a
+ * code that is no number and does not count for the scale.
+ */
+int lst_quantize(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t ldx,
+                 uint8_t* codes, uint8_t* scales, void* hip_stream);
+
+/*
+ * lst_scores -- outputs of a layer held in 8 bits: O = H W^T.
+ *   H                m x d of type dtype, quantised by the call as lst_quantize does.
+ *   codes, scales    W (D x d) as lst_quantize leaves it.
+ *   O                m x D of type out_dtype.
+ * The quantised values are multiplied exactly and summed in float32.
+ */
+int lst_scores(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int32_t d, const void* H,
+               int64_t ldh, const uint8_t* codes, const uint8_t* scales, void* O, int64_t ldo,
+               void* workspace, void* hip_stream);
+int64_t lst_scores_workspace(int32_t m, int32_t d); /* bytes; -1 for a bad size */
+
 /* lst_strerror -- static description of a status code. */
 const char* lst_strerror(int status);
 

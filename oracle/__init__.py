@@ -23,6 +23,8 @@ Modules
             the update of the rows of W_in the inputs refer to).
   between   dropout's generator and mask, and the gated linear recurrence with its
             gradients.
+  answers   weights in 8 bits with a scale for each block of 128, the outputs from
+            them, and the choice of a token from outputs.
 
 Pin status (what fixes each function other than itself) is listed in each
 function's docstring; the only function without a pin by the paper is the
@@ -30,4 +32,4 @@ minibatch forms of the two spherical-softmax factored steps, which are pinned
 by the explicit definition (itself pinned by closed forms, finite differences
 and the normalisation of the class probabilities) instead.
 """
-from . import between, explicit, factored, input_layer, stabilize  # noqa: F401
+from . import answers, between, explicit, factored, input_layer, stabilize  # noqa: F401

@@ -143,6 +143,12 @@ _SIGS = {
     "lst_recur_workspace": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32]),
     "lst_recur_step": (ctypes.c_int, [ctypes.c_int32] * 4 + [
         _P, ctypes.c_int64, _P, ctypes.c_int64, _P, _P, _P, ctypes.c_int64, _P, _P]),
+    "lst_quantize": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, _P,
+                                    ctypes.c_int64, _P, _P, _P]),
+    "lst_scores_workspace": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32]),
+    "lst_scores": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64,
+                                  ctypes.c_int32, _P, ctypes.c_int64, _P, _P, _P, ctypes.c_int64,
+                                  _P, _P]),
     "lst_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "lst_free": (None, [_P]),
 }
@@ -568,6 +574,53 @@ def lst_recur_step(x, g, h, slots=None, *, out=None, status=None):
     return out
 
 
+def lst_quantize(x, *, codes=None, scales=None):
+    """(codes, scales) of a matrix in 8 bits, one scale for each block of 128 columns."""
+    import torch
+
+    px, ldx = _matrix(x, "x")
+    code = _dtype_code(x, "x")
+    rows, cols = x.shape
+    blocks = (cols + 127) // 128
+    if codes is None:
+        codes = torch.empty((rows, 128 * blocks), dtype=torch.uint8, device=x.device)
+    if scales is None:
+        scales = torch.empty((rows, blocks), dtype=torch.uint8, device=x.device)
+    _enqueue("lst_quantize", x.device, code, rows, cols, px, ldx,
+             _vector(codes, torch.uint8, "codes", x.device, rows * 128 * blocks),
+             _vector(scales, torch.uint8, "scales", x.device, rows * blocks))
+    return codes, scales
+
+
+def lst_scores_workspace(m: int, d: int) -> int:
+    return int(load_library().lst_scores_workspace(m, d))
+
+
+def lst_scores(H, codes, scales, *, dtype=None, out=None):
+    """O = H W^T from the weights' codes and scales; dtype: that of O (H's when not given)."""
+    import torch
+
+    ph, ldh = _matrix(H, "H")
+    code = _dtype_code(H, "H")
+    (m, d), dev = H.shape, H.device
+    D = scales.shape[0]
+    blocks = (d + 127) // 128
+    if scales.dim() != 2 or scales.shape[1] != blocks or codes.shape != (D, 128 * blocks):
+        raise ValueError(f"codes and scales must be those of a matrix with {d} columns")
+    if out is None:
+        out = torch.empty((m, D), dtype=dtype or H.dtype, device=dev)
+    elif dtype is not None and out.dtype != dtype:
+        raise TypeError(f"out must be {dtype}, got {out.dtype}")
+    po, ldo = _matrix(out, "out", shape=(m, D))
+    if out.device != dev:
+        raise TypeError(f"out must be on {dev}")
+    work = torch.empty(max(0, lst_scores_workspace(m, d)), dtype=torch.uint8, device=dev)
+    _enqueue("lst_scores", dev, code, _dtype_code(out, "out"), m, D, d, ph, ldh,
+             _vector(codes, torch.uint8, "codes", dev),
+             _vector(scales, torch.uint8, "scales", dev), po, ldo, work.data_ptr())
+    return out
+
+
 # ------------------------------------------------------------------- classes
 class _Layer:
     def __init__(self, handle, D: int, d: int, m_max: int, K_max: int, device):
@@ -808,3 +861,35 @@ class GatedRecurrence:
         if code:
             self._status.zero_()
         return code
+
+
+class EightBitOutputLayer:
+    """The outputs O = H W^T of a trained layer, its weights held in 8 bits (a quarter of the
+    bytes): W is any D x d matrix, or an output layer, whose materialize_W gives one."""
+
+    def __init__(self, W):
+        W = self._weights(W)
+        self.D, self.d = W.shape
+        self.codes, self.scales = lst_quantize(W)
+
+    @staticmethod
+    def _weights(W):
+        if not isinstance(W, _Layer):
+            return W
+        import torch
+
+        W = W.materialize_W()
+        torch.cuda.synchronize(W.device)  # a layer works on the stream of its own
+        return W
+
+    def load(self, W) -> None:
+        """Take new weights of the same shape, into the same memory."""
+        W = self._weights(W)
+        if tuple(W.shape) != (self.D, self.d):
+            raise ValueError(f"W must be ({self.D}, {self.d})")
+        lst_quantize(W, codes=self.codes, scales=self.scales)
+
+    def scores(self, H, *, dtype=None, out=None):
+        if H.dim() != 2 or H.shape[1] != self.d:
+            raise ValueError(f"H must have {self.d} columns")
+        return lst_scores(H, self.codes, self.scales, dtype=dtype, out=out)

@@ -19,7 +19,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "liblst.so")
 
 SOURCES = ["gemm.hip", "step.hip", "small.hip", "stabilize.hip", "input_layer.hip", "online.hip",
-           "lu.hip", "shifted.hip", "dropout.hip", "recur.hip", "lst_api.hip"]
+           "lu.hip", "shifted.hip", "dropout.hip", "recur.hip",
+           "eight_bit.hip", "lst_api.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

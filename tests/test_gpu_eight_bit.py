@@ -1,0 +1,261 @@
+"""lst_quantize and lst_scores against oracle.answers: codes and scales bit for bit, outputs
+within the roundings of a float32 sum."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1412_7091_amd as lst
+from oracle import answers
+
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _check_codes(x, got):
+    codes, scales = answers.quantize(_np(x))
+    assert np.array_equal(got[1].cpu().numpy(), scales)
+    have = got[0].cpu().numpy()
+    nan = (codes & 127) == 127
+    assert np.array_equal((have & 127) == 127, nan)
+    assert np.array_equal(have[~nan], codes[~nan])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 127), (5, 128), (2, 129), (33, 500), (7, 1024),
+                                       (2, 4096)])
+def test_quantize(gpu_lib, dtype, rows, cols):
+    g = torch.Generator("cuda").manual_seed(rows + 10 * cols)
+    x = torch.randn((rows, cols), device="cuda", generator=g).to(dtype)
+    _check_codes(x, lst.lst_quantize(x))
+    big = torch.zeros((rows, cols + 5), device="cuda", dtype=dtype)
+    big[:, 1:1 + cols] = x
+    a, b = lst.lst_quantize(x), lst.lst_quantize(big[:, 1:1 + cols])
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.gpu
+def test_quantize_borders(gpu_lib):
+    """Largest values at and beside the borders of the scale; ties; zeros; extremes; not finite."""
+    g = torch.Generator("cuda").manual_seed(3)
+    x = torch.randn((24, 256), device="cuda", generator=g)
+    one = torch.ones((), device="cuda")
+    for i, v in enumerate((448.0, 450.0, 1.75, 3.5, 2.0 ** -100, 2.0 ** 100, 0.875)):
+        at = torch.full((1,), v, device="cuda")
+        x[3 * i] = x[3 * i].clamp(-1, 1) * v * 0.99
+        x[3 * i + 1], x[3 * i + 2] = x[3 * i], x[3 * i]
+        x[3 * i, 5] = v
+        x[3 * i + 1, 5] = torch.nextafter(at, 2 * at * one)
+        x[3 * i + 2, 5] = -torch.nextafter(at, 0 * at)
+    x[21] = 0
+    x[22, :128], x[22, 128:] = 1e-41, 3.4e38
+    x[23, 7], x[23, 8], x[23, 9] = float("inf"), -float("inf"), float("nan")
+    _check_codes(x, lst.lst_quantize(x))
+    # every value halfway between two codes, and the codes themselves
+    up = torch.from_numpy(answers.e4m3_table()[:127]).cuda()
+    t = torch.cat((up, (up[1:] + up[:-1]) / 2, torch.zeros(3, device="cuda"))).float()
+    t[-1] = 448.0
+    t = torch.cat((t, -t))[None, :]
+    x = torch.zeros((1, 512), device="cuda")
+    x[0, :t.shape[1]] = t
+    x[0, 0::128] = 448.0  # the scale is one in every block
+    _check_codes(x, lst.lst_quantize(x))
+
+
+def _scores(m, D, d, dtype, out, seed):
+    g = torch.Generator("cuda").manual_seed(seed)
+    W = torch.randn((D, d), device="cuda", generator=g) / d ** 0.5
+    H = torch.randn((m, d), device="cuda", generator=g).to(dtype)
+    # rows and blocks of very different sizes
+    W *= torch.exp2(torch.randint(-9, 9, (D, 1), device="cuda", generator=g).float())
+    W[:, :d // 2] *= 64
+    layer = lst.EightBitOutputLayer(W)
+    got = layer.scores(H, dtype=out)
+    assert got.dtype == out and got.shape == (m, D)
+    _check_scores(H, layer, got)
+    return H, layer, got
+
+
+def _check_scores(H, layer, got):
+    hq = answers.values(*answers.quantize(_np(H)))
+    want, bar = answers.scores(hq, answers.values(layer.codes.cpu().numpy(),
+                                                  layer.scales.cpu().numpy()))
+    bar = bar + torch.finfo(got.dtype).eps / 2 * (np.abs(want) + bar)
+    if got.dtype == torch.float16:
+        bar += 2.0 ** -25
+    assert (np.abs(_np(got) - want) <= bar).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,D,d", [
+    (1, 1, 1), (1, 15, 128), (2, 16, 129), (5, 63, 500), (16, 64, 37), (17, 65, 300),
+    (33, 1000, 500), (64, 127, 512), (65, 128, 1024), (100, 129, 130), (128, 2001, 500),
+    (129, 257, 256), (300, 700, 385), (513, 4097, 128), (3, 300, 4096)])
+def test_scores(gpu_lib, m, D, d):
+    _scores(m, D, d, torch.float32, torch.float32, m + D + d)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("m", [1, 20, 140])
+def test_scores_types(gpu_lib, dtype, out, m):
+    # float16 outputs stay within its range: |H| < 6, |W| < 64 512 8 / sqrt(d) would not
+    g = torch.Generator("cuda").manual_seed(m)
+    W = torch.randn((333, 200), device="cuda", generator=g)
+    H = torch.randn((m, 200), device="cuda", generator=g).to(dtype)
+    layer = lst.EightBitOutputLayer(W)
+    _check_scores(H, layer, layer.scores(H, dtype=out))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("out", TYPES)
+def test_scores_strides_and_what_is_beside(gpu_lib, out):
+    m, D, d = 37, 203, 150
+    g = torch.Generator("cuda").manual_seed(12)
+    W = torch.randn((D, d), device="cuda", generator=g)
+    big = torch.randn((m, d + 9), device="cuda", generator=g)
+    H = big[:, 3:3 + d]
+    layer = lst.EightBitOutputLayer(W)
+    whole = torch.full((m + 2, D + 4), 7.0, device="cuda").to(out)
+    o = whole[1:1 + m, 1:1 + D]
+    layer.scores(H, out=o)
+    assert torch.equal(o, layer.scores(H.contiguous(), dtype=out))
+    o.fill_(7.0)
+    assert (whole == 7).all()
+
+
+@pytest.mark.gpu
+def test_scores_not_finite_stays_in_its_row(gpu_lib):
+    H, layer, want = _scores(20, 100, 140, torch.float32, torch.float32, 2)
+    H[3, 5] = float("inf")
+    H[7, 139] = float("nan")
+    got = layer.scores(H)
+    bad = torch.zeros(20, dtype=torch.bool)
+    bad[3] = bad[7] = True
+    assert got[bad].isnan().all() and not got[~bad].isnan().any()
+    H[3, 5], H[7, 139] = 0, 0
+    assert torch.equal(layer.scores(H)[~bad], want[~bad])
+
+
+@pytest.mark.gpu
+def test_of_a_trained_layer_and_load(gpu_lib):
+    """The weights of a factored layer after a step, and again after another."""
+    g = torch.Generator("cuda").manual_seed(5)
+    D, d, m, K = 3000, 40, 16, 5
+    V = torch.randn((D, d), device="cuda", generator=g) / d ** 0.5
+    layer = lst.FactoredOutputLayer(V, m_max=m, K_max=K)
+    H = torch.randn((m, d), device="cuda", generator=g) / d ** 0.5
+    idx = torch.randint(0, D, (m, K), device="cuda", generator=g, dtype=torch.int32)
+    val = torch.randn((m, K), device="cuda", generator=g)
+    held = None
+    for _ in range(2):
+        layer.step(H, idx, val, 1e-2)
+        if held is None:
+            held = lst.EightBitOutputLayer(layer)
+        else:
+            held.load(layer)
+        W = layer.materialize_W()
+        assert layer.sync() == 0
+        codes, scales = lst.lst_quantize(W)
+        assert torch.equal(codes, held.codes) and torch.equal(scales, held.scales)
+        _check_scores(H, held, held.scores(H))
+        # 8 bits keep each weight to 2^-4 of itself (or 2^-10 of 448ths of its block's largest)
+        rel = (held.scores(H).double() - H.double() @ W.double().T).norm() / \
+            (H.double() @ W.double().T).norm()
+        assert rel < 2 * 2.0 ** -4
+    with pytest.raises(ValueError):
+        held.load(torch.zeros((D, d + 1), device="cuda"))
+    layer.close()
+
+
+@pytest.mark.gpu
+def test_captured(gpu_lib):
+    H, layer, want = _scores(40, 500, 260, torch.bfloat16, torch.float32, 8)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = layer.scores(H, dtype=torch.float32)
+    for k in range(3):
+        H.mul_(2.0)  # a power of two: the outputs move by it exactly
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want * 2.0 ** (k + 1))
+
+
+@pytest.mark.gpu
+def test_large(gpu_lib):
+    """Codes and outputs past 2^31 elements; a few rows checked."""
+    D, d, m = 4_300_000, 500, 512
+    codes = torch.zeros((D, 512), dtype=torch.uint8, device="cuda")
+    scales = torch.full((D, 4), 127, dtype=torch.uint8, device="cuda")
+    g = torch.Generator("cuda").manual_seed(1)
+    H = torch.randn((m, d), device="cuda", generator=g)
+    at = [0, 2_097_152, 4_194_303, 4_194_304, D - 1]
+    W = torch.randn((len(at), d), device="cuda", generator=g)
+    codes[at], scales[at] = lst.lst_quantize(W)
+    out = lst.lst_scores(H, codes, scales, dtype=torch.bfloat16)
+    want = lst.lst_scores(H, *lst.lst_quantize(W), dtype=torch.bfloat16)
+    assert torch.equal(out[:, at], want)
+    assert int((out != 0).sum(dtype=torch.int64)) == int((want != 0).sum())
+    del out
+    X = torch.zeros((D, d), device="cuda", dtype=torch.bfloat16)
+    X[at] = W.bfloat16()
+    c2, s2 = lst.lst_quantize(X)
+    w2 = lst.lst_quantize(W.bfloat16())
+    assert torch.equal(c2[at], w2[0]) and torch.equal(s2[at], w2[1])
+
+
+@pytest.mark.gpu
+def test_refusals(gpu_lib):
+    layer = lst.EightBitOutputLayer(torch.zeros((10, 140), device="cuda"))
+    H = torch.zeros((3, 140), device="cuda")
+    with pytest.raises(ValueError):
+        layer.scores(H[:, :139])
+    with pytest.raises(ValueError):
+        lst.lst_scores(H[:, :100], layer.codes, layer.scales)
+    with pytest.raises(ValueError):
+        lst.lst_scores(H, layer.codes[:9], layer.scales)
+    with pytest.raises(TypeError):
+        lst.lst_scores(H, layer.codes.int(), layer.scales)
+    with pytest.raises(TypeError):
+        lst.lst_scores(H, layer.codes, layer.scales.cpu())
+    with pytest.raises(TypeError):
+        layer.scores(H.double())
+    with pytest.raises(TypeError):
+        layer.scores(H, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        layer.scores(H, out=torch.zeros((3, 9), device="cuda"))
+    with pytest.raises(ValueError):
+        layer.scores(H, out=torch.zeros((10, 3), device="cuda").T)
+    with pytest.raises(lst.LstError):
+        lst.lst_quantize(torch.zeros((2, 4097), device="cuda"))
+    assert layer.scores(H[:0]).shape == (0, 10)
+
+
+def test_refusals_on_host():
+    lib = lst.load_library()
+    P = 64  # never dereferenced
+
+    def quantize(dtype=0, rows=2, cols=8, x=P, ldx=8, codes=P, scales=P):
+        return lib.lst_quantize(dtype, rows, cols, x, ldx, codes, scales, None)
+
+    for kw in (dict(dtype=3), dict(rows=-1), dict(cols=0), dict(cols=4097), dict(x=None),
+               dict(codes=None), dict(scales=None), dict(ldx=7), dict(codes=P + 8)):
+        assert quantize(**kw) == lst.LST_EINVAL, kw
+    assert quantize(rows=0, x=None) == lst.LST_OK
+
+    def scores(dtype=0, out=0, m=2, D=5, d=8, H=P, ldh=8, codes=P, scales=P, O=P, ldo=5, work=P):
+        return lib.lst_scores(dtype, out, m, D, d, H, ldh, codes, scales, O, ldo, work, None)
+
+    for kw in (dict(dtype=3), dict(out=-1), dict(m=-1), dict(D=0), dict(d=0), dict(d=4097),
+               dict(H=None), dict(codes=None), dict(scales=None), dict(O=None), dict(work=None),
+               dict(ldh=7), dict(ldo=4), dict(codes=P + 4), dict(work=P + 8), dict(D=1 << 40)):
+        assert scores(**{**kw, **({"ldo": 1 << 41} if "D" in kw and kw["D"] else {})}) \
+            == lst.LST_EINVAL, kw
+    assert scores(m=0, H=None) == lst.LST_OK
+    assert lst.lst_scores_workspace(3, 129) >= 3 * 258 and lst.lst_scores_workspace(1, 5000) == -1
