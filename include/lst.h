@@ -509,6 +509,33 @@ int lst_scores(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int32_t d
                void* workspace, void* hip_stream);
 int64_t lst_scores_workspace(int32_t m, int32_t d); /* bytes; -1 for a bad size */
 
+/*
+ * lst_sample -- a token from each row of outputs.
+ *   logits            m x D, D >= 1.  Entries that are -inf or no number are never
+ *                     chosen; when some are +inf, the choice is among those.
+ *   temperature, top_k, top_p, min_p, u (device, m values each; the first four may
+ *                     be NULL: 1, 0, 1, 0).
+ *   tokens (device)   m ints: receives the tokens.
+ *   prob   (device)   m floats, or NULL: receives each token's probability among the
+ *                     entries that were kept.
+ * With the entries ordered by value, equal ones by index, and
+ * w_i = exp((x_i - max) / temperature):
+ *   1. top_k > 0 keeps the first top_k entries;
+ *   2. top_p < 1 keeps those before which less than top_p of the weight that is left
+ *      stands, at least the first;
+ *   3. min_p > 0 keeps those with w_i >= min_p, at least the first;
+ *   4. the token is the first, by index, at which the sum of the kept weights exceeds
+ *      u times their total.
+ * temperature 0 takes the first entry of the order.  Weights have 64 bits.  A row
+ * without an entry to choose from, with a negative or infinite temperature, u outside
+ * [0, 1) or a parameter that is no number gets the token -1 and the probability 0.
+ */
+int lst_sample(int32_t dtype, int32_t m, int32_t D, const void* logits, int64_t ldx,
+               const float* temperature, const int32_t* top_k, const float* top_p,
+               const float* min_p, const float* u, int32_t* tokens, float* prob, void* workspace,
+               void* hip_stream);
+int64_t lst_sample_workspace(int32_t m, int32_t D); /* bytes; -1 for a bad size */
+
 /* lst_strerror -- static description of a status code. */
 const char* lst_strerror(int status);
 

@@ -149,6 +149,9 @@ _SIGS = {
     "lst_scores": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64,
                                   ctypes.c_int32, _P, ctypes.c_int64, _P, _P, _P, ctypes.c_int64,
                                   _P, _P]),
+    "lst_sample": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P,
+                                  ctypes.c_int64, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "lst_sample_workspace": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32]),
     "lst_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "lst_free": (None, [_P]),
 }
@@ -621,6 +624,37 @@ def lst_scores(H, codes, scales, *, dtype=None, out=None):
     return out
 
 
+def lst_sample_workspace(m: int, D: int) -> int:
+    return int(load_library().lst_sample_workspace(m, D))
+
+
+def lst_sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, tokens=None,
+               prob=None):
+    """(tokens, prob): a token for each row of outputs from the random numbers u (one a row, in
+    [0, 1)); temperature, top_k, top_p and min_p are device vectors, one value a row, or None."""
+    import torch
+
+    px, ldx = _matrix(logits, "logits")
+    code = _dtype_code(logits, "logits")
+    (m, D), dev = logits.shape, logits.device
+    if tokens is None:
+        tokens = torch.empty(m, dtype=torch.int32, device=dev)
+    if prob is None:
+        prob = torch.empty(m, dtype=torch.float32, device=dev)
+    n = lst_sample_workspace(m, D)
+    work = torch.empty(n, dtype=torch.uint8, device=dev) if n > 0 else None
+    f32 = torch.float32
+    if u is None:
+        raise TypeError("u must be a device vector of float32")
+    _enqueue("lst_sample", dev, code, m, D, px, ldx,
+             _vector(temperature, f32, "temperature", dev, m),
+             _vector(top_k, torch.int32, "top_k", dev, m), _vector(top_p, f32, "top_p", dev, m),
+             _vector(min_p, f32, "min_p", dev, m), _vector(u, f32, "u", dev, m),
+             _vector(tokens, torch.int32, "tokens", dev, m), _vector(prob, f32, "prob", dev, m),
+             None if work is None else work.data_ptr())
+    return tokens, prob
+
+
 # ------------------------------------------------------------------- classes
 class _Layer:
     def __init__(self, handle, D: int, d: int, m_max: int, K_max: int, device):
@@ -893,3 +927,7 @@ class EightBitOutputLayer:
         if H.dim() != 2 or H.shape[1] != self.d:
             raise ValueError(f"H must have {self.d} columns")
         return lst_scores(H, self.codes, self.scales, dtype=dtype, out=out)
+
+    def sample(self, H, u, **settings):
+        """(tokens, prob) chosen from the outputs for H: lst_sample's settings."""
+        return lst_sample(self.scores(H, dtype=settings.pop("dtype", None)), u, **settings)

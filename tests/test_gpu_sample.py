@@ -1,0 +1,243 @@
+"""lst_sample against oracle.answers: the same tokens."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1412_7091_amd as lst
+from oracle import answers
+
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+NAMES = ("temperature", "top_k", "top_p", "min_p")
+
+
+def _device(name, values):
+    return torch.tensor(values, dtype=torch.int32 if name == "top_k" else torch.float32,
+                        device="cuda")
+
+
+def _check(x, u, settings):
+    """settings: per row a dict; every row is compared with the oracle."""
+    m = x.shape[0]
+    default = dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0)
+    rows = [{**default, **s} for s in settings]
+    kw = {n: _device(n, [r[n] for r in rows]) for n in NAMES}
+    tokens, prob = lst.lst_sample(x, _device("u", u), **kw)
+    tokens, prob = tokens.cpu().numpy(), prob.cpu().numpy()
+    xs = x.float().cpu().numpy()
+    for i in range(m):
+        want, p = answers.sample(xs[i], u[i], **rows[i])
+        assert tokens[i] == want, (i, rows[i], u[i], tokens[i], want, prob[i], p)
+        # a float32 quotient of sums in 64 bits (and integers of 2^-42 or finer)
+        assert abs(prob[i] - p) <= 2.0 ** -23 * p + 2.0 ** -40, (i, prob[i], p)
+    return tokens
+
+
+MIX = [dict(), dict(temperature=0.0), dict(temperature=0.6), dict(temperature=3.0, top_k=1),
+       dict(top_k=2), dict(top_k=50, top_p=0.9), dict(top_p=0.5), dict(top_p=0.97, min_p=0.01),
+       dict(min_p=0.05), dict(min_p=1.0), dict(top_p=0.0), dict(top_k=7, min_p=0.3),
+       dict(top_k=500, temperature=1.7), dict(top_p=0.999, temperature=0.3),
+       dict(temperature=40.0, top_p=0.8), dict(temperature=1e-3), dict(top_k=1500, top_p=0.99),
+       dict(top_k=10 ** 9), dict(top_k=-3), dict(top_p=2.0, min_p=-1.0)]
+
+
+def _logits(m, D, dtype, seed, spread=2.0):
+    g = torch.Generator("cuda").manual_seed(seed)
+    x = torch.randn((m, D), device="cuda", generator=g) * spread
+    x -= 0.5 * torch.log(torch.arange(1, D + 1, device="cuda").float())
+    u = torch.rand(m, device="cuda", generator=g).tolist()
+    return x.to(dtype), [float(np.float32(v)) for v in u]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [1, 2, 63, 64, 65, 500, 2000, 2047, 4097, 20_011])
+def test_settings(gpu_lib, dtype, D):
+    x, u = _logits(2 * len(MIX), D, dtype, D)
+    _check(x, u, MIX + MIX)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,spread", [(131_073, 2.0), (200_000, 0.3), (793_471, 4.0)])
+def test_large_rows(gpu_lib, dtype, D, spread):
+    x, u = _logits(len(MIX), D, dtype, D, spread)
+    _check(x, u, MIX)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [300, 30_000, 200_000])
+def test_ends_of_the_random_numbers(gpu_lib, D):
+    x, _ = _logits(len(MIX), D, torch.float32, 5)
+    x[:, ::3] = -float("inf")
+    last = float(np.nextafter(np.float32(1), np.float32(0)))
+    for u in (0.0, last, 2.0 ** -24, 0.5):
+        _check(x, [u] * len(MIX), MIX)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [100, 5000, 150_000])
+def test_equal_entries(gpu_lib, dtype, D):
+    """Ties at every border: all entries equal, two values, a staircase."""
+    rows = []
+    x = torch.zeros((3 * len(MIX), D), device="cuda")
+    x[len(MIX):2 * len(MIX)] = (torch.arange(D, device="cuda") % 7 == 3).float()
+    x[2 * len(MIX):] = -(torch.arange(D, device="cuda") % 40).float() / 8
+    u = [(i * 0.37 + 0.21) % 1 for i in range(3 * len(MIX))]
+    u = [float(np.float32(v)) for v in u]
+    tokens = _check(x.to(dtype), u, 3 * MIX)
+    assert tokens[1] == 0 and tokens[len(MIX) + 1] == 3  # greedy: the first of the equal ones
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [40, 9000, 180_000])
+def test_masked_rows_and_what_is_not_finite(gpu_lib, D):
+    inf, nan = float("inf"), float("nan")
+    lowest = torch.finfo(torch.float32).min
+    base, _ = _logits(1, D, torch.float32, 9)
+    x = base.repeat(12, 1)
+    x[0] = -inf
+    x[1] = nan
+    x[2] = -inf
+    x[2, D // 2] = -5.0
+    x[3] = lowest
+    x[3, [3, 5]] = 1.0
+    x[4] = lowest                       # nothing but the lowest value: all of them alike
+    x[5, ::2] = nan
+    x[6, [1, D - 1]] = inf
+    x[7] = -inf
+    x[7, D - 1] = lowest
+    x[8] = torch.where(torch.arange(D, device="cuda") % 2 == 0, 0.0, -0.0)
+    x[9] = 3.4e38
+    x[9, 7] = -3.4e38
+    x[10] = 1e-42 * torch.arange(D, device="cuda")
+    x[11, : D // 2] = -inf
+    for s in (dict(), dict(temperature=0.0), dict(top_k=3), dict(top_p=0.6), dict(min_p=0.1),
+              dict(top_k=20, top_p=0.5, min_p=0.01, temperature=0.5)):
+        for u in (0.0, 0.3, 0.77):
+            t = _check(x, [float(np.float32(u))] * 12, [s] * 12)
+            assert t[0] == -1 and t[1] == -1 and t[2] == D // 2 and t[3] in (3, 5)
+            assert t[6] in (1, D - 1) and t[7] == D - 1
+
+
+@pytest.mark.gpu
+def test_bad_parameters_give_no_token(gpu_lib):
+    inf, nan = float("inf"), float("nan")
+    bad = [dict(temperature=-1.0), dict(temperature=nan), dict(temperature=inf), dict(top_p=nan),
+           dict(min_p=nan), dict(), dict(), dict(), dict()]
+    u = [0.5] * 5 + [1.0, -0.25, nan, 0.5]
+    for D in (700, 70_000):
+        x, _ = _logits(len(bad), D, torch.float32, 3)
+        t = _check(x, u, bad)
+        assert (t[:8] == -1).all() and t[8] >= 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_strides_and_missing_parameters(gpu_lib, dtype):
+    m, D = 6, 50_003
+    x, u = _logits(m, D, dtype, 21)
+    big = torch.full((m, D + 9), 99.0, device="cuda").to(dtype)
+    big[:, 5:5 + D] = x
+    uv = _device("u", u)
+    a = lst.lst_sample(x, uv)
+    b = lst.lst_sample(big[:, 5:5 + D], uv)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    for i in range(m):
+        assert int(a[0][i]) == answers.sample(x[i].float().cpu().numpy(), u[i])[0]
+    k = _device("top_k", [40] * m)
+    c = lst.lst_sample(big[:, 5:5 + D], uv, top_k=k)
+    for i in range(m):
+        assert int(c[0][i]) == answers.sample(x[i].float().cpu().numpy(), u[i], top_k=40)[0]
+    # one row's last entries end the memory of the matrix
+    d = lst.lst_sample(x[m - 1:], uv[m - 1:])
+    assert torch.equal(d[0], a[0][m - 1:])
+
+
+@pytest.mark.gpu
+def test_many_rows(gpu_lib):
+    m, D = 700, 3000
+    x, u = _logits(m, D, torch.float32, 33)
+    _check(x, u, [MIX[i % len(MIX)] for i in range(m)])
+
+
+@pytest.mark.gpu
+def test_frequencies(gpu_lib):
+    """Evenly spread random numbers over one row: each token as often as its probability says."""
+    m, D = 4096, 20_000
+    x, _ = _logits(1, D, torch.float32, 6)
+    x[0, :5] = x.max() + torch.tensor([0.5, 0.1, 0.7, 0.3, 0.2], device="cuda")
+    u = (torch.arange(m, device="cuda") + 0.5) / m
+    kw = {n: _device(n, [v] * m) for n, v in dict(top_k=5, temperature=0.8).items()}
+    tokens, prob = lst.lst_sample(x.expand(m, D).contiguous(), u, **kw)
+    w = torch.softmax(x[0, :5].double() / 0.8, 0).cpu().numpy()
+    have = np.bincount(tokens.cpu().numpy(), minlength=5) / m
+    assert len(have) == 5 and np.abs(have - w).max() <= 1.5 / m
+
+
+@pytest.mark.gpu
+def test_captured_and_repeated(gpu_lib):
+    m, D = 24, 100_000
+    x, u = _logits(m, D, torch.float32, 41, spread=1.0)
+    kw = {n: _device(n, [{**dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0),
+                          **MIX[i % len(MIX)]}[n] for i in range(m)]) for n in NAMES}
+    uv = _device("u", u)
+    eager = lst.lst_sample(x, uv, **kw)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = lst.lst_sample(x, uv, **kw)
+    for k in range(4):
+        got[0].fill_(-7)
+        again = lst.lst_sample(x, uv, **kw)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b, c in zip(got, eager, again):
+            assert torch.equal(a, b) and torch.equal(a, c)
+    # new random numbers in the same memory
+    uv.copy_(1 - uv)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], lst.lst_sample(x, uv, **kw)[0])
+
+
+@pytest.mark.gpu
+def test_refusals(gpu_lib):
+    x, u = torch.zeros((3, 8), device="cuda"), torch.zeros(3, device="cuda")
+    with pytest.raises(TypeError):
+        lst.lst_sample(x, None)
+    with pytest.raises(ValueError):
+        lst.lst_sample(x, u[:2])
+    with pytest.raises(TypeError):
+        lst.lst_sample(x, u.double())
+    with pytest.raises(TypeError):
+        lst.lst_sample(x, u, top_k=u)
+    with pytest.raises(TypeError):
+        lst.lst_sample(x, u, temperature=torch.ones(3))
+    with pytest.raises(ValueError):
+        lst.lst_sample(x, u, top_p=torch.ones(4, device="cuda"))
+    with pytest.raises(ValueError):
+        lst.lst_sample(x.T, u)
+    with pytest.raises(TypeError):
+        lst.lst_sample(x.double(), u)
+    with pytest.raises(TypeError):
+        lst.lst_sample(x, u, tokens=torch.zeros(3, dtype=torch.int64, device="cuda"))
+    with pytest.raises(lst.LstError):
+        lst.lst_sample(torch.zeros((3, 0), device="cuda"), u)
+    assert lst.lst_sample(x[:0], u[:0])[0].shape == (0,)
+
+
+def test_refusals_on_host():
+    lib = lst.load_library()
+    P = 64  # never dereferenced
+
+    def call(dtype=0, m=2, D=5, x=P, ldx=5, u=P, tokens=P, work=P):
+        return lib.lst_sample(dtype, m, D, x, ldx, None, None, None, None, u, tokens, None, work,
+                              None)
+
+    for kw in (dict(dtype=3), dict(m=-1), dict(D=0), dict(x=None), dict(u=None),
+               dict(tokens=None), dict(ldx=4)):
+        assert call(**kw) == lst.LST_EINVAL, kw
+    assert call(m=0, x=None) == lst.LST_OK
+    assert lst.lst_sample_workspace(-1, 5) == -1 and lst.lst_sample_workspace(1, 0) == -1
