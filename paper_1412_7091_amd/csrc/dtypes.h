@@ -11,27 +11,21 @@
 
 namespace lst {
 
-// N elements at any address that an element may have: one access of up to 16
-// bytes each, which global memory takes without further alignment.
-template <class T, int N>
-struct VecOf {
-  typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
-};
-template <class T>
-struct VecOf<T, 1> {
-  typedef T type;
-};
-template <class T, int N>
-using vec_t = typename VecOf<T, N>::type;
-
+// N elements at any address that an element may have, in accesses of up to 16 bytes,
+// which global memory takes without further alignment.
 template <class T, int N>
 __device__ inline void load_vec(const T* p, T (&v)[N]) {
   if constexpr (N == 1) {
     v[0] = *p;
   } else {
-    const vec_t<T, N> w = *reinterpret_cast<const vec_t<T, N>*>(p);
+    constexpr int M = (int)sizeof(T) * N > 16 ? 16 / (int)sizeof(T) : N;
+    typedef T vec __attribute__((ext_vector_type(M), aligned(sizeof(T))));
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = w[i];
+    for (int j = 0; j < N; j += M) {
+      const vec w = *reinterpret_cast<const vec*>(p + j);
+#pragma unroll
+      for (int i = 0; i < M; ++i) v[j + i] = w[i];
+    }
   }
 }
 
@@ -40,10 +34,15 @@ __device__ inline void store_vec(T* p, const T (&v)[N]) {
   if constexpr (N == 1) {
     *p = v[0];
   } else {
-    vec_t<T, N> w;
+    constexpr int M = (int)sizeof(T) * N > 16 ? 16 / (int)sizeof(T) : N;
+    typedef T vec __attribute__((ext_vector_type(M), aligned(sizeof(T))));
 #pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = v[i];
-    *reinterpret_cast<vec_t<T, N>*>(p) = w;
+    for (int j = 0; j < N; j += M) {
+      vec w;
+#pragma unroll
+      for (int i = 0; i < M; ++i) w[i] = v[j + i];
+      *reinterpret_cast<vec*>(p + j) = w;
+    }
   }
 }
 
