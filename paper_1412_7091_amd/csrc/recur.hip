@@ -12,6 +12,30 @@
 //
 // f and 1 - f are both formed from exp(-|g|): neither loses its digits where the
 // gate saturates.  States, gates and sums are float32.
+//
+// Both passes read each row once.  The packed rows are cut into chunks of 128,
+// whatever sequences they hold, and a block has one chunk of 64 or 128 channels:
+// eight waves of 16 rows, held in registers.  A row's map h -> f h + (1 - f) x, and
+// so every stretch of rows, is a pair (A, B) with h -> A h + B.  The block publishes
+// the pair of its chunk, gathers those of the chunks before it, back to the one in
+// which the sequence of its first row begins, and only then runs over its rows.
+//
+//  - Blocks take their chunks by a ticket, so the chunks that a block waits for have
+//    blocks that run already, and a block publishes before it waits: no wait is
+//    without end.
+//  - A pair is one 64-bit word, written and read by one atomic access, and no fence is
+//    needed; the workspace starts out as words that no pair has.
+//  - Every sixteenth block publishes the pair of its sixteen chunks too, so a block
+//    reads at most 15 pairs and one for each sixteen chunks farther back.  Which pairs
+//    it reads and how it joins them depends on the chunk alone: the result does not
+//    depend on which block was faster.
+//  - The first row of a sequence forgets what comes in.  Its pair has A = -0, which no
+//    product of gates has (they are not negative): h -> B then, also where h is no
+//    number.
+//
+// The backward pass runs the same way from the last chunk to the first on
+// (f L)_t = f_t (dL/dy_t + (f L)_{t+1}), and computes the states within a chunk again
+// from the state before it, which the forward pass saves.
 #include "dtypes.h"
 
 namespace lst {
@@ -47,68 +71,475 @@ __device__ inline void raise(int32_t* status) {
   if (status) atomicCAS(status, 0, LST_EINDEX);
 }
 
-// Rows [b, e) of sequence s; false (and the status) when they are not rows of the call.
-__device__ inline bool rows_of(const RecurArgs& a, int s, int& b, int& e) {
-  if (a.offsets) {
-    b = a.offsets[s];
-    e = a.offsets[s + 1];
-  } else {
-    const int n = a.rows / a.n_seq;
-    b = s * n;
-    e = b + n;
+// -------------------------------------------------------------- pairs (A, B)
+struct Pair {
+  float a, b;
+};
+
+__device__ inline bool forgets(float a) { return __float_as_uint(a) == 0x80000000u; }
+__device__ inline float through(Pair p, float h) { return forgets(p.a) ? p.b : fmaf(p.a, h, p.b); }
+// first p, then q
+__device__ inline Pair join(Pair p, Pair q) {
+  return {forgets(q.a) ? q.a : q.a * p.a, through(q, p.b)};
+}
+
+constexpr unsigned long long kNone = ~0ull;  // A: a number that pack() does not leave
+
+__device__ inline unsigned long long pack(Pair p) {
+  const float a = p.a == p.a ? p.a : __uint_as_float(0x7FC00000u);
+  return (unsigned long long)__float_as_uint(a) << 32 | __float_as_uint(p.b);
+}
+
+__device__ inline Pair unpack(unsigned long long v) {
+  return {__uint_as_float((uint32_t)(v >> 32)), __uint_as_float((uint32_t)v)};
+}
+
+// ------------------------------------------------------------- the workspace
+constexpr int kRows = 16;                    // rows a wave
+constexpr int kWaves = kChunk / kRows;       // waves a block
+constexpr int kThreads = 64 * kWaves;
+constexpr int kGroupChunks = 16;             // chunks whose pair is published together
+constexpr int kHead = 64;                    // bytes before the words: the ticket
+constexpr int kPolls = 1 << 22;              // several seconds: never reached
+
+struct Shape {
+  int chunks, tiles, width;  // width: channels of all tiles
+  int groups;
+  bool joined() const { return chunks > 1; }
+  int64_t words() const { return joined() ? (int64_t)(chunks + groups) * width : 0; }
+};
+
+Shape shape_of(int rows, int d, int vec) {
+  Shape s;
+  s.chunks = rows ? (int)(((int64_t)rows + kChunk - 1) / kChunk) : 1;
+  s.tiles = (d + 64 * vec - 1) / (64 * vec);
+  s.width = s.tiles * 64 * vec;
+  s.groups = s.chunks / kGroupChunks;
+  return s;
+}
+
+__global__ __launch_bounds__(256) void recur_clear_kernel(unsigned long long* words, int64_t n,
+                                                          unsigned* ticket) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i == 0) *ticket = 0;
+  if (i < n) words[i] = kNone;
+}
+
+struct Workspace {
+  unsigned* ticket;
+  unsigned long long *chunk, *group;  // pairs, width words each
+};
+
+// ------------------------------------------------- what a block knows of its rows
+template <int VEC>
+struct Block {
+  float2 own[kWaves][64 * VEC];   // the waves' pairs
+  float2 far[kWaves][64 * VEC];   // of the chunks before: groups (first half), chunks
+  int start[kChunk], end[kChunk];  // 1 + the sequence whose first (last) row it is, or 0
+  int ticket;
+  int s0;     // first sequence that ends behind the first row
+  int reach;  // first row (forward) or last row (backward) of the sequence that goes on
+  int valid0, valid1;  // rows of any sequence
+};
+
+// The sequences' borders among rows [r0, r1) of the chunk, and how far the sequence
+// that enters the chunk (forward: at its first row, else at its last) reaches.
+template <bool FORWARD, int VEC>
+__device__ void find_borders(Block<VEC>& sh, const RecurArgs& a, int r0, int r1) {
+  const int tid = threadIdx.x, n = a.n_seq;
+  if (tid < kChunk) sh.start[tid] = sh.end[tid] = 0;
+  const int enter = FORWARD ? r0 : r1 - 1;
+  if (tid == 0) {
+    sh.reach = enter;
+    sh.valid0 = a.offsets ? a.offsets[0] : 0;
+    sh.valid1 = a.offsets ? a.offsets[n] : a.rows;
   }
-  if (b >= 0 && b <= e && e <= a.rows) return true;
-  raise(a.status);
-  return false;
+  auto mark = [&](int s, int b, int e) {
+    if (b < 0 || b >= e || e > a.rows) return;
+    if (b >= r0 && b < r1) sh.start[b - r0] = s + 1;
+    if (e > r0 && e <= r1) sh.end[e - 1 - r0] = s + 1;
+    if (b <= enter && enter < e) sh.reach = FORWARD ? b : e - 1;
+  };
+  if (!a.offsets) {
+    const int len = a.rows / n;
+    __syncthreads();
+    if (len && tid < kChunk && r0 + tid < r1) {
+      const int s = (r0 + tid) / len;
+      if (tid == 0 || (r0 + tid) % len == 0) mark(s, s * len, s * len + len);
+    }
+    __syncthreads();
+    return;
+  }
+  // the first sequence that ends behind r0, by kThreads probes at a time
+  int lo = 0, hi = n;
+  while (hi - lo > kThreads) {
+    const int64_t step = ((int64_t)hi - lo + kThreads - 1) / kThreads;
+    if (tid == 0) sh.s0 = kThreads;
+    __syncthreads();
+    if (a.offsets[min(lo + (tid + 1) * step, (int64_t)hi)] > r0) atomicMin(&sh.s0, tid);
+    __syncthreads();
+    const int t = sh.s0;
+    __syncthreads();
+    const int64_t from = t == kThreads ? hi : lo + t * step;
+    hi = (int)min(from + step - 1, (int64_t)hi);
+    lo = (int)min(from, (int64_t)hi);
+  }
+  __syncthreads();
+  for (int base = lo; base < n; base += kThreads) {
+    const int s = base + tid;
+    const int b = s < n ? a.offsets[s] : 0x7FFFFFFF;
+    if (s < n) mark(s, b, a.offsets[s + 1]);
+    if (__syncthreads_or(s >= n || b >= r1)) break;
+  }
+  __syncthreads();
+}
+
+// The sequences without rows among this chunk's share of all of them: to <- from (zeros); and
+// the status, once for every pair of offsets that is none.
+template <int VEC>
+__device__ void empty_sequences(const RecurArgs& a, int chunk, int chunks, int c, bool on,
+                                const float* from, float* to, bool check) {
+  const int64_t n = a.n_seq;
+  const int s0 = (int)(n * chunk / chunks), s1 = (int)(n * (chunk + 1) / chunks);
+  for (int s = s0 + (int)threadIdx.x / 64; s < s1; s += kWaves) {
+    int b = 0, e = 0;
+    if (a.offsets) {
+      b = a.offsets[s];
+      e = a.offsets[s + 1];
+    } else {
+      e = a.rows / a.n_seq;
+    }
+    if (check && (b < 0 || b > e || e > a.rows)) raise(a.status);
+    if (b == e && to && on)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v)
+        to[(int64_t)s * a.d + c + v] = from ? from[(int64_t)s * a.d + c + v] : 0.f;
+  }
+}
+
+// The pairs [from, to) of `words` joined, first to last; lane l's VEC channels are at `at`.
+template <int VEC>
+__device__ void gather(const unsigned long long* words, int64_t width, int64_t at, int from,
+                       int to, Pair (&out)[VEC], int32_t* status) {
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) out[v] = {1.f, 0.f};
+  constexpr int kAhead = 4;  // words under way together
+  for (int i0 = from; i0 < to; i0 += kAhead) {
+    unsigned long long w[kAhead][VEC];
+    for (int poll = 0;; ++poll) {
+      bool have = true;
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const int i = min(i0 + j, to - 1);
+#pragma unroll
+        for (int v = 0; v < VEC; ++v)
+          w[j][v] = __hip_atomic_load(words + i * width + at + v, __ATOMIC_RELAXED,
+                                      __HIP_MEMORY_SCOPE_AGENT);
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) have &= w[j][v] != kNone;
+      if (__all(have)) break;
+      if (poll == kPolls) {
+        if (status) atomicCAS(status, 0, LST_EHIP);
+        break;
+      }
+      __builtin_amdgcn_s_sleep(1);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (i0 + j < to)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) out[v] = join(out[v], unpack(w[j][v]));
+  }
+}
+
+// What comes into the chunk.  j counts chunks in the direction of the scan, j0 is the
+// one in which the sequence that comes in begins; the waves' pairs are in sh.own,
+// ORDER(w) the w-th of them in that direction.  Publishes the chunk's pair, and the
+// group's where it is complete.
+template <int VEC, class Order>
+__device__ void come_in(Block<VEC>& sh, const Shape& z, const Workspace& ws, int j, int j0,
+                        int64_t at, Order order, float (&carry)[VEC], int32_t* status) {
+  const int w = threadIdx.x / 64, l = threadIdx.x % 64;
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) carry[v] = 0.f;
+  if (z.chunks == 1) return;
+  Pair all[VEC];
+  if (w == 0) {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      all[v] = {1.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < kWaves; ++k) {
+        const float2 p = sh.own[order(k)][l * VEC + v];
+        all[v] = join(all[v], {p.x, p.y});
+      }
+      __hip_atomic_store(ws.chunk + (int64_t)j * z.width + at + v, pack(all[v]),
+                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  }
+  const int group = j / kGroupChunks, g0 = group * kGroupChunks;
+  const bool closes = j % kGroupChunks == kGroupChunks - 1;
+  if (j0 >= j && !closes) return;
+  // half of the waves take the groups before, half the chunks of this group before; a block
+  // that closes its group publishes the group's pair before it waits for other groups
+  constexpr int kHalf = kWaves / 2;
+  const bool near = w >= kHalf;
+  const int first = near ? (closes ? g0 : max(g0, j0)) : min(j0 / kGroupChunks, group);
+  const int last = near ? j : (j0 < g0 ? group : first);
+  const int per = (max(last - first, 0) + kHalf - 1) / kHalf;
+  const int from = first + (w % kHalf) * per, to = min(last, from + per);
+  auto collect = [&]() {
+    Pair p[VEC];
+    gather<VEC>(near ? ws.chunk : ws.group, z.width, at, from, to, p, status);
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) sh.far[w][l * VEC + v] = make_float2(p[v].a, p[v].b);
+  };
+  if (near || !closes) collect();
+  __syncthreads();
+  if (closes) {
+    if (w == 0)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        Pair p{1.f, 0.f};
+#pragma unroll
+        for (int k = kHalf; k < kWaves; ++k) {
+          const float2 q = sh.far[k][l * VEC + v];
+          p = join(p, {q.x, q.y});
+        }
+        __hip_atomic_store(ws.group + (int64_t)group * z.width + at + v, pack(join(p, all[v])),
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+    if (j0 >= j) return;
+    if (!near) collect();
+    __syncthreads();
+  }
+#pragma unroll
+  for (int v = 0; v < VEC; ++v)
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      const float2 q = sh.far[k][l * VEC + v];
+      // what a closing block gathered before the sequence's chunk ends at its first row
+      carry[v] = through({q.x, q.y}, carry[v]);
+    }
+}
+
+// A lane's VEC elements of a row in one register: two of 16 bits, or one.
+template <class T, int VEC>
+__device__ inline uint32_t load_word(const T* p) {
+  if constexpr (sizeof(T) == 4) return __float_as_uint(*p);
+  if constexpr (VEC == 1) return *reinterpret_cast<const uint16_t*>(p);
+  typedef uint32_t word __attribute__((aligned(2)));
+  return *reinterpret_cast<const word*>(p);
 }
 
 template <class T>
-__global__ __launch_bounds__(64) void recur_forward_kernel(RecurArgs a, const T* x, const T* g,
-                                                           T* y) {
-  const int c = blockIdx.y * 64 + threadIdx.x, s = blockIdx.x;
-  int b, e;
-  if (c >= a.d || !rows_of(a, s, b, e)) return;
-  float h = a.h0 ? a.h0[(int64_t)s * a.d + c] : 0.f;
-  for (int64_t t = b; t < e; ++t) {
-    if (a.saved && t % kChunk == 0) a.saved[t / kChunk * a.d + c] = h;
-    float f, i;
-    gate((float)g[t * a.ldg + c], f, i);
-    h = f * h + i * (float)x[t * a.ldx + c];
-    y[t * a.ldy + c] = (T)h;
-  }
-  if (a.h_last) a.h_last[(int64_t)s * a.d + c] = h;
+__device__ inline float part(uint32_t w, int v) {
+  if constexpr (sizeof(T) == 4) return __uint_as_float(w);
+  if constexpr (std::is_same_v<T, __bf16>)
+    return __uint_as_float(v ? w & 0xFFFF0000u : w << 16);
+  else
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)(v ? w >> 16 : w));
 }
 
-template <class T>
-__global__ __launch_bounds__(64) void recur_backward_kernel(RecurArgs a, const T* x, const T* g,
-                                                            const T* dy, T* dx, T* dg) {
-  __shared__ float before[kChunk][64];  // the state that each row of a chunk starts from
-  const int l = threadIdx.x, c = blockIdx.y * 64 + l, s = blockIdx.x;
-  int b, e;
-  if (c >= a.d || !rows_of(a, s, b, e)) return;
-  float m = a.grad_last ? a.grad_last[(int64_t)s * a.d + c] : 0.f;
-  for (int hi = e; hi > b;) {
-    const int lo = max(b, (hi - 1) / kChunk * kChunk);
-    float h = lo > b || lo % kChunk == 0
-                  ? a.saved_in[(int64_t)(lo / kChunk) * a.d + c]
-                  : (a.h0 ? a.h0[(int64_t)s * a.d + c] : 0.f);
-    for (int64_t t = lo; t < hi; ++t) {
-      before[t - lo][l] = h;
+template <class T, int VEC>
+__device__ inline void load_rows(const T* p, int64_t ld, int r, int rows, int c,
+                                 uint32_t (&w)[kRows]) {
+#pragma unroll
+  for (int t = 0; t < kRows; ++t)
+    w[t] = load_word<T, VEC>(p + (int64_t)min(r + t, rows - 1) * ld + c);
+}
+
+// Keeps what was computed from the words from being held across this place: a gate takes
+// fewer cycles to compute again than its two registers a row would cost in waves.
+__device__ inline void forget(uint32_t (&w)[kRows]) {
+#pragma unroll
+  for (int t = 0; t < kRows; ++t) asm volatile("" : "+v"(w[t]));
+}
+
+template <class T, int VEC>
+__global__ __launch_bounds__(kThreads) void recur_forward_kernel(RecurArgs a, Shape z,
+                                                                 Workspace ws, const T* x,
+                                                                 const T* g, T* y) {
+  __shared__ Block<VEC> sh;
+  const int w = threadIdx.x / 64, l = threadIdx.x % 64;
+  if (threadIdx.x == 0) sh.ticket = z.chunks > 1 ? (int)atomicAdd(ws.ticket, 1u) : blockIdx.x;
+  __syncthreads();
+  const int j = sh.ticket / z.tiles, tile = sh.ticket % z.tiles;
+  const int r0 = j * kChunk, r1 = min(a.rows, r0 + kChunk), r = r0 + w * kRows;
+  const int c = (tile * 64 + l) * VEC;
+  const bool on = c < a.d;
+  empty_sequences<VEC>(a, j, z.chunks, c, on, a.h0, a.h_last, tile == 0);
+  if (a.rows == 0) return;
+  uint32_t rx[kRows], rg[kRows];
+  load_rows<T, VEC>(x, a.ldx, r, a.rows, on ? c : 0, rx);
+  load_rows<T, VEC>(g, a.ldg, r, a.rows, on ? c : 0, rg);
+  find_borders<true>(sh, a, r0, r1);
+  const int border = l < kRows ? sh.start[w * kRows + l]
+                               : l < 2 * kRows ? sh.end[w * kRows + l - kRows] : 0;
+  const bool plain = __ballot(border != 0) == 0;
+  auto before = [&](int t, int v, float h) {  // the state that row t starts from
+    const int s = plain ? 0 : __builtin_amdgcn_readlane(border, t);
+    if (s == 0) return h;
+    return a.h0 && on ? a.h0[(int64_t)(s - 1) * a.d + c + v] : 0.f;
+  };
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    Pair p{1.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < kRows; ++t) {
       float f, i;
-      gate((float)g[t * a.ldg + c], f, i);
-      h = f * h + i * (float)x[t * a.ldx + c];
+      gate(part<T>(rg[t], v), f, i);
+      const bool first = !plain && __builtin_amdgcn_readlane(border, t) != 0;
+      p.b = fmaf(f, before(t, v, p.b), i * part<T>(rx[t], v));
+      p.a = first ? -0.f : f * p.a;
     }
-    for (int64_t t = hi - 1; t >= lo; --t) {
-      float f, i;
-      gate((float)g[t * a.ldg + c], f, i);
-      const float L = (float)dy[t * a.ldy + c] + m;
-      dx[t * a.lddx + c] = (T)(i * L);
-      dg[t * a.lddg + c] = (T)((before[t - lo][l] - (float)x[t * a.ldx + c]) * (f * i) * L);
-      m = f * L;
-    }
-    hi = lo;
+    sh.own[w][l * VEC + v] = make_float2(p.a, p.b);
   }
-  if (a.grad_h0) a.grad_h0[(int64_t)s * a.d + c] = m;
+  __syncthreads();
+  forget(rg);
+  float h[VEC];
+  come_in(sh, z, ws, j, sh.reach / kChunk, c, [](int k) { return k; }, h, a.status);
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    if (w == 0 && a.saved && on) a.saved[(int64_t)j * a.d + c + v] = h[v];
+    for (int k = 0; k < w; ++k) {
+      const float2 p = sh.own[k][l * VEC + v];
+      h[v] = through({p.x, p.y}, h[v]);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < kRows; ++t) {
+    T out[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      float f, i;
+      gate(part<T>(rg[t], v), f, i);
+      h[v] = fmaf(f, before(t, v, h[v]), i * part<T>(rx[t], v));
+      out[v] = (T)h[v];
+    }
+    const int row = r + t;
+    if (on && row >= sh.valid0 && row < min(sh.valid1, r1))
+      store_vec(y + (int64_t)row * a.ldy + c, out);
+    const int s = plain ? 0 : __builtin_amdgcn_readlane(border, kRows + t);
+    if (s && a.h_last && on)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) a.h_last[(int64_t)(s - 1) * a.d + c + v] = h[v];
+  }
+}
+
+template <class T, int VEC>
+__global__ __launch_bounds__(kThreads) void recur_backward_kernel(RecurArgs a, Shape z,
+                                                                  Workspace ws, const T* x,
+                                                                  const T* g, const T* dy, T* dx,
+                                                                  T* dg) {
+  __shared__ Block<VEC> sh;
+  const int w = threadIdx.x / 64, l = threadIdx.x % 64;
+  if (threadIdx.x == 0) sh.ticket = z.chunks > 1 ? (int)atomicAdd(ws.ticket, 1u) : blockIdx.x;
+  __syncthreads();
+  // from the last chunk to the first
+  const int j = sh.ticket / z.tiles, tile = sh.ticket % z.tiles, chunk = z.chunks - 1 - j;
+  const int r0 = chunk * kChunk, r1 = min(a.rows, r0 + kChunk), r = r0 + w * kRows;
+  const int c = (tile * 64 + l) * VEC;
+  const bool on = c < a.d;
+  empty_sequences<VEC>(a, chunk, z.chunks, c, on, a.grad_last, a.grad_h0, tile == 0);
+  if (a.rows == 0) return;
+  uint32_t rx[kRows], rg[kRows], ry[kRows];
+  load_rows<T, VEC>(x, a.ldx, r, a.rows, on ? c : 0, rx);
+  load_rows<T, VEC>(g, a.ldg, r, a.rows, on ? c : 0, rg);
+  load_rows<T, VEC>(dy, a.ldy, r, a.rows, on ? c : 0, ry);
+  float h[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) h[v] = on ? a.saved_in[(int64_t)chunk * a.d + c + v] : 0.f;
+  find_borders<false>(sh, a, r0, r1);
+  const int border = l < kRows ? sh.start[w * kRows + l]
+                               : l < 2 * kRows ? sh.end[w * kRows + l - kRows] : 0;
+  const bool plain = __ballot(border != 0) == 0;
+  auto state = [&](int at, const float* p, int v, float otherwise) {
+    const int s = plain ? 0 : __builtin_amdgcn_readlane(border, at);
+    if (s == 0) return otherwise;
+    return p && on ? p[(int64_t)(s - 1) * a.d + c + v] : 0.f;
+  };
+  auto flag = [&](int at) { return !plain && __builtin_amdgcn_readlane(border, at) != 0; };
+  // the states before the waves' rows
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    Pair p{1.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < kRows; ++t) {
+      float f, i;
+      gate(part<T>(rg[t], v), f, i);
+      p.b = fmaf(f, state(t, a.h0, v, p.b), i * part<T>(rx[t], v));
+      p.a = flag(t) ? -0.f : f * p.a;
+    }
+    sh.own[w][l * VEC + v] = make_float2(p.a, p.b);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < VEC; ++v)
+    for (int k = 0; k < w; ++k) {
+      const float2 p = sh.own[k][l * VEC + v];
+      h[v] = through({p.x, p.y}, h[v]);
+    }
+  __syncthreads();
+  forget(rg);
+  // what the gate's gradient is of L, and the waves' pairs from the end
+  float of[kRows][VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+#pragma unroll
+    for (int t = 0; t < kRows; ++t) {
+      float f, i;
+      gate(part<T>(rg[t], v), f, i);
+      const float b = state(t, a.h0, v, h[v]), in = part<T>(rx[t], v);
+      of[t][v] = (b - in) * (f * i);
+      h[v] = fmaf(f, b, i * in);
+    }
+    Pair p{1.f, 0.f};
+#pragma unroll
+    for (int t = kRows - 1; t >= 0; --t) {
+      float f, i;
+      gate(part<T>(rg[t], v), f, i);
+      p.b = f * (part<T>(ry[t], v) + state(kRows + t, a.grad_last, v, p.b));
+      p.a = flag(kRows + t) ? -0.f : f * p.a;
+    }
+    sh.own[w][l * VEC + v] = make_float2(p.a, p.b);
+  }
+  __syncthreads();
+  forget(rg);
+  float m[VEC];
+  come_in(sh, z, ws, j, z.chunks - 1 - sh.reach / kChunk, c,
+          [](int k) { return kWaves - 1 - k; }, m, a.status);
+#pragma unroll
+  for (int v = 0; v < VEC; ++v)
+    for (int k = kWaves - 1; k > w; --k) {
+      const float2 p = sh.own[k][l * VEC + v];
+      m[v] = through({p.x, p.y}, m[v]);
+    }
+#pragma unroll
+  for (int t = kRows - 1; t >= 0; --t) {
+    T ox[VEC], og[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      float f, i;
+      gate(part<T>(rg[t], v), f, i);
+      const float L = part<T>(ry[t], v) + state(kRows + t, a.grad_last, v, m[v]);
+      ox[v] = (T)(i * L);
+      og[v] = (T)(of[t][v] * L);
+      m[v] = f * L;
+    }
+    const int row = r + t;
+    if (on && row >= sh.valid0 && row < min(sh.valid1, r1)) {
+      store_vec(dx + (int64_t)row * a.lddx + c, ox);
+      store_vec(dg + (int64_t)row * a.lddg + c, og);
+    }
+    const int s = plain ? 0 : __builtin_amdgcn_readlane(border, t);
+    if (s && a.grad_h0 && on)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) a.grad_h0[(int64_t)(s - 1) * a.d + c + v] = m[v];
+  }
 }
 
 template <class T>
@@ -146,6 +577,32 @@ int check_recur(int dtype, int rows, int n_seq, int d, const void* x, int64_t ld
   return LST_OK;
 }
 
+// Calls run with the element type, the channels a lane, the shape and the workspace, cleared.
+template <class F>
+int with_shape(int dtype, int rows, int d, void* workspace, hipStream_t stream, F run) {
+  return with_dtype(dtype, [&](auto t) {
+    auto go = [&](auto vec) {
+      const Shape z = shape_of(rows, d, decltype(vec)::value);
+      if ((int64_t)z.chunks * z.tiles > 0x7FFFFFFF) return (int)LST_EINVAL;
+      Workspace ws{};
+      if (z.joined()) {
+        if (!workspace || ((uintptr_t)workspace & 15)) return (int)LST_EINVAL;
+        ws.ticket = (unsigned*)workspace;
+        ws.chunk = (unsigned long long*)((char*)workspace + kHead);
+        ws.group = ws.chunk + (int64_t)z.chunks * z.width;
+        hipLaunchKernelGGL(recur_clear_kernel, dim3((unsigned)((z.words() + 255) / 256)),
+                           dim3(256), 0, stream, ws.chunk, z.words(), ws.ticket);
+      }
+      run(t, vec, z, ws);
+      return launched();
+    };
+    // two channels a lane where they make up the 4 bytes that a lane loads
+    if constexpr (sizeof(t) == 2)
+      if (d % 2 == 0) return go(std::integral_constant<int, 2>{});
+    return go(std::integral_constant<int, 1>{});
+  });
+}
+
 }  // namespace
 }  // namespace lst
 
@@ -157,7 +614,11 @@ int64_t lst_recur_saved(int32_t rows, int32_t d) {
   return rows < 0 || d < 1 ? -1 : ((int64_t)rows + kChunk - 1) / kChunk * d;
 }
 
-int64_t lst_recur_workspace(int32_t rows, int32_t d) { return rows < 0 || d < 1 ? -1 : 0; }
+int64_t lst_recur_workspace(int32_t rows, int32_t d) {
+  if (rows < 0 || d < 1) return -1;
+  const Shape s = shape_of(rows, d, 2);  // as wide as with one channel a lane, or wider
+  return s.joined() ? kHead + s.words() * (int64_t)sizeof(unsigned long long) : 0;
+}
 
 int lst_recur_forward(int32_t dtype, int32_t rows, int32_t n_seq, int32_t d, const void* x,
                       int64_t ldx, const void* g, int64_t ldg, const int32_t* offsets,
@@ -171,11 +632,12 @@ int lst_recur_forward(int32_t dtype, int32_t rows, int32_t n_seq, int32_t d, con
   a.rows = rows, a.n_seq = n_seq, a.d = d;
   a.ldx = ldx, a.ldg = ldg, a.ldy = ldy;
   a.offsets = offsets, a.h0 = h0, a.h_last = h_last, a.saved = saved, a.status = status;
-  return with_dtype(dtype, [&](auto t) {
+  return with_shape(dtype, rows, d, workspace, (hipStream_t)hip_stream,
+                    [&](auto t, auto vec, const Shape& z, const Workspace& ws) {
     using T = decltype(t);
-    hipLaunchKernelGGL(recur_forward_kernel<T>, dim3(n_seq, (d + 63) / 64), dim3(64), 0,
-                       (hipStream_t)hip_stream, a, (const T*)x, (const T*)g, (T*)y);
-    return launched();
+    hipLaunchKernelGGL((recur_forward_kernel<T, decltype(vec)::value>),
+                       dim3((unsigned)(z.chunks * z.tiles)), dim3(kThreads), 0,
+                       (hipStream_t)hip_stream, a, z, ws, (const T*)x, (const T*)g, (T*)y);
   });
 }
 
@@ -195,12 +657,13 @@ int lst_recur_backward(int32_t dtype, int32_t rows, int32_t n_seq, int32_t d, co
   a.ldx = ldx, a.ldg = ldg, a.ldy = ldgy, a.lddx = ldgx, a.lddg = ldgg;
   a.offsets = offsets, a.h0 = h0, a.grad_last = grad_last, a.saved_in = saved;
   a.grad_h0 = grad_h0, a.status = status;
-  return with_dtype(dtype, [&](auto t) {
+  return with_shape(dtype, rows, d, workspace, (hipStream_t)hip_stream,
+                    [&](auto t, auto vec, const Shape& z, const Workspace& ws) {
     using T = decltype(t);
-    hipLaunchKernelGGL(recur_backward_kernel<T>, dim3(n_seq, (d + 63) / 64), dim3(64), 0,
-                       (hipStream_t)hip_stream, a, (const T*)x, (const T*)g, (const T*)grad_y,
-                       (T*)grad_x, (T*)grad_g);
-    return launched();
+    hipLaunchKernelGGL((recur_backward_kernel<T, decltype(vec)::value>),
+                       dim3((unsigned)(z.chunks * z.tiles)), dim3(kThreads), 0,
+                       (hipStream_t)hip_stream, a, z, ws, (const T*)x, (const T*)g,
+                       (const T*)grad_y, (T*)grad_x, (T*)grad_g);
   });
 }
 
