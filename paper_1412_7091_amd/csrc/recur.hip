@@ -15,7 +15,7 @@
 //
 // Both passes read each row once.  The packed rows are cut into chunks of 128,
 // whatever sequences they hold, and a block has one chunk of 64 or 128 channels:
-// eight waves of 16 rows, held in registers.  A row's map h -> f h + (1 - f) x, and
+// sixteen waves of 8 rows, held in registers.  A row's map h -> f h + (1 - f) x, and
 // so every stretch of rows, is a pair (A, B) with h -> A h + B.  The block publishes
 // the pair of its chunk, gathers those of the chunks before it, back to the one in
 // which the sequence of its first row begins, and only then runs over its rows.
@@ -71,6 +71,10 @@ __device__ inline void raise(int32_t* status) {
   if (status) atomicCAS(status, 0, LST_EINDEX);
 }
 
+// The wave's number, known to be the same for all of its lanes: row addresses stay in scalar
+// registers.
+__device__ inline int wave_of() { return __builtin_amdgcn_readfirstlane(threadIdx.x / 64); }
+
 // -------------------------------------------------------------- pairs (A, B)
 struct Pair {
   float a, b;
@@ -95,7 +99,7 @@ __device__ inline Pair unpack(unsigned long long v) {
 }
 
 // ------------------------------------------------------------- the workspace
-constexpr int kRows = 16;                    // rows a wave
+constexpr int kRows = 16;                     // rows a wave
 constexpr int kWaves = kChunk / kRows;       // waves a block
 constexpr int kThreads = 64 * kWaves;
 constexpr int kGroupChunks = 16;             // chunks whose pair is published together
@@ -139,21 +143,28 @@ struct Block {
   int ticket;
   int s0;     // first sequence that ends behind the first row
   int reach;  // first row (forward) or last row (backward) of the sequence that goes on
-  int valid0, valid1;  // rows of any sequence
+};
+
+// A thread's pair of offsets where there are no more sequences than threads, asked for before
+// the rows are: what is asked for later arrives later.
+struct Early {
+  int b, e;
+  __device__ explicit Early(const RecurArgs& a) : b(0x7FFFFFFF), e(0) {
+    if (a.offsets && a.n_seq <= kThreads && (int)threadIdx.x < a.n_seq) {
+      b = a.offsets[threadIdx.x];
+      e = a.offsets[threadIdx.x + 1];
+    }
+  }
 };
 
 // The sequences' borders among rows [r0, r1) of the chunk, and how far the sequence
 // that enters the chunk (forward: at its first row, else at its last) reaches.
 template <bool FORWARD, int VEC>
-__device__ void find_borders(Block<VEC>& sh, const RecurArgs& a, int r0, int r1) {
+__device__ void find_borders(Block<VEC>& sh, const RecurArgs& a, Early early, int r0, int r1) {
   const int tid = threadIdx.x, n = a.n_seq;
   if (tid < kChunk) sh.start[tid] = sh.end[tid] = 0;
   const int enter = FORWARD ? r0 : r1 - 1;
-  if (tid == 0) {
-    sh.reach = enter;
-    sh.valid0 = a.offsets ? a.offsets[0] : 0;
-    sh.valid1 = a.offsets ? a.offsets[n] : a.rows;
-  }
+  if (tid == 0) sh.reach = enter;
   auto mark = [&](int s, int b, int e) {
     if (b < 0 || b >= e || e > a.rows) return;
     if (b >= r0 && b < r1) sh.start[b - r0] = s + 1;
@@ -167,6 +178,12 @@ __device__ void find_borders(Block<VEC>& sh, const RecurArgs& a, int r0, int r1)
       const int s = (r0 + tid) / len;
       if (tid == 0 || (r0 + tid) % len == 0) mark(s, s * len, s * len + len);
     }
+    __syncthreads();
+    return;
+  }
+  if (n <= kThreads) {
+    __syncthreads();
+    mark(tid, early.b, early.e);
     __syncthreads();
     return;
   }
@@ -201,7 +218,7 @@ __device__ void empty_sequences(const RecurArgs& a, int chunk, int chunks, int c
                                 const float* from, float* to, bool check) {
   const int64_t n = a.n_seq;
   const int s0 = (int)(n * chunk / chunks), s1 = (int)(n * (chunk + 1) / chunks);
-  for (int s = s0 + (int)threadIdx.x / 64; s < s1; s += kWaves) {
+  for (int s = s0 + wave_of(); s < s1; s += kWaves) {
     int b = 0, e = 0;
     if (a.offsets) {
       b = a.offsets[s];
@@ -260,68 +277,55 @@ __device__ void gather(const unsigned long long* words, int64_t width, int64_t a
 // ORDER(w) the w-th of them in that direction.  Publishes the chunk's pair, and the
 // group's where it is complete.
 template <int VEC, class Order>
-__device__ void come_in(Block<VEC>& sh, const Shape& z, const Workspace& ws, int j, int j0,
+__device__ void come_in(Block<VEC>& sh, const Shape& z, Workspace ws, int j, int j0,
                         int64_t at, Order order, float (&carry)[VEC], int32_t* status) {
-  const int w = threadIdx.x / 64, l = threadIdx.x % 64;
+  const int w = wave_of(), l = threadIdx.x % 64;
 #pragma unroll
   for (int v = 0; v < VEC; ++v) carry[v] = 0.f;
   if (z.chunks == 1) return;
-  Pair all[VEC];
-  if (w == 0) {
+  if (w == 0)
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      all[v] = {1.f, 0.f};
-#pragma unroll
+      Pair all{1.f, 0.f};
+#pragma unroll 2
       for (int k = 0; k < kWaves; ++k) {
         const float2 p = sh.own[order(k)][l * VEC + v];
-        all[v] = join(all[v], {p.x, p.y});
+        all = join(all, {p.x, p.y});
       }
-      __hip_atomic_store(ws.chunk + (int64_t)j * z.width + at + v, pack(all[v]),
-                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(ws.chunk + (int64_t)j * z.width + at + v, pack(all), __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
     }
-  }
   const int group = j / kGroupChunks, g0 = group * kGroupChunks;
-  const bool closes = j % kGroupChunks == kGroupChunks - 1;
-  if (j0 >= j && !closes) return;
-  // half of the waves take the groups before, half the chunks of this group before; a block
-  // that closes its group publishes the group's pair before it waits for other groups
+  if (w == 0 && j % kGroupChunks == kGroupChunks - 1 && j + 1 + kGroupChunks < z.chunks) {
+    // before this block waits for other groups
+    Pair all[VEC];
+    gather<VEC>(ws.chunk, z.width, at, g0, j + 1, all, status);
+#pragma unroll
+    for (int v = 0; v < VEC; ++v)
+      __hip_atomic_store(ws.group + (int64_t)group * z.width + at + v, pack(all[v]),
+                         __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  if (j0 >= j) return;
+  // Half of the waves take the chunks of this group and the one before, half the groups
+  // before those: a group's pair comes later than its chunks', and by then it is there.
   constexpr int kHalf = kWaves / 2;
+  const int n0 = max(g0 - kGroupChunks, 0);  // the first chunk taken by itself
   const bool near = w >= kHalf;
-  const int first = near ? (closes ? g0 : max(g0, j0)) : min(j0 / kGroupChunks, group);
-  const int last = near ? j : (j0 < g0 ? group : first);
+  const int first = near ? max(n0, j0) : j0 / kGroupChunks;
+  const int last = near ? j : n0 / kGroupChunks;
   const int per = (max(last - first, 0) + kHalf - 1) / kHalf;
   const int from = first + (w % kHalf) * per, to = min(last, from + per);
-  auto collect = [&]() {
-    Pair p[VEC];
-    gather<VEC>(near ? ws.chunk : ws.group, z.width, at, from, to, p, status);
+  Pair p[VEC];
+  const unsigned long long *chunk = ws.chunk, *far = ws.group;
+  gather<VEC>(near ? chunk : far, z.width, at, from, to, p, status);
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) sh.far[w][l * VEC + v] = make_float2(p[v].a, p[v].b);
-  };
-  if (near || !closes) collect();
+  for (int v = 0; v < VEC; ++v) sh.far[w][l * VEC + v] = make_float2(p[v].a, p[v].b);
   __syncthreads();
-  if (closes) {
-    if (w == 0)
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        Pair p{1.f, 0.f};
-#pragma unroll
-        for (int k = kHalf; k < kWaves; ++k) {
-          const float2 q = sh.far[k][l * VEC + v];
-          p = join(p, {q.x, q.y});
-        }
-        __hip_atomic_store(ws.group + (int64_t)group * z.width + at + v, pack(join(p, all[v])),
-                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      }
-    if (j0 >= j) return;
-    if (!near) collect();
-    __syncthreads();
-  }
 #pragma unroll
   for (int v = 0; v < VEC; ++v)
-#pragma unroll
+#pragma unroll 2
     for (int k = 0; k < kWaves; ++k) {
       const float2 q = sh.far[k][l * VEC + v];
-      // what a closing block gathered before the sequence's chunk ends at its first row
       carry[v] = through({q.x, q.y}, carry[v]);
     }
 }
@@ -349,7 +353,7 @@ __device__ inline void load_rows(const T* p, int64_t ld, int r, int rows, int c,
                                  uint32_t (&w)[kRows]) {
 #pragma unroll
   for (int t = 0; t < kRows; ++t)
-    w[t] = load_word<T, VEC>(p + (int64_t)min(r + t, rows - 1) * ld + c);
+    w[t] = load_word<T, VEC>(p + (int64_t)min(r + t, rows - 1) * ld + (uint32_t)c);
 }
 
 // Keeps what was computed from the words from being held across this place: a gate takes
@@ -359,187 +363,287 @@ __device__ inline void forget(uint32_t (&w)[kRows]) {
   for (int t = 0; t < kRows; ++t) asm volatile("" : "+v"(w[t]));
 }
 
+// The borders among a wave's rows, and the states that its sequences start from (or the
+// gradients that they end with), the first two of them loaded ahead.
+template <int VEC>
+struct Borders {
+  uint32_t start, end;  // a bit a row
+  int seq;              // lane t: 1 + the sequence that starts in row t, lane 16 + t: that ends
+  int first, last;      // rows [first, last) belong to sequences,
+  bool whole;           // all of the wave's among them
+
+  __device__ bool holds(int row) const { return whole || (row >= first && row < last); }
+  __device__ int starts(int t) const { return __builtin_amdgcn_readlane(seq, t) - 1; }
+  __device__ int ends(int t) const { return __builtin_amdgcn_readlane(seq, kRows + t) - 1; }
+};
+
+template <int VEC>
+__device__ inline Borders<VEC> borders_of(const Block<VEC>& sh, const RecurArgs& a, int w,
+                                          int r, int r1) {
+  const int l = threadIdx.x % 64;
+  Borders<VEC> b;
+  b.seq = l < kRows ? sh.start[w * kRows + l]
+                    : l < 2 * kRows ? sh.end[w * kRows + l - kRows] : 0;
+  const uint64_t any = __ballot(b.seq != 0);
+  b.start = (uint32_t)any & ((1u << kRows) - 1);
+  b.end = (uint32_t)any >> kRows;
+  b.first = a.offsets ? a.offsets[0] : 0;
+  b.last = min(a.offsets ? a.offsets[a.n_seq] : a.rows, r1);
+  b.whole = r >= b.first && r + kRows <= b.last;
+  return b;
+}
+
+// n_seq x d floats (null: zeros), one row of them for each bit of `mask`.  The first and the
+// last one are loaded ahead: a wave has rarely more, and those between belong to sequences
+// that begin and end among the wave's own rows (so that one buffer for the states at both
+// ends is read before it is written).
+template <int VEC, bool END>
+struct States {
+  const float* p;
+  int64_t d;
+  uint32_t mask;
+  float first[VEC], last[VEC];
+
+  __device__ void load(const Borders<VEC>& b, int t, float (&out)[VEC]) const {
+    const float* q = p + (int64_t)(END ? b.ends(t) : b.starts(t)) * d;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) out[v] = p ? q[v] : 0.f;
+  }
+  __device__ States(const float* p_, int64_t d_, const Borders<VEC>& b, int c, bool on)
+      : p(on && p_ ? p_ + c : nullptr), d(d_), mask(END ? b.end : b.start) {
+    if (!mask) return;
+    load(b, __builtin_ctz(mask), first);
+    if (mask & (mask - 1)) load(b, 31 - __builtin_clz(mask), last);
+  }
+  // h becomes, in a row of the mask, what stands for it
+  __device__ void replace(const Borders<VEC>& b, int t, float (&h)[VEC]) const {
+    const uint32_t bit = 1u << t;
+    if (!(mask & bit)) return;
+    if (!(mask & (bit - 1))) {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) h[v] = first[v];
+    } else if (mask < 2 * bit) {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) h[v] = last[v];
+    } else {
+      load(b, t, h);
+    }
+  }
+};
+
+// A wave's rows in registers, gone through forwards or backwards.
+template <class T, int VEC>
+struct Rows {
+  uint32_t g[kRows];
+
+  // each(t, f, 1 - f) for every row, after h has become the state that the row starts from
+  // (END: the gradient that comes into it) where a sequence does.
+  template <bool END, class Each>
+  __device__ void walk(const Borders<VEC>& b, const States<VEC, END>& states, float (&h)[VEC],
+                       Each each) const {
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const int t = END ? kRows - 1 - k : k;
+      states.replace(b, t, h);
+      float f[VEC], i[VEC];
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) gate(part<T>(g[t], v), f[v], i[v]);
+      each(t, f, i);
+      // four rows' gates at a time: the scheduler would hold all of them
+      if (k % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+};
+
 template <class T, int VEC>
 __global__ __launch_bounds__(kThreads) void recur_forward_kernel(RecurArgs a, Shape z,
-                                                                 Workspace ws, const T* x,
-                                                                 const T* g, T* y) {
+                                                                    Workspace ws, const T* x,
+                                                                    const T* g, T* y) {
   __shared__ Block<VEC> sh;
-  const int w = threadIdx.x / 64, l = threadIdx.x % 64;
+  const int w = wave_of(), l = threadIdx.x % 64;
   if (threadIdx.x == 0) sh.ticket = z.chunks > 1 ? (int)atomicAdd(ws.ticket, 1u) : blockIdx.x;
   __syncthreads();
-  const int j = sh.ticket / z.tiles, tile = sh.ticket % z.tiles;
+  const int ticket = __builtin_amdgcn_readfirstlane(sh.ticket);
+  const int j = ticket / z.tiles, tile = ticket % z.tiles;
   const int r0 = j * kChunk, r1 = min(a.rows, r0 + kChunk), r = r0 + w * kRows;
   const int c = (tile * 64 + l) * VEC;
   const bool on = c < a.d;
-  empty_sequences<VEC>(a, j, z.chunks, c, on, a.h0, a.h_last, tile == 0);
-  if (a.rows == 0) return;
-  uint32_t rx[kRows], rg[kRows];
-  load_rows<T, VEC>(x, a.ldx, r, a.rows, on ? c : 0, rx);
-  load_rows<T, VEC>(g, a.ldg, r, a.rows, on ? c : 0, rg);
-  find_borders<true>(sh, a, r0, r1);
-  const int border = l < kRows ? sh.start[w * kRows + l]
-                               : l < 2 * kRows ? sh.end[w * kRows + l - kRows] : 0;
-  const bool plain = __ballot(border != 0) == 0;
-  auto before = [&](int t, int v, float h) {  // the state that row t starts from
-    const int s = plain ? 0 : __builtin_amdgcn_readlane(border, t);
-    if (s == 0) return h;
-    return a.h0 && on ? a.h0[(int64_t)(s - 1) * a.d + c + v] : 0.f;
-  };
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) {
-    Pair p{1.f, 0.f};
-#pragma unroll
-    for (int t = 0; t < kRows; ++t) {
-      float f, i;
-      gate(part<T>(rg[t], v), f, i);
-      const bool first = !plain && __builtin_amdgcn_readlane(border, t) != 0;
-      p.b = fmaf(f, before(t, v, p.b), i * part<T>(rx[t], v));
-      p.a = first ? -0.f : f * p.a;
-    }
-    sh.own[w][l * VEC + v] = make_float2(p.a, p.b);
+  if (a.rows == 0) {
+    empty_sequences<VEC>(a, j, z.chunks, c, on, a.h0, a.h_last, tile == 0);
+    return;
   }
+  const Early early(a);
+  uint32_t rx[kRows];
+  Rows<T, VEC> rows;
+  load_rows<T, VEC>(x, a.ldx, r, a.rows, on ? c : 0, rx);
+  load_rows<T, VEC>(g, a.ldg, r, a.rows, on ? c : 0, rows.g);
+  find_borders<true>(sh, a, early, r0, r1);
+  const Borders<VEC> b = borders_of<VEC>(sh, a, w, r, r1);
+  const States<VEC, false> first(a.h0, a.d, b, c, on);
+  float h[VEC], prod[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) h[v] = 0.f, prod[v] = 1.f;
+  rows.template walk<false>(
+      b, first, h, [&](int t, const float(&f)[VEC], const float(&i)[VEC]) {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          h[v] = fmaf(f[v], h[v], i[v] * part<T>(rx[t], v));
+          prod[v] *= f[v];
+        }
+      });
+#pragma unroll
+  for (int v = 0; v < VEC; ++v)
+    sh.own[w][l * VEC + v] = make_float2(b.start ? -0.f : prod[v], h[v]);
   __syncthreads();
-  forget(rg);
-  float h[VEC];
+  forget(rows.g);
   come_in(sh, z, ws, j, sh.reach / kChunk, c, [](int k) { return k; }, h, a.status);
 #pragma unroll
   for (int v = 0; v < VEC; ++v) {
     if (w == 0 && a.saved && on) a.saved[(int64_t)j * a.d + c + v] = h[v];
+#pragma unroll 2
     for (int k = 0; k < w; ++k) {
       const float2 p = sh.own[k][l * VEC + v];
       h[v] = through({p.x, p.y}, h[v]);
     }
   }
+  rows.template walk<false>(
+      b, first, h, [&](int t, const float(&f)[VEC], const float(&i)[VEC]) {
+        T out[VEC];
 #pragma unroll
-  for (int t = 0; t < kRows; ++t) {
-    T out[VEC];
+        for (int v = 0; v < VEC; ++v) {
+          h[v] = fmaf(f[v], h[v], i[v] * part<T>(rx[t], v));
+          out[v] = (T)h[v];
+        }
+        const int row = r + t;
+        if (on && b.holds(row))
+          store_vec(y + (int64_t)row * a.ldy + (uint32_t)c, out);
+        if ((b.end >> t & 1) && a.h_last && on)
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      float f, i;
-      gate(part<T>(rg[t], v), f, i);
-      h[v] = fmaf(f, before(t, v, h[v]), i * part<T>(rx[t], v));
-      out[v] = (T)h[v];
-    }
-    const int row = r + t;
-    if (on && row >= sh.valid0 && row < min(sh.valid1, r1))
-      store_vec(y + (int64_t)row * a.ldy + c, out);
-    const int s = plain ? 0 : __builtin_amdgcn_readlane(border, kRows + t);
-    if (s && a.h_last && on)
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) a.h_last[(int64_t)(s - 1) * a.d + c + v] = h[v];
-  }
+            for (int v = 0; v < VEC; ++v)
+              a.h_last[(int64_t)b.ends(t) * a.d + c + v] = h[v];
+      });
+  empty_sequences<VEC>(a, j, z.chunks, c, on, a.h0, a.h_last, tile == 0);
 }
 
 template <class T, int VEC>
 __global__ __launch_bounds__(kThreads) void recur_backward_kernel(RecurArgs a, Shape z,
-                                                                  Workspace ws, const T* x,
-                                                                  const T* g, const T* dy, T* dx,
-                                                                  T* dg) {
+                                                                     Workspace ws, const T* x,
+                                                                     const T* g, const T* dy,
+                                                                     T* dx, T* dg) {
   __shared__ Block<VEC> sh;
-  const int w = threadIdx.x / 64, l = threadIdx.x % 64;
+  const int w = wave_of(), l = threadIdx.x % 64;
   if (threadIdx.x == 0) sh.ticket = z.chunks > 1 ? (int)atomicAdd(ws.ticket, 1u) : blockIdx.x;
   __syncthreads();
+  const int ticket = __builtin_amdgcn_readfirstlane(sh.ticket);
   // from the last chunk to the first
-  const int j = sh.ticket / z.tiles, tile = sh.ticket % z.tiles, chunk = z.chunks - 1 - j;
+  const int j = ticket / z.tiles, tile = ticket % z.tiles, chunk = z.chunks - 1 - j;
   const int r0 = chunk * kChunk, r1 = min(a.rows, r0 + kChunk), r = r0 + w * kRows;
   const int c = (tile * 64 + l) * VEC;
   const bool on = c < a.d;
-  empty_sequences<VEC>(a, chunk, z.chunks, c, on, a.grad_last, a.grad_h0, tile == 0);
-  if (a.rows == 0) return;
-  uint32_t rx[kRows], rg[kRows], ry[kRows];
-  load_rows<T, VEC>(x, a.ldx, r, a.rows, on ? c : 0, rx);
-  load_rows<T, VEC>(g, a.ldg, r, a.rows, on ? c : 0, rg);
-  load_rows<T, VEC>(dy, a.ldy, r, a.rows, on ? c : 0, ry);
-  float h[VEC];
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) h[v] = on ? a.saved_in[(int64_t)chunk * a.d + c + v] : 0.f;
-  find_borders<false>(sh, a, r0, r1);
-  const int border = l < kRows ? sh.start[w * kRows + l]
-                               : l < 2 * kRows ? sh.end[w * kRows + l - kRows] : 0;
-  const bool plain = __ballot(border != 0) == 0;
-  auto state = [&](int at, const float* p, int v, float otherwise) {
-    const int s = plain ? 0 : __builtin_amdgcn_readlane(border, at);
-    if (s == 0) return otherwise;
-    return p && on ? p[(int64_t)(s - 1) * a.d + c + v] : 0.f;
-  };
-  auto flag = [&](int at) { return !plain && __builtin_amdgcn_readlane(border, at) != 0; };
-  // the states before the waves' rows
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) {
-    Pair p{1.f, 0.f};
-#pragma unroll
-    for (int t = 0; t < kRows; ++t) {
-      float f, i;
-      gate(part<T>(rg[t], v), f, i);
-      p.b = fmaf(f, state(t, a.h0, v, p.b), i * part<T>(rx[t], v));
-      p.a = flag(t) ? -0.f : f * p.a;
-    }
-    sh.own[w][l * VEC + v] = make_float2(p.a, p.b);
+  if (a.rows == 0) {
+    empty_sequences<VEC>(a, chunk, z.chunks, c, on, a.grad_last, a.grad_h0, tile == 0);
+    return;
   }
-  __syncthreads();
+  const Early early(a);
+  uint32_t rx[kRows], ry[kRows];
+  Rows<T, VEC> rows;
+  load_rows<T, VEC>(x, a.ldx, r, a.rows, on ? c : 0, rx);
+  load_rows<T, VEC>(g, a.ldg, r, a.rows, on ? c : 0, rows.g);
+  load_rows<T, VEC>(dy, a.ldy, r, a.rows, on ? c : 0, ry);
+  float before[VEC];  // the state before the chunk
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) before[v] = on ? a.saved_in[(int64_t)chunk * a.d + c + v] : 0.f;
+  find_borders<false>(sh, a, early, r0, r1);
+  const Borders<VEC> b = borders_of<VEC>(sh, a, w, r, r1);
+  const States<VEC, false> first(a.h0, a.d, b, c, on);
+  const States<VEC, true> last(a.grad_last, a.d, b, c, on);
+  float h[VEC], prod[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) h[v] = 0.f, prod[v] = 1.f;
+  rows.template walk<false>(
+      b, first, h, [&](int t, const float(&f)[VEC], const float(&i)[VEC]) {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          h[v] = fmaf(f[v], h[v], i[v] * part<T>(rx[t], v));
+          prod[v] *= f[v];
+        }
+      });
 #pragma unroll
   for (int v = 0; v < VEC; ++v)
+    sh.own[w][l * VEC + v] = make_float2(b.start ? -0.f : prod[v], h[v]);
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    h[v] = before[v];
+#pragma unroll 2
     for (int k = 0; k < w; ++k) {
       const float2 p = sh.own[k][l * VEC + v];
       h[v] = through({p.x, p.y}, h[v]);
     }
-  __syncthreads();
-  forget(rg);
-  // what the gate's gradient is of L, and the waves' pairs from the end
-  float of[kRows][VEC];
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) {
-#pragma unroll
-    for (int t = 0; t < kRows; ++t) {
-      float f, i;
-      gate(part<T>(rg[t], v), f, i);
-      const float b = state(t, a.h0, v, h[v]), in = part<T>(rx[t], v);
-      of[t][v] = (b - in) * (f * i);
-      h[v] = fmaf(f, b, i * in);
-    }
-    Pair p{1.f, 0.f};
-#pragma unroll
-    for (int t = kRows - 1; t >= 0; --t) {
-      float f, i;
-      gate(part<T>(rg[t], v), f, i);
-      p.b = f * (part<T>(ry[t], v) + state(kRows + t, a.grad_last, v, p.b));
-      p.a = flag(kRows + t) ? -0.f : f * p.a;
-    }
-    sh.own[w][l * VEC + v] = make_float2(p.a, p.b);
   }
   __syncthreads();
-  forget(rg);
-  float m[VEC];
+  forget(rows.g);
+  forget(rx);
+  // what the gates' gradients are of L, and the waves' pairs from the end
+  float of[kRows][VEC], m[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) m[v] = 0.f, prod[v] = 1.f;
+  rows.template walk<false>(
+      b, first, h, [&](int t, const float(&f)[VEC], const float(&i)[VEC]) {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          const float in = part<T>(rx[t], v);
+          of[t][v] = (h[v] - in) * (f[v] * i[v]);
+          asm volatile("" : "+v"(of[t][v]));  // the product, not its three factors
+          h[v] = fmaf(f[v], h[v], i[v] * in);
+        }
+      });
+  forget(rows.g);
+  forget(ry);
+  rows.template walk<true>(
+      b, last, m, [&](int t, const float(&f)[VEC], const float(&)[VEC]) {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          m[v] = f[v] * (part<T>(ry[t], v) + m[v]);
+          prod[v] *= f[v];
+        }
+      });
+#pragma unroll
+  for (int v = 0; v < VEC; ++v)
+    sh.own[w][l * VEC + v] = make_float2(b.end ? -0.f : prod[v], m[v]);
+  __syncthreads();
+  forget(rows.g);
+  forget(ry);
   come_in(sh, z, ws, j, z.chunks - 1 - sh.reach / kChunk, c,
           [](int k) { return kWaves - 1 - k; }, m, a.status);
 #pragma unroll
   for (int v = 0; v < VEC; ++v)
+#pragma unroll 2
     for (int k = kWaves - 1; k > w; --k) {
       const float2 p = sh.own[k][l * VEC + v];
       m[v] = through({p.x, p.y}, m[v]);
     }
+  rows.template walk<true>(
+      b, last, m, [&](int t, const float(&f)[VEC], const float(&i)[VEC]) {
+        T ox[VEC], og[VEC];
 #pragma unroll
-  for (int t = kRows - 1; t >= 0; --t) {
-    T ox[VEC], og[VEC];
+        for (int v = 0; v < VEC; ++v) {
+          const float L = part<T>(ry[t], v) + m[v];
+          ox[v] = (T)(i[v] * L);
+          og[v] = (T)(of[t][v] * L);
+          m[v] = f[v] * L;
+        }
+        const int row = r + t;
+        if (on && b.holds(row)) {
+          store_vec(dx + (int64_t)row * a.lddx + (uint32_t)c, ox);
+          store_vec(dg + (int64_t)row * a.lddg + (uint32_t)c, og);
+        }
+        if ((b.start >> t & 1) && a.grad_h0 && on)
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      float f, i;
-      gate(part<T>(rg[t], v), f, i);
-      const float L = part<T>(ry[t], v) + state(kRows + t, a.grad_last, v, m[v]);
-      ox[v] = (T)(i * L);
-      og[v] = (T)(of[t][v] * L);
-      m[v] = f * L;
-    }
-    const int row = r + t;
-    if (on && row >= sh.valid0 && row < min(sh.valid1, r1)) {
-      store_vec(dx + (int64_t)row * a.lddx + c, ox);
-      store_vec(dg + (int64_t)row * a.lddg + c, og);
-    }
-    const int s = plain ? 0 : __builtin_amdgcn_readlane(border, t);
-    if (s && a.grad_h0 && on)
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) a.grad_h0[(int64_t)(s - 1) * a.d + c + v] = m[v];
-  }
+            for (int v = 0; v < VEC; ++v)
+              a.grad_h0[(int64_t)b.starts(t) * a.d + c + v] = m[v];
+      });
+  empty_sequences<VEC>(a, chunk, z.chunks, c, on, a.grad_last, a.grad_h0, tile == 0);
 }
 
 template <class T>
