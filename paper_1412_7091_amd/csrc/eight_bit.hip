@@ -14,21 +14,27 @@
 // of the largest product that is summed with it (measured: a product of 2^2 beside
 // one of 2^16), which is an error of 1.2e-5 in the sums of 128 ordinary products.
 //
-// The rows of H are quantised in the same way by a launch of their own, and left in
-// bfloat16: they are few, and every wave reads them.
+// The rows of H are quantised in the same way and left in bfloat16, in the order in
+// which the matrix instruction takes them: a fragment, 16 rows by 32 columns, is 64
+// lanes of 16 bytes.
+#include <algorithm>
+
 #include "dtypes.h"
+#include "gemm_tile.h"
 
 namespace lst {
 namespace {
 
 constexpr int kBlock = 128;
 
+constexpr int kFragment = 64 * 8;          // bfloat16 of a fragment: 16 rows, 32 columns
+constexpr int kTile = 4 * kFragment;       // of 16 rows of one block
+
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Biased exponent of the scale for the bits of a block's largest finite magnitude:
 // 448 = 1.75 2^8, so 1.f 2^E needs 2^(E - 8) when 1.f <= 1.75, else 2^(E - 7).
@@ -63,24 +69,16 @@ __device__ inline bf16x8 widen(uintx2 q, float scale) {
   return f;
 }
 
-// 16 lanes a block, eight columns a lane.  Bound by memory: 793 471 x 300 floats (1.26 GB
-// with the codes) take 213 us, 5.9 TB/s; 32 lanes a block, four columns a lane with an access
-// for each, took 305 us.  WIDE: the values in bfloat16 instead of codes.
-template <class T, class I, bool WIDE>
-__global__ __launch_bounds__(256) void quantize_kernel(const T* x, int64_t ldx, int64_t rows,
-                                                       int cols, int blocks, void* codes,
-                                                       uint8_t* scales) {
-  const I at = (I)blockIdx.x * 16 + threadIdx.x / 16;  // the block
-  if (at >= (I)(rows * blocks)) return;
-  const I row = at / (I)blocks;
-  const int l = threadIdx.x % 16, col = (int)(at - row * (I)blocks) * kBlock + 8 * l;
-  const T* p = x + (int64_t)row * ldx + col;
+// Eight columns from `col` of a row, a block being in 16 neighbouring lanes: their codes and
+// the block's biased exponent.
+template <class T>
+__device__ inline void block_codes(const T* row, int col, int cols, uint32_t (&q)[2], int& e) {
   T raw[8];
   if (col + 8 <= cols) {
-    load_vec(p, raw);
+    load_vec(row + col, raw);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) raw[i] = col + i < cols ? p[i] : (T)0.f;
+    for (int i = 0; i < 8; ++i) raw[i] = col + i < cols ? row[col + i] : (T)0.f;
   }
   float v[8];
   uint32_t big = 0;  // largest magnitude, by its bits
@@ -89,7 +87,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const T* x, int64_t ldx, 
     v[i] = (float)raw[i];
     big = max(big, __float_as_uint(v[i]) & 0x7FFFFFFFu);
   }
-  uint64_t bad = 0;  // lanes' bytes that are no number in e4m3
+  uint64_t bad = 0;  // bytes that are no number in e4m3
   if (big >= 0x7F800000u) {
     big = 0;
     for (int i = 0; i < 8; ++i) {
@@ -104,78 +102,206 @@ __global__ __launch_bounds__(256) void quantize_kernel(const T* x, int64_t ldx, 
   }
 #pragma unroll
   for (int o = 8; o; o >>= 1) big = max(big, (uint32_t)__shfl_xor((int)big, o));
-  const int e = scale_of(big);
-  uint32_t q[2];
+  e = scale_of(big);
   codes_of(v, e, q);
   q[0] |= (uint32_t)bad;
   q[1] |= (uint32_t)(bad >> 32);
-  if constexpr (WIDE) {
-    reinterpret_cast<bf16x8*>(codes)[(int64_t)at * 16 + l] =
-        widen(uintx2{q[0], q[1]}, scale_value(e));
+}
+
+// 16 lanes a block, eight columns a lane.  Bound by memory: 793 471 x 300 floats (1.26 GB
+// with the codes) take 213 us, 5.9 TB/s; 32 lanes a block, four columns a lane with an access
+// for each, took 305 us.
+template <class T, class I>
+__global__ __launch_bounds__(256) void quantize_kernel(const T* x, int64_t ldx, int64_t rows,
+                                                       int cols, int blocks, uint8_t* codes,
+                                                       uint8_t* scales) {
+  const I at = (I)blockIdx.x * 16 + threadIdx.x / 16;  // the block
+  if (at >= (I)(rows * blocks)) return;
+  const I row = at / (I)blocks;
+  const int l = threadIdx.x % 16, col = (int)(at - row * (I)blocks) * kBlock + 8 * l;
+  uint32_t q[2];
+  int e;
+  block_codes(x + (int64_t)row * ldx, col, cols, q, e);
+  reinterpret_cast<uintx2*>(codes)[(int64_t)at * 16 + l] = uintx2{q[0], q[1]};
+  if (l == 0) scales[at] = (uint8_t)e;
+}
+
+// Where the eight columns of lane l of a block belong among the fragments of 16 rows.  Lane q
+// of four takes columns 16 q .. 16 q + 15 of each half of a block: which columns one
+// instruction adds up is free as long as both sides agree, and a wave then reads 64
+// contiguous bytes of each row of codes at a time.
+__device__ inline int fragment_at(int n16, int l) {
+  const int s = l % 2 + 2 * (l / 8), q = l / 2 % 4;
+  return s * kFragment + (q * 16 + n16) * 8;
+}
+
+// Rows of H into fragments, tiles of 16 rows of one block: tile (b, n / 16) of the workspace.
+// Rows behind the last one of the last tile are zeros.
+template <class T>
+__global__ __launch_bounds__(256) void fragments_kernel(const T* x, int64_t ldx, int m, int cols,
+                                                        int blocks, int tiles, __bf16* out) {
+  const int at = blockIdx.x * 16 + threadIdx.x / 16;
+  if (at >= tiles * 16 * blocks) return;
+  const int n = at / blocks, b = at - n * blocks, l = threadIdx.x % 16;
+  uint32_t q[2] = {0, 0};
+  int e = 0;
+  if (n < m) block_codes(x + (int64_t)n * ldx, b * kBlock + 8 * l, cols, q, e);
+  __bf16* p = out + ((int64_t)b * tiles + n / 16) * kTile + fragment_at(n % 16, l);
+  *reinterpret_cast<bf16x8*>(p) = widen(uintx2{q[0], q[1]}, scale_value(e));
+}
+
+// A lane's codes of one block of a row of W, and their scale.
+struct Codes {
+  uintx4 lo, hi;
+  int e;
+  __device__ void load(const uint8_t* w, const uint8_t* scale) {
+    lo = *reinterpret_cast<const uintx4*>(w);
+    hi = *reinterpret_cast<const uintx4*>(w + 64);
+    e = *scale;
+  }
+  __device__ bf16x8 fragment(int s) const {
+    const uintx4 c = s < 2 ? lo : hi;
+    return widen(uintx2{c[s % 2 * 2], c[s % 2 * 2 + 1]}, scale_value(e));
+  }
+};
+
+// The sums of 16 rows of W (from r) and 16 rows of H (from n): four rows of W a lane.
+template <class T>
+__device__ inline void store_tile(T* O, int64_t ldo, int m, int64_t D, int n, int64_t r,
+                                  f32x4 acc) {
+  if (n >= m || r >= D) return;
+  T* o = O + n * ldo + r;
+  T v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (T)acc[i];
+  if (r + 4 <= D) {
+    store_vec(o, v);
   } else {
-    reinterpret_cast<uintx2*>(codes)[(int64_t)at * 16 + l] = uintx2{q[0], q[1]};
-    if (l == 0) scales[at] = (uint8_t)e;
+    for (int i = 0; i < 4; ++i)
+      if (r + i < D) o[i] = v[i];
   }
 }
 
-// 16 rows of W and 16 NT rows of H a wave; four waves a block on neighbouring rows.
-template <class T, int NT>
-__global__ __launch_bounds__(256) void scores_kernel(const uint8_t* W, const uint8_t* sw,
+// At most 16 rows of H: one launch.  Every block quantises them by itself, into LDS, and its
+// waves go through tiles of 16 rows of W, four blocks' codes under way at a time.
+template <class TH, class T>
+__global__ __launch_bounds__(512) void scores_few_kernel(const TH* H, int64_t ldh, int d,
+                                                         const uint8_t* W, const uint8_t* sw,
+                                                         int m, int64_t D, int blocks, T* O,
+                                                         int64_t ldo) {
+  extern __shared__ __attribute__((aligned(16))) __bf16 few_lds[];
+  const int l = threadIdx.x % 64, i16 = l % 16, q4 = l / 16;
+  for (int at = threadIdx.x / 16; at < 16 * blocks; at += 512 / 16) {
+    const int n = at / blocks, b = at - n * blocks, c = threadIdx.x % 16;
+    uint32_t q[2] = {0, 0};
+    int e = 0;
+    if (n < m) block_codes(H + n * ldh, b * kBlock + 8 * c, d, q, e);
+    *reinterpret_cast<bf16x8*>(few_lds + b * kTile + fragment_at(n, c)) =
+        widen(uintx2{q[0], q[1]}, scale_value(e));
+  }
+  __syncthreads();
+  const int64_t ld = (int64_t)blocks * kBlock, tiles = (D + 15) / 16;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  for (int64_t tile = (int64_t)blockIdx.x * 8 + w; tile < tiles; tile += (int64_t)gridDim.x * 8) {
+    const int64_t row = min(tile * 16 + i16, D - 1);
+    const uint8_t *p = W + row * ld + 16 * q4, *ps = sw + row * blocks;
+    f32x4 acc = {};
+    for (int b0 = 0; b0 < blocks; b0 += 4) {
+      Codes c[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int b = min(b0 + j, blocks - 1);
+        c[j].load(p + b * kBlock, ps + b);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (b0 + j < blocks)
+#pragma unroll
+          for (int s = 0; s < 4; ++s) {
+            const bf16x8 h = *reinterpret_cast<const bf16x8*>(few_lds + (b0 + j) * kTile +
+                                                              s * kFragment + l * 8);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c[j].fragment(s), h, acc, 0, 0, 0);
+          }
+    }
+    store_tile(O, ldo, m, D, i16, tile * 16 + 4 * q4, acc);
+  }
+}
+
+// 16 MT rows of W a wave, four waves a block one after another, 16 NT rows of H a block.  A
+// block of H's columns goes to LDS by DMA while the one before is multiplied; the codes of a
+// wave's own rows go to registers.
+template <class T, int MT, int NT>
+__global__ __launch_bounds__(256, 2) void scores_kernel(const uint8_t* W, const uint8_t* sw,
                                                      const __bf16* H, int m, int64_t D,
-                                                     int blocks, T* O, int64_t ldo) {
-  const int l = threadIdx.x % 64, i16 = l % 16, q = l / 16;
-  const int64_t r0 = ((int64_t)blockIdx.x * 4 + threadIdx.x / 64) * 16;
-  const int n0 = blockIdx.y * 16 * NT;
-  if (r0 >= D) return;
-  const int64_t row = min(r0 + i16, D - 1);
-  const int64_t ld = (int64_t)blocks * kBlock;
-  floatx4 acc[NT] = {};
+                                                     int blocks, int row_blocks, T* O,
+                                                     int64_t ldo) {
+  __shared__ __attribute__((aligned(16))) __bf16 hb[2][NT * kTile];
+  const int l = threadIdx.x % 64, i16 = l % 16, q4 = l / 16;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  // the blocks of the same rows of W follow each other on one XCD, and share its L2
+  const int tiles = (m + 15) / 16, cols = (tiles + NT - 1) / NT;
+  const int xcd = blockIdx.x % 8, i = blockIdx.x / 8;
+  const int row_block = i / cols * 8 + xcd, t0 = i % cols * NT;
+  if (row_block >= row_blocks) return;
+  const int64_t r0 = ((int64_t)row_block * 4 + w) * 16 * MT, ld = (int64_t)blocks * kBlock;
+  const uint8_t *p[MT], *ps[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int64_t row = min(r0 + 16 * t + i16, D - 1);
+    p[t] = W + row * ld + 16 * q4;
+    ps[t] = sw + row * blocks;
+  }
+  auto fetch = [&](int b) {  // NT tiles of 4 KB, a quarter of them a wave
+#pragma unroll
+    for (int k = 0; k < NT; ++k) {
+      const int piece = w * NT + k, t = min(t0 + piece / 4, tiles - 1);
+      dma16((const float*)(H + ((int64_t)b * tiles + t) * kTile + piece % 4 * kFragment + l * 8),
+            lds_u32(&hb[b % 2][piece * kFragment]));
+    }
+  };
+  f32x4 acc[MT][NT] = {};
+  Codes next[MT];
+  fetch(0);
+#pragma unroll
+  for (int t = 0; t < MT; ++t) next[t].load(p[t], ps[t]);
   for (int b = 0; b < blocks; ++b) {
-    // the order of k within a block is free as long as both sides have the same
-    const uint8_t* w = W + row * ld + b * kBlock + 16 * q;
-    const uintx4 lo = *reinterpret_cast<const uintx4*>(w);
-    const uintx4 hi = *reinterpret_cast<const uintx4*>(w + 64);
-    const float e = scale_value(sw[row * blocks + b]);
+    wait_vm_le(0);
+    lds_barrier();  // block b has landed; every wave is done with block b - 1
+    Codes c[MT];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uintx4 c = k < 2 ? lo : hi;
-      const bf16x8 a = widen(uintx2{c[k % 2 * 2], c[k % 2 * 2 + 1]}, e);
+    for (int t = 0; t < MT; ++t) c[t] = next[t];
+    if (b + 1 < blocks) {
+      fetch(b + 1);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int n = min(n0 + 16 * j + i16, m - 1);
-        const bf16x8 h = *reinterpret_cast<const bf16x8*>(H + n * ld + b * kBlock + 16 * q +
-                                                          8 * (k % 2) + 64 * (k / 2));
-        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, h, acc[j], 0, 0, 0);
+      for (int t = 0; t < MT; ++t) next[t].load(p[t] + (b + 1) * kBlock, ps[t] + b + 1);
+    }
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      bf16x8 a[MT];
+#pragma unroll
+      for (int t = 0; t < MT; ++t) a[t] = c[t].fragment(s);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const bf16x8 h = *reinterpret_cast<const bf16x8*>(
+            &hb[b % 2][n * kTile + s * kFragment + l * 8]);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+          acc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t], h, acc[t][n], 0, 0, 0);
       }
     }
   }
-  for (int j = 0; j < NT; ++j) {
-    const int n = n0 + 16 * j + i16;
-    if (n >= m) break;
-    T* o = O + n * ldo + r0 + 4 * q;
-    const int have = (int)min((int64_t)4, D - r0 - 4 * q);
-    for (int i = 0; i < have; ++i) o[i] = (T)acc[j][i];
-  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+      store_tile(O, ldo, m, D, (t0 + n) * 16 + i16, r0 + 16 * t + 4 * q4, acc[t][n]);
 }
+
+constexpr int kFew = 16;          // rows of H that one launch takes
+constexpr int kFewColumns = 2048;  // that fit 64 KB of LDS in bfloat16
+constexpr int kFewBlocks = 512;   // blocks of that launch, two a compute unit
 
 int64_t blocks_of(int32_t cols) { return ((int64_t)cols + kBlock - 1) / kBlock; }
-
-template <bool WIDE>
-int quantize(int dtype, int64_t rows, int32_t cols, const void* x, int64_t ldx, void* codes,
-             uint8_t* scales, hipStream_t s) {
-  const int64_t blocks = rows * blocks_of(cols), n = (blocks + 15) / 16;
-  if (n > 0x7FFFFFFF) return LST_EINVAL;
-  return with_dtype(dtype, [&](auto t) {
-    using T = decltype(t);
-    auto run = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(256), 0, s, (const T*)x, ldx, rows, cols,
-                         (int)blocks_of(cols), codes, scales);
-    };
-    blocks <= 0x7FFFFFFF ? run(quantize_kernel<T, uint32_t, WIDE>)
-                         : run(quantize_kernel<T, int64_t, WIDE>);
-    return launched();
-  });
-}
 
 }  // namespace
 }  // namespace lst
@@ -189,12 +315,22 @@ int lst_quantize(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64
   if (!known_dtype(dtype) || rows < 0 || cols < 1 || cols > 4096) return LST_EINVAL;
   if (rows == 0) return LST_OK;
   if (!x || !codes || !scales || ldx < cols || ((uintptr_t)codes & 15)) return LST_EINVAL;
-  return quantize<false>(dtype, rows, cols, x, ldx, codes, scales, (hipStream_t)hip_stream);
+  const int64_t blocks = rows * blocks_of(cols), n = (blocks + 15) / 16;
+  if (n > 0x7FFFFFFF) return LST_EINVAL;
+  return with_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    auto run = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(256), 0, (hipStream_t)hip_stream,
+                         (const T*)x, ldx, rows, cols, (int)blocks_of(cols), codes, scales);
+    };
+    blocks <= 0x7FFFFFFF ? run(quantize_kernel<T, uint32_t>) : run(quantize_kernel<T, int64_t>);
+    return launched();
+  });
 }
 
 int64_t lst_scores_workspace(int32_t m, int32_t d) {
   if (m < 0 || d < 1 || d > 4096) return -1;
-  return m * blocks_of(d) * kBlock * (int64_t)sizeof(__bf16);
+  return ((int64_t)m + 15) / 16 * blocks_of(d) * kTile * (int64_t)sizeof(__bf16);
 }
 
 int lst_scores(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int32_t d, const void* H,
@@ -205,20 +341,43 @@ int lst_scores(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int32_t d
   if (m == 0) return LST_OK;
   if (!H || !codes || !scales || !O || !workspace || ldh < d || ldo < D) return LST_EINVAL;
   if (((uintptr_t)codes & 15) || ((uintptr_t)workspace & 15)) return LST_EINVAL;
-  const int64_t groups = (D + 63) / 64;
-  if (groups > 0x7FFFFFFF) return LST_EINVAL;
+  if (m > 1 << 20 || D > (int64_t)1 << 36) return LST_EINVAL;
   hipStream_t s = (hipStream_t)hip_stream;
-  const int blocks = (int)blocks_of(d);
-  int rc = quantize<true>(dtype, m, d, H, ldh, workspace, nullptr, s);
+  const int blocks = (int)blocks_of(d), tiles = (m + 15) / 16;
+  if (m <= kFew && blocks <= kFewColumns / kBlock)
+    return with_dtype(dtype, [&](auto th) {
+      return with_dtype(out_dtype, [&](auto t) {
+        using TH = decltype(th);
+        using T = decltype(t);
+        const int64_t groups = (D + 127) / 128;
+        const size_t lds = (size_t)blocks * kTile * sizeof(__bf16);
+        hipLaunchKernelGGL((scores_few_kernel<TH, T>),
+                           dim3((unsigned)std::min<int64_t>(groups, kFewBlocks)), dim3(512), lds,
+                           s, (const TH*)H, ldh, d, codes, scales, m, D, blocks, (T*)O, ldo);
+        return launched();
+      });
+    });
+  __bf16* fragments = (__bf16*)workspace;
+  int rc = with_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    hipLaunchKernelGGL(fragments_kernel<T>, dim3(tiles * blocks), dim3(256), 0, s, (const T*)H,
+                       ldh, m, d, blocks, tiles, fragments);
+    return launched();
+  });
   if (rc != LST_OK) return rc;
   return with_dtype(out_dtype, [&](auto t) {
     using T = decltype(t);
-    auto run = [&](auto kernel, int nt) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)groups, (m + 16 * nt - 1) / (16 * nt)), dim3(256),
-                         0, s, codes, scales, (const __bf16*)workspace, m, D, blocks, (T*)O, ldo);
+    auto run = [&](auto kernel, int mt, int nt) {
+      const int64_t row_blocks = (D + 64 * mt - 1) / (64 * mt), cols = (tiles + nt - 1) / nt;
+      const int64_t grid = (row_blocks + 7) / 8 * 8 * cols;
+      if (row_blocks > 0x7FFFFFF0 || grid > 0x7FFFFFFF) return (int)LST_EINVAL;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, s, codes, scales, fragments,
+                         m, D, blocks, (int)row_blocks, (T*)O, ldo);
+      return launched();
     };
-    m <= 16 ? run(scores_kernel<T, 1>, 1) : run(scores_kernel<T, 4>, 4);
-    return launched();
+    if (tiles <= 2) return run(scores_kernel<T, 4, 2>, 4, 2);
+    if (tiles <= 4) return run(scores_kernel<T, 4, 4>, 4, 4);
+    return run(scores_kernel<T, 4, 8>, 4, 8);
   });
 }
 
