@@ -19,7 +19,11 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 2048;
-constexpr int kDigit = 11;  // bits of a pass: kBins = 2^kDigit
+constexpr int kDigit = 11;     // bits of a pass: kBins = 2^kDigit
+constexpr int kChunk = 128;    // entries whose largest key is kept
+constexpr int kStretch = 4096; // entries of one block of the first launch
+constexpr int kList = 4096;    // entries that are listed, at most
+constexpr int kShort = 8192;   // rows up to this length take one launch
 
 struct SampleArgs {
   int m, D;
@@ -28,7 +32,14 @@ struct SampleArgs {
   const int32_t* top_k;
   int32_t* tokens;
   float* prob;
+  int shift;    // weights are multiples of 2^-shift
   double unit;  // 2^shift
+  // the workspace, for rows longer than kShort: the largest key of each chunk; of each stretch
+  // the smallest key and the sum of its weights, relative to its largest; whether a row is done
+  int chunks, stretches;
+  uint32_t *chunk_max, *stretch_min;
+  double* stretch_sum;
+  int* done;
 };
 
 // What one row asks for.
@@ -61,13 +72,55 @@ __device__ inline float value_of(uint32_t k) {
   return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xFFFFFFFFu));
 }
 
-__device__ inline double weight(uint32_t key, uint32_t top, double t) {
-  if (key == top) return 1.0;  // also where the largest is infinite
-  if (key == 0) return 0.0;
-  return exp(((double)value_of(key) - (double)value_of(top)) / t);
+// Weights exp((x - top) / t) = 2^(y / 64) with y = (x - top) 64 / (t ln 2): a table of the
+// 64 roots of two, and a polynomial of the rest, at most ln 2 / 128, to 4e-17.
+struct Weights {
+  const double* roots;  // 2^(i / 64), in LDS
+  double c, top_value, unit;
+  uint32_t top;
+  int shift;
+
+  // 2^e v with v in [0.99, 2.02); e = -4096: nothing, whatever v is
+  __device__ double parts(uint32_t key, int& e) const {
+    const double y = ((double)value_of(key) - top_value) * c;
+    const double n = rint(y);
+    const double r = (y - n) * 0.010830424696249145;  // ln 2 / 64
+    double q = fma(r, 1.0 / 120, 1.0 / 24);
+    q = fma(r, q, 1.0 / 6);
+    q = fma(r, q, 0.5);
+    q = fma(r, q, 1.0);
+    q = fma(r, q, 1.0);
+    const bool some = y > -64.0 * 1000 && key != 0;
+    const int i = some ? (int)n : 0;
+    e = some ? i >> 6 : -4096;
+    return roots[i & 63] * q;
+  }
+  __device__ double of(uint32_t key) const {
+    if (key == top) return 1.0;  // also where the largest is infinite
+    int e;
+    const double v = parts(key, e);
+    return e == -4096 ? 0.0 : ldexp(v, e);
+  }
+  __device__ uint64_t whole(uint32_t key) const {
+    if (key == top) return (uint64_t)1 << shift;
+    int e;
+    const double v = parts(key, e);
+    return e < -shift - 2 ? 0 : (uint64_t)(ldexp(v, e + shift) + 0.5);
+  }
+};
+
+__device__ inline Weights weights_of(const SampleArgs& a, const double* roots, uint32_t top,
+                                     float t) {
+  return {roots, 92.332482616893656 / (double)t,  // 64 / ln 2
+          (double)value_of(top), a.unit, top, a.shift};
+}
+
+__device__ inline void fill_roots(double* roots) {
+  if (threadIdx.x < 64) roots[threadIdx.x] = exp2(threadIdx.x / 64.0);
 }
 
 struct Shared {
+  double roots[64];
   uint64_t bin[kBins];
   uint64_t wave[kWaves];
   uint64_t above;
@@ -126,72 +179,161 @@ struct Border {
   __device__ bool holds(uint32_t k, int i) const { return k > key || (k == key && i <= last); }
 };
 
-// The beginning of those that `in` holds whose values (value(key), an integer) reach target.
-template <class T, class V>
-__device__ Border border_of(Shared& sh, const T* x, int D, uint32_t top, uint32_t low, Border in,
-                            uint64_t target, V value) {
+// Where entries come from: a row in memory, or a list of some of its entries.
+template <class T>
+struct RowEntries {
+  const T* x;
+  int n;
+  __device__ int from(int64_t first) const { return (int)first; }
+  __device__ int to(int64_t end) const { return (int)end; }
+  __device__ int index(int p) const { return p; }
+  __device__ uint32_t key(int p) const { return key_of((float)x[p]); }
+};
+
+struct ListEntries {
+  const uint32_t* keys;
+  const int* indexes;
+  int n;
+  __device__ int from(int64_t) const { return 0; }
+  __device__ int to(int64_t) const { return n; }
+  __device__ int index(int p) const { return indexes[p]; }
+  __device__ uint32_t key(int p) const { return keys[p]; }
+};
+
+// The index at which the sum by index of value(key) over those entries that `in` holds reaches
+// target, which it does.
+template <class S, class V>
+__device__ int index_at(Shared& sh, const S& src, int D, Border in, uint64_t target, V value) {
+  // by stretches of indexes, and then within one
+  int64_t first = 0, size = D;
+  while (size > 1) {
+    const int64_t end = first + size < D ? first + size : D;
+    const uint32_t step = (uint32_t)((size + kBins - 1) / kBins);
+    clear_bins(sh);
+    for (int p = src.from(first) + threadIdx.x; p < src.to(end); p += kThreads) {
+      const int i = src.index(p);
+      const uint32_t k = src.key(p);
+      if (i < first || i >= end || !k || !in.holds(k, i)) continue;
+      const uint64_t v = value(k);
+      if (v) atomicAdd((unsigned long long*)&sh.bin[(uint32_t)(i - first) / step], (unsigned long long)v);
+    }
+    find_bin(sh, target);
+    target -= sh.above;
+    first += (int64_t)sh.found * step;
+    size = step;
+  }
+  return (int)first;
+}
+
+// The key at which the sum from the largest key down, of value(key) over those entries that
+// `in` holds, reaches target, which it does; of target is left what equal keys have to give.
+template <class S, class V>
+__device__ uint32_t key_at(Shared& sh, const S& src, uint32_t top, uint32_t low, Border in,
+                           uint64_t& target, V value) {
   // by the distance of the keys from the largest one, from its leading digit down
   int bits = 32 - __clz((int)(top - low) | 1);
   uint32_t prefix = 0;
-  uint64_t above = 0;
   while (bits > 0) {
     const int shift = max(bits - kDigit, 0);
     clear_bins(sh);
-    for (int i = threadIdx.x; i < D; i += kThreads) {
-      const uint32_t k = key_of((float)x[i]);
-      if (!k || !in.holds(k, i)) continue;
+    for (int p = threadIdx.x; p < src.n; p += kThreads) {
+      const uint32_t k = src.key(p);
+      if (!k || !in.holds(k, src.index(p))) continue;
       const uint32_t d = top - k;
       if (bits < 32 && (d >> bits) != prefix) continue;
       atomicAdd((unsigned long long*)&sh.bin[(d >> shift) & ((1u << (bits - shift)) - 1)],
                 (unsigned long long)value(k));
     }
-    find_bin(sh, target - above);
-    above += sh.above;
+    find_bin(sh, target);
+    target -= sh.above;
     prefix = (prefix << (bits - shift)) | (uint32_t)sh.found;
     bits = shift;
   }
-  Border out{top - prefix, D};
-  // of the equal ones the first ones by index
-  const uint64_t v = value(out.key);
-  const uint64_t want = (target - above + v - 1) / v;
-  const int size = (int)(((int64_t)D + kBins - 1) / kBins);
-  clear_bins(sh);
-  for (int i = threadIdx.x; i < D; i += kThreads)
-    if (key_of((float)x[i]) == out.key && in.holds(out.key, i))
-      atomicAdd((unsigned long long*)&sh.bin[i / size], 1ull);
-  find_bin(sh, want);
-  const int64_t first = (int64_t)sh.found * size;
-  const int end = (int)min((int64_t)D, first + size);
-  uint64_t left = want - sh.above;
-  for (int64_t at = first; at < end; at += kBins) {  // rarely more than once
-    clear_bins(sh);
-    for (int j = threadIdx.x; j < kBins; j += kThreads) {
-      const int64_t i = at + j;
-      if (i < end) sh.bin[j] = key_of((float)x[i]) == out.key && in.holds(out.key, (int)i);
-    }
-    const uint64_t have = sum_bins(sh);
-    if (have >= left) {
-      find_bin(sh, left);
-      out.last = (int)(at + sh.found);
-      break;
-    }
-    left -= have;
-  }
-  return out;
+  return top - prefix;
 }
 
-// One block a row, over and over the row.
+// The beginning of those that `in` holds whose values (value(key), an integer) reach target:
+// of the entries with its last key the first ones by index.
+template <class S, class V>
+__device__ Border border_of(Shared& sh, const S& src, int D, uint32_t top, uint32_t low,
+                            Border in, uint64_t target, V value) {
+  const uint32_t key = key_at(sh, src, top, low, in, target, value);
+  const uint64_t v = value(key), want = (target + v - 1) / v;
+  return {key, index_at(sh, src, D, in, want, [&](uint32_t k) { return (uint64_t)(k == key); })};
+}
+
+template <class S, class V>
+__device__ uint64_t sum_of(Shared& sh, const S& src, Border in, V value) {
+  uint64_t sum = 0;
+  for (int p = threadIdx.x; p < src.n; p += kThreads) {
+    const uint32_t k = src.key(p);
+    if (k && in.holds(k, src.index(p))) sum += value(k);
+  }
+  __syncthreads();
+  sh.bin[2 * threadIdx.x] = sum;
+  sh.bin[2 * threadIdx.x + 1] = 0;
+  return sum_bins(sh);
+}
+
+// The three filters and the choice.  total: the sum of the row's weights where the entries are
+// not all of them and top-k is off; 0: the sum of these is it.
+template <class S>
+__device__ void choose(Shared& sh, const SampleArgs& a, int row, const Wish& w, const Weights& of,
+                       const S& src, uint32_t low, uint64_t total) {
+  const int D = a.D;
+  const uint32_t top = of.top;
+  auto mass = [&](uint32_t k) { return of.whole(k); };
+  Border b{0, D};
+  if (w.k > 0 && w.k < D) {
+    auto one = [](uint32_t) { return (uint64_t)1; };
+    if (sum_of(sh, src, b, one) > (uint64_t)w.k)
+      b = border_of(sh, src, D, top, low, b, (uint64_t)w.k, one);
+  }
+  if (w.p < 1.f) {
+    const uint64_t have = sum_of(sh, src, b, mass);
+    const double want = ceil((double)w.p * (double)(total ? total : have));
+    const uint64_t target = want > 1.0 ? (uint64_t)want : 1;
+    if (target <= have) b = border_of(sh, src, D, top, low, b, target, mass);
+  }
+  const double q = w.q;
+  auto kept = [&](uint32_t k) { return k == top || q <= 0.0 || of.of(k) >= q ? of.whole(k) : 0; };
+  const uint64_t all = sum_of(sh, src, b, kept);
+  int at;
+  if (w.u == 0.f) {
+    // the first entry with any weight, however small beside 2^-shift
+    at = index_at(sh, src, D, b, 1, [&](uint32_t k) {
+      const double v = of.of(k);
+      return (uint64_t)(v > 0.0 && (k == top || v >= q));
+    });
+  } else {
+    at = index_at(sh, src, D, b, (uint64_t)((double)w.u * (double)all) + 1, kept);
+  }
+  for (int p = src.from(at) + threadIdx.x; p < src.to(at + 1); p += kThreads)
+    if (src.index(p) == at) {
+      a.tokens[row] = at;
+      if (a.prob) a.prob[row] = (float)(of.of(src.key(p)) / ((double)all / a.unit));
+    }
+}
+
+__device__ inline void give(const SampleArgs& a, int row, int token, float prob) {
+  a.tokens[row] = token;
+  if (a.prob) a.prob[row] = prob;
+}
+
+// One block a row, over and over the row: short rows, and those that the other launches leave.
 template <class T>
 __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, const T* logits) {
   __shared__ Shared sh;
   const int row = blockIdx.x, tid = threadIdx.x, D = a.D;
-  const T* x = logits + row * a.ldx;
+  if (a.done && a.done[row]) return;
+  fill_roots(sh.roots);
+  const RowEntries<T> src{logits + row * a.ldx, D};
   const Wish w = wish_of(a, row);
   // the largest key, its first index, and the smallest key
   uint32_t top = 0, low = 0xFFFFFFFFu;
   int at = D;
   for (int i = tid; i < D; i += kThreads) {
-    const uint32_t k = key_of((float)x[i]);
+    const uint32_t k = src.key(i);
     if (k > top) top = k, at = i;
     if (k) low = min(low, k);
   }
@@ -209,77 +351,241 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, cons
     low = min(low, (uint32_t)sh.wave[i]);
   }
   if (!w.good || top == 0 || w.t == 0.f) {
-    if (tid == 0) {
-      const bool none = !w.good || top == 0;
-      a.tokens[row] = none ? -1 : at;
-      if (a.prob) a.prob[row] = none ? 0.f : 1.f;
-    }
+    const bool none = !w.good || top == 0;
+    if (tid == 0) give(a, row, none ? -1 : at, none ? 0.f : 1.f);
     return;
   }
-  const double t = w.t;
-  auto whole = [&](double v) { return (uint64_t)(v * a.unit + 0.5); };
-  auto mass = [&](uint32_t k) { return whole(weight(k, top, t)); };
-  // u = 0 takes the first entry with any weight, however small beside 2^-shift
-  const bool any = w.u == 0.f;
-  auto part = [&](double v) { return any ? (uint64_t)(v > 0.0) : (uint64_t)(v * a.unit + 0.5); };
-  // sums of the weights from q on that b holds, by stretches of indexes
-  auto sums = [&](Border b, double q, int size, auto part) {
-    clear_bins(sh);
-    for (int i = tid; i < D; i += kThreads) {
-      const uint32_t k = key_of((float)x[i]);
-      if (!k || !b.holds(k, i)) continue;
-      const double v = weight(k, top, t);
-      if (k != top && v < q) continue;
-      const uint64_t n = part(v);
-      if (n) atomicAdd((unsigned long long*)&sh.bin[i / size], (unsigned long long)n);
+  choose(sh, a, row, w, weights_of(a, sh.roots, top, w.t), src, low, 0);
+}
+
+// ------------------------------------------------------------- long rows
+// Whether the sum of all of a row's weights is wanted before any entry is listed.
+__device__ inline bool wants_sum(const Wish& w, int D) {
+  const bool k = w.k > 0 && w.k < D;
+  return w.good && w.t > 0.f && !k && (w.p < 1.f) == (w.q > 0.f);
+}
+
+// The largest key of every chunk, and the smallest key and the sum of every stretch: one read
+// of the row.  A block has one stretch, a half-wave a chunk at a time.
+template <class T>
+__global__ __launch_bounds__(256) void sample_stats_kernel(SampleArgs a, const T* logits) {
+  __shared__ double roots[64];
+  __shared__ uint32_t wave_max[4], wave_min[4];
+  __shared__ double wave_sum[4];
+  const int row = blockIdx.y, stretch = blockIdx.x, tid = threadIdx.x;
+  const T* x = logits + row * a.ldx;
+  const int64_t base = (int64_t)stretch * kStretch + 4 * tid;
+  constexpr int kSteps = kStretch / 1024;
+  fill_roots(roots);
+  uint32_t key[kSteps][4], top = 0, low = 0xFFFFFFFFu;
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const int64_t i = base + s * 1024;
+    T v[4];
+    if (i + 4 <= a.D) {
+      load_vec(x + i, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = i + j < a.D ? x[i + j] : (T)-INFINITY;
     }
-    return sum_bins(sh);
-  };
-  const int size = (int)(((int64_t)D + kBins - 1) / kBins);
-  Border b{0, D};
-  if (w.k > 0 && w.k < D) {
-    clear_bins(sh);  // as many as there are, when they are fewer than k
-    int n = 0;
-    for (int i = tid; i < D; i += kThreads) n += key_of((float)x[i]) != 0;
-    sh.bin[tid] = n;
-    if (sum_bins(sh) > (uint64_t)w.k)
-      b = border_of(sh, x, D, top, low, b, (uint64_t)w.k, [](uint32_t) { return (uint64_t)1; });
+#pragma unroll
+    for (int j = 0; j < 4; ++j) key[s][j] = key_of((float)v[j]);
   }
-  if (w.p < 1.f) {
-    const uint64_t all = sums(b, 0.0, size, whole);
-    const double want = ceil((double)w.p * (double)all);
-    b = border_of(sh, x, D, top, low, b, want > 1.0 ? (uint64_t)want : 1, mass);
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    uint32_t k = max(max(key[s][0], key[s][1]), max(key[s][2], key[s][3]));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) low = min(low, key[s][j] - 1);  // 0, none, becomes the largest
+#pragma unroll
+    for (int o = 16; o; o >>= 1) k = max(k, (uint32_t)__shfl_xor((int)k, o));
+    const int64_t chunk = (base + s * 1024) / kChunk;
+    if (tid % 32 == 0 && chunk < a.chunks) a.chunk_max[(int64_t)row * a.chunks + chunk] = k;
+    top = max(top, k);
   }
-  const uint64_t all = sums(b, (double)w.q, size, whole);
-  if (any) sums(b, (double)w.q, size, part);
-  const uint64_t want = (uint64_t)floor((double)w.u * (double)all) + 1;
-  find_bin(sh, want);
-  const int64_t first = (int64_t)sh.found * size;
-  const int end = (int)min((int64_t)D, first + size);
-  uint64_t left = want - sh.above;
-  for (int64_t i0 = first; i0 < end; i0 += kBins) {
+  top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+  for (int o = 32; o; o >>= 1) low = min(low, (uint32_t)__shfl_xor((int)low, o));
+  if (tid % 64 == 0) wave_max[tid / 64] = top, wave_min[tid / 64] = low;
+  __syncthreads();
+  top = max(max(wave_max[0], wave_max[1]), max(wave_max[2], wave_max[3]));
+  const int64_t at = (int64_t)row * a.stretches + stretch;
+  if (tid == 0)
+    a.stretch_min[at] = min(min(wave_min[0], wave_min[1]), min(wave_min[2], wave_min[3])) + 1;
+  const Wish w = wish_of(a, row);
+  if (!wants_sum(w, a.D)) return;
+  const Weights of = weights_of(a, roots, top, w.t);
+  double sum = 0.0;
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum += of.of(key[s][j]);
+  if (top == 0) sum = 0.0;
+  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  if (tid % 64 == 0) wave_sum[tid / 64] = sum;
+  __syncthreads();
+  if (tid == 0) a.stretch_sum[at] = (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]);
+}
+
+struct PlanShared {
+  Shared sh;
+  uint32_t keys[kList];
+  int indexes[kList];
+  int hits[kList];  // chunks that hold entries of the list
+  int count, n_hits;
+};
+
+// One block a row: what the chunks' largest keys leave of it.  Takes the rows that ask for the
+// largest entry, for all of them, or for few that a bound on the key tells apart.
+template <class T>
+__global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, const T* logits) {
+  __shared__ PlanShared ps;
+  Shared& sh = ps.sh;
+  const int row = blockIdx.x, tid = threadIdx.x, D = a.D, n = a.chunks;
+  const T* x = logits + row * a.ldx;
+  const uint32_t* cmax = a.chunk_max + (int64_t)row * n;
+  const Wish w = wish_of(a, row);
+  if (tid == 0) a.done[row] = 0, ps.count = ps.n_hits = 0;
+  fill_roots(sh.roots);
+  uint32_t top = 0, low = 0xFFFFFFFFu;
+  for (int i = tid; i < n; i += kThreads) {
+    const uint32_t k = cmax[i];
+    top = max(top, k);
+    if (k) low = min(low, k);
+  }
+  for (int o = 32; o; o >>= 1) {
+    top = max(top, (uint32_t)__shfl_xor((int)top, o));
+    low = min(low, (uint32_t)__shfl_xor((int)low, o));
+  }
+  if (tid % 64 == 0) sh.key[tid / 64] = top, sh.idx[tid / 64] = (int)low;
+  __syncthreads();
+  for (int i = 0; i < kWaves; ++i) top = max(top, sh.key[i]), low = min(low, (uint32_t)sh.idx[i]);
+  if (!w.good || top == 0) {
+    if (tid == 0) give(a, row, -1, 0.f), a.done[row] = 1;
+    return;
+  }
+  const bool k_on = w.k > 0 && w.k < D;
+  const Weights of = weights_of(a, sh.roots, top, w.t);
+  uint64_t total = 0;
+  if (wants_sum(w, D) && w.u > 0.f && a.stretches <= kBins) {
     clear_bins(sh);
-    for (int j = tid; j < kBins; j += kThreads) {
-      const int64_t i = i0 + j;
-      if (i >= end) break;
-      const uint32_t k = key_of((float)x[i]);
-      if (!k || !b.holds(k, (int)i)) continue;
-      const double v = weight(k, top, t);
-      if (k == top || v >= (double)w.q) sh.bin[j] = part(v);
-    }
-    const uint64_t have = sum_bins(sh);
-    if (have >= left) {
-      find_bin(sh, left);
-      if (tid == 0) {
-        const int i = (int)(i0 + sh.found);
-        a.tokens[row] = i;
-        if (a.prob)
-          a.prob[row] = (float)(weight(key_of((float)x[i]), top, t) / ((double)all / a.unit));
+    for (int i = tid; i < a.stretches; i += kThreads) {
+      uint32_t k = 0;
+      for (int j = 0; j < kStretch / kChunk; ++j) {
+        const int c = i * (kStretch / kChunk) + j;
+        if (c < n) k = max(k, cmax[c]);
       }
-      break;
+      const double sum = a.stretch_sum[(int64_t)row * a.stretches + i] * of.of(k);
+      sh.bin[i] = k ? (uint64_t)(sum * a.unit + 0.5) : 0;
     }
-    left -= have;
+    total = sum_bins(sh);
+    if (w.q <= 0.f) {
+      // nothing is left out: the stretch, and the entry in it
+      find_bin(sh, (uint64_t)((double)w.u * (double)total) + 1);
+      const int64_t first = (int64_t)sh.found * kStretch;
+      uint64_t left = (uint64_t)((double)w.u * (double)total) + 1 - sh.above;
+      const int64_t end = first + kStretch < D ? first + kStretch : D;
+      for (int half = 0; half < kStretch / kBins; ++half) {
+        clear_bins(sh);
+        for (int j = tid; j < kBins; j += kThreads) {
+          const int64_t i = first + half * kBins + j;
+          if (i < end) sh.bin[j] = of.whole(key_of((float)x[i]));
+        }
+        const uint64_t have = sum_bins(sh);
+        if (have >= left) {
+          find_bin(sh, left);
+          if (tid == 0) {
+            const int i = (int)(first + half * kBins) + sh.found;
+            give(a, row, i, (float)(of.of(key_of((float)x[i])) / ((double)total / a.unit)));
+            a.done[row] = 1;
+          }
+          return;
+        }
+        left -= have;
+      }
+      return;  // the entries' roundings fell short of the stretch's: the row's own block
+    }
   }
+  // no entry that is kept has a smaller key than this
+  uint32_t least = top;
+  if (w.t > 0.f) {
+    least = 0;
+    if (k_on && w.k <= n) {
+      // the k-th largest of the chunks' largest keys: k entries are at least as large
+      struct Maxima {
+        const uint32_t* k;
+        int n;
+        __device__ int index(int p) const { return p; }
+        __device__ uint32_t key(int p) const { return k[p]; }
+      } maxima{cmax, n};
+      auto one = [](uint32_t) { return (uint64_t)1; };
+      uint64_t left = w.k;
+      if (sum_of(sh, maxima, Border{0, n}, one) >= (uint64_t)w.k)
+        least = key_at(sh, maxima, top, low, Border{0, n}, left, one);
+    }
+    // (not where top-p asks for the weight of all that top-k leaves)
+    if (w.q > 0.f && (w.p >= 1.f || total)) {
+      // w >= q: x >= top + t ln q, with room for the roundings
+      const double x0 = (double)value_of(top) + (double)w.t * (log((double)w.q) - 1e-9);
+      const double room = fabs((double)value_of(top)) * 1e-12;
+      float f = (float)(x0 - room);
+      if ((double)f > x0 - room) f = nextafterf(f, -INFINITY);
+      if (top != key_of(INFINITY) && f > -INFINITY) least = max(least, min(key_of(f), top));
+    }
+    if (least == 0 || w.u == 0.f) return;  // left to the next launches
+  }
+  // the chunks that have such entries, and those entries
+  for (int i = tid; i < n; i += kThreads)
+    if (cmax[i] >= least) {
+      const int h = atomicAdd(&ps.n_hits, 1);
+      if (h < kList) ps.hits[h] = i;
+    }
+  __syncthreads();
+  if (ps.n_hits > kList) return;
+  for (int h = tid / 32; h < ps.n_hits; h += kThreads / 32) {
+    const int64_t i0 = (int64_t)ps.hits[h] * kChunk + tid % 32;
+#pragma unroll
+    for (int j = 0; j < kChunk; j += 32) {
+      const int64_t i = i0 + j;
+      const uint32_t k = i < D ? key_of((float)x[i]) : 0;
+      if (k >= least) {
+        const int c = atomicAdd(&ps.count, 1);
+        if (c < kList) ps.keys[c] = k, ps.indexes[c] = (int)i;
+      }
+    }
+  }
+  __syncthreads();
+  if (ps.count > kList) return;
+  const ListEntries list{ps.keys, ps.indexes, ps.count};
+  if (w.t == 0.f) {
+    const int at = index_at(sh, list, D, Border{top - 1, -1}, 1, [](uint32_t) { return (uint64_t)1; });
+    if (tid == 0) give(a, row, at, 1.f), a.done[row] = 1;
+    return;
+  }
+  choose(sh, a, row, w, of, list, least, total);
+  if (tid == 0) a.done[row] = 1;
+}
+
+struct Layout {
+  SampleArgs args;
+  int64_t bytes;
+};
+
+// The workspace of rows longer than kShort.
+Layout layout(int m, int D, char* p) {
+  Layout r{};
+  SampleArgs& a = r.args;
+  a.chunks = (int)(((int64_t)D + kChunk - 1) / kChunk);
+  a.stretches = (int)(((int64_t)D + kStretch - 1) / kStretch);
+  int64_t at = 0;
+  auto take = [&](auto*& q, int64_t n) {
+    q = (std::remove_reference_t<decltype(q)>)(p + at);
+    at += (n * (int64_t)sizeof(*q) + 15) / 16 * 16;
+  };
+  take(a.stretch_sum, (int64_t)m * a.stretches);
+  take(a.stretch_min, (int64_t)m * a.stretches);
+  take(a.chunk_max, (int64_t)m * a.chunks);
+  take(a.done, m);
+  r.bytes = at;
+  return r;
 }
 
 }  // namespace
@@ -289,7 +595,10 @@ using namespace lst;
 
 extern "C" {
 
-int64_t lst_sample_workspace(int32_t m, int32_t D) { return m < 0 || D < 1 ? -1 : 0; }
+int64_t lst_sample_workspace(int32_t m, int32_t D) {
+  if (m < 0 || D < 1) return -1;
+  return D <= kShort ? 0 : layout(m, D, nullptr).bytes;
+}
 
 int lst_sample(int32_t dtype, int32_t m, int32_t D, const void* logits, int64_t ldx,
                const float* temperature, const int32_t* top_k, const float* top_p,
@@ -298,17 +607,25 @@ int lst_sample(int32_t dtype, int32_t m, int32_t D, const void* logits, int64_t 
   if (!known_dtype(dtype) || m < 0 || D < 1) return LST_EINVAL;
   if (m == 0) return LST_OK;
   if (!logits || !u || !tokens || ldx < D) return LST_EINVAL;
+  if (D > kShort && (!workspace || ((uintptr_t)workspace & 15) || m > 65535)) return LST_EINVAL;
   SampleArgs a{};
+  if (D > kShort) a = layout(m, D, (char*)workspace).args;
   a.m = m, a.D = D, a.ldx = ldx;
   a.temperature = temperature, a.top_k = top_k, a.top_p = top_p, a.min_p = min_p, a.u = u;
   a.tokens = tokens, a.prob = prob;
   int log = 0;
   while (((int64_t)1 << log) < D) ++log;
-  a.unit = (double)((int64_t)1 << (62 - log));
+  a.shift = 62 - log;
+  a.unit = (double)((int64_t)1 << a.shift);
+  hipStream_t s = (hipStream_t)hip_stream;
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
-    hipLaunchKernelGGL(sample_row_kernel<T>, dim3(m), dim3(kThreads), 0, (hipStream_t)hip_stream,
-                       a, (const T*)logits);
+    const T* x = (const T*)logits;
+    if (D > kShort) {
+      hipLaunchKernelGGL(sample_stats_kernel<T>, dim3(a.stretches, m), dim3(256), 0, s, a, x);
+      hipLaunchKernelGGL(sample_plan_kernel<T>, dim3(m), dim3(kThreads), 0, s, a, x);
+    }
+    hipLaunchKernelGGL(sample_row_kernel<T>, dim3(m), dim3(kThreads), 0, s, a, x);
     return launched();
   });
 }

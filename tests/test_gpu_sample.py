@@ -232,12 +232,13 @@ def test_refusals_on_host():
     lib = lst.load_library()
     P = 64  # never dereferenced
 
-    def call(dtype=0, m=2, D=5, x=P, ldx=5, u=P, tokens=P, work=P):
+    def call(dtype=0, m=2, D=5, x=P, ldx=1 << 20, u=P, tokens=P, work=P):
         return lib.lst_sample(dtype, m, D, x, ldx, None, None, None, None, u, tokens, None, work,
                               None)
 
     for kw in (dict(dtype=3), dict(m=-1), dict(D=0), dict(x=None), dict(u=None),
-               dict(tokens=None), dict(ldx=4)):
+               dict(tokens=None), dict(ldx=4), dict(D=100_000, work=None),
+               dict(D=100_000, work=P + 8)):
         assert call(**kw) == lst.LST_EINVAL, kw
     assert call(m=0, x=None) == lst.LST_OK
     assert lst.lst_sample_workspace(-1, 5) == -1 and lst.lst_sample_workspace(1, 0) == -1
