@@ -11,6 +11,8 @@
 // Weights are computed in float64 and added as integers, multiples of 2^-shift with
 // the shift as large as D sums of at most 1 allow: sums of integers do not depend on
 // the order in which the atomics arrive, so the choice does not either.
+#include <algorithm>
+
 #include "dtypes.h"
 
 namespace lst {
@@ -22,8 +24,25 @@ constexpr int kBins = 2048;
 constexpr int kDigit = 11;     // bits of a pass: kBins = 2^kDigit
 constexpr int kChunk = 128;    // entries whose largest key is kept
 constexpr int kStretch = 4096; // entries of one block of the first launch
-constexpr int kList = 4096;    // entries that are listed, at most
+constexpr int kList = 4096;    // entries that one block lists, at most
+constexpr int kFine = 4096;    // bins of a row's values
+constexpr int kSegment = 32768; // entries of one block that sorts them into bins
+constexpr int kLong = 8192;    // entries of a row's list in memory, at most
 constexpr int kShort = 8192;   // rows up to this length take one launch
+constexpr int kBatch = 1024;   // rows of one set of launches
+
+// What the launches leave each other of a long row.
+enum { ROW_OPEN = 0, ROW_DONE = 1, ROW_MASS = 2, ROW_COUNT = 3 };
+struct RowPlan {
+  int state;
+  uint32_t top;     // the largest key
+  float top_value, scale;  // bin = (top_value - x) scale
+  int bin;          // the one that holds the last entry kept
+  unsigned blocks;  // that have added their bins
+  unsigned listed;  // entries of the bin (ROW_COUNT: of all up to it)
+  uint32_t least, most;  // smallest and largest key of the bin
+  uint64_t left;    // ROW_MASS: what the bin's entries have to give
+};
 
 struct SampleArgs {
   int m, D;
@@ -35,11 +54,18 @@ struct SampleArgs {
   int shift;    // weights are multiples of 2^-shift
   double unit;  // 2^shift
   // the workspace, for rows longer than kShort: the largest key of each chunk; of each stretch
-  // the smallest key and the sum of its weights, relative to its largest; whether a row is done
-  int chunks, stretches;
+  // the smallest key and the sum of its weights, relative to its largest, then the weight of
+  // its entries in the bins before the last and the number of those in it; per row its plan,
+  // bins, and a list
+  int chunks, stretches, segments;
   uint32_t *chunk_max, *stretch_min;
   double* stretch_sum;
-  int* done;
+  uint64_t* stretch_mass;
+  int* stretch_count;
+  RowPlan* plan;
+  uint64_t* bins;
+  uint32_t* list_keys;
+  int* list_indexes;
 };
 
 // What one row asks for.
@@ -117,6 +143,11 @@ __device__ inline Weights weights_of(const SampleArgs& a, const double* roots, u
 
 __device__ inline void fill_roots(double* roots) {
   if (threadIdx.x < 64) roots[threadIdx.x] = exp2(threadIdx.x / 64.0);
+}
+
+// The bins go down from the largest value; the last one holds all that is far below.
+__device__ inline int bin_of(const RowPlan& p, uint32_t key) {
+  return min((int)((p.top_value - value_of(key)) * p.scale), kFine - 1);
 }
 
 struct Shared {
@@ -200,6 +231,14 @@ struct ListEntries {
   __device__ uint32_t key(int p) const { return keys[p]; }
 };
 
+// The largest keys of a row's chunks.
+struct Maxima {
+  const uint32_t* k;
+  int n;
+  __device__ int index(int p) const { return p; }
+  __device__ uint32_t key(int p) const { return k[p]; }
+};
+
 // The index at which the sum by index of value(key) over those entries that `in` holds reaches
 // target, which it does.
 template <class S, class V>
@@ -227,9 +266,10 @@ __device__ int index_at(Shared& sh, const S& src, int D, Border in, uint64_t tar
 
 // The key at which the sum from the largest key down, of value(key) over those entries that
 // `in` holds, reaches target, which it does; of target is left what equal keys have to give.
+// enough > 0: or a smaller key, when the sum of the keys between is at most that.
 template <class S, class V>
 __device__ uint32_t key_at(Shared& sh, const S& src, uint32_t top, uint32_t low, Border in,
-                           uint64_t& target, V value) {
+                           uint64_t& target, V value, uint64_t enough = 0) {
   // by the distance of the keys from the largest one, from its leading digit down
   int bits = 32 - __clz((int)(top - low) | 1);
   uint32_t prefix = 0;
@@ -248,6 +288,7 @@ __device__ uint32_t key_at(Shared& sh, const S& src, uint32_t top, uint32_t low,
     target -= sh.above;
     prefix = (prefix << (bits - shift)) | (uint32_t)sh.found;
     bits = shift;
+    if (bits && sh.bin[sh.found] <= enough) return top - min(top, (prefix << bits) + ((1u << bits) - 1));
   }
   return top - prefix;
 }
@@ -318,44 +359,6 @@ __device__ void choose(Shared& sh, const SampleArgs& a, int row, const Wish& w, 
 __device__ inline void give(const SampleArgs& a, int row, int token, float prob) {
   a.tokens[row] = token;
   if (a.prob) a.prob[row] = prob;
-}
-
-// One block a row, over and over the row: short rows, and those that the other launches leave.
-template <class T>
-__global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, const T* logits) {
-  __shared__ Shared sh;
-  const int row = blockIdx.x, tid = threadIdx.x, D = a.D;
-  if (a.done && a.done[row]) return;
-  fill_roots(sh.roots);
-  const RowEntries<T> src{logits + row * a.ldx, D};
-  const Wish w = wish_of(a, row);
-  // the largest key, its first index, and the smallest key
-  uint32_t top = 0, low = 0xFFFFFFFFu;
-  int at = D;
-  for (int i = tid; i < D; i += kThreads) {
-    const uint32_t k = src.key(i);
-    if (k > top) top = k, at = i;
-    if (k) low = min(low, k);
-  }
-  for (int o = 32; o; o >>= 1) {
-    const uint32_t k = __shfl_xor(top, o);
-    const int i = __shfl_xor(at, o);
-    if (k > top || (k == top && i < at)) top = k, at = i;
-    low = min(low, (uint32_t)__shfl_xor(low, o));
-  }
-  if ((tid & 63) == 0) sh.key[tid >> 6] = top, sh.idx[tid >> 6] = at, sh.wave[tid >> 6] = low;
-  __syncthreads();
-  for (int i = 0; i < kWaves; ++i) {
-    const uint32_t k = sh.key[i];
-    if (k > top || (k == top && sh.idx[i] < at)) top = k, at = sh.idx[i];
-    low = min(low, (uint32_t)sh.wave[i]);
-  }
-  if (!w.good || top == 0 || w.t == 0.f) {
-    const bool none = !w.good || top == 0;
-    if (tid == 0) give(a, row, none ? -1 : at, none ? 0.f : 1.f);
-    return;
-  }
-  choose(sh, a, row, w, weights_of(a, sh.roots, top, w.t), src, low, 0);
 }
 
 // ------------------------------------------------------------- long rows
@@ -443,7 +446,8 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
   const T* x = logits + row * a.ldx;
   const uint32_t* cmax = a.chunk_max + (int64_t)row * n;
   const Wish w = wish_of(a, row);
-  if (tid == 0) a.done[row] = 0, ps.count = ps.n_hits = 0;
+  RowPlan& plan = a.plan[row];
+  if (tid == 0) plan.state = ROW_OPEN, ps.count = ps.n_hits = 0;
   fill_roots(sh.roots);
   uint32_t top = 0, low = 0xFFFFFFFFu;
   for (int i = tid; i < n; i += kThreads) {
@@ -459,7 +463,7 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
   __syncthreads();
   for (int i = 0; i < kWaves; ++i) top = max(top, sh.key[i]), low = min(low, (uint32_t)sh.idx[i]);
   if (!w.good || top == 0) {
-    if (tid == 0) give(a, row, -1, 0.f), a.done[row] = 1;
+    if (tid == 0) give(a, row, -1, 0.f), plan.state = ROW_DONE;
     return;
   }
   const bool k_on = w.k > 0 && w.k < D;
@@ -495,7 +499,7 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
           if (tid == 0) {
             const int i = (int)(first + half * kBins) + sh.found;
             give(a, row, i, (float)(of.of(key_of((float)x[i])) / ((double)total / a.unit)));
-            a.done[row] = 1;
+            plan.state = ROW_DONE;
           }
           return;
         }
@@ -509,17 +513,13 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
   if (w.t > 0.f) {
     least = 0;
     if (k_on && w.k <= n) {
-      // the k-th largest of the chunks' largest keys: k entries are at least as large
-      struct Maxima {
-        const uint32_t* k;
-        int n;
-        __device__ int index(int p) const { return p; }
-        __device__ uint32_t key(int p) const { return k[p]; }
-      } maxima{cmax, n};
+      // the k-th largest of the chunks' largest keys, or a little less: k entries are at
+      // least as large
       auto one = [](uint32_t) { return (uint64_t)1; };
+      const Maxima maxima{cmax, n};
       uint64_t left = w.k;
       if (sum_of(sh, maxima, Border{0, n}, one) >= (uint64_t)w.k)
-        least = key_at(sh, maxima, top, low, Border{0, n}, left, one);
+        least = key_at(sh, maxima, top, low, Border{0, n}, left, one, kList / 8);
     }
     // (not where top-p asks for the weight of all that top-k leaves)
     if (w.q > 0.f && (w.p >= 1.f || total)) {
@@ -530,38 +530,325 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
       if ((double)f > x0 - room) f = nextafterf(f, -INFINITY);
       if (top != key_of(INFINITY) && f > -INFINITY) least = max(least, min(key_of(f), top));
     }
-    if (least == 0 || w.u == 0.f) return;  // left to the next launches
+    if (w.u == 0.f) return;  // the row's own block
   }
-  // the chunks that have such entries, and those entries
-  for (int i = tid; i < n; i += kThreads)
-    if (cmax[i] >= least) {
-      const int h = atomicAdd(&ps.n_hits, 1);
-      if (h < kList) ps.hits[h] = i;
-    }
-  __syncthreads();
-  if (ps.n_hits > kList) return;
-  for (int h = tid / 32; h < ps.n_hits; h += kThreads / 32) {
-    const int64_t i0 = (int64_t)ps.hits[h] * kChunk + tid % 32;
+  if (least) {
+    // the chunks that have such entries, and those entries
+    for (int i = tid; i < n; i += kThreads)
+      if (cmax[i] >= least) {
+        const int h = atomicAdd(&ps.n_hits, 1);
+        if (h < kList) ps.hits[h] = i;
+      }
+    __syncthreads();
+    for (int h = tid / 32; h < (ps.n_hits <= kList ? ps.n_hits : 0); h += kThreads / 32) {
+      const int64_t i0 = (int64_t)ps.hits[h] * kChunk + tid % 32;
 #pragma unroll
-    for (int j = 0; j < kChunk; j += 32) {
-      const int64_t i = i0 + j;
-      const uint32_t k = i < D ? key_of((float)x[i]) : 0;
-      if (k >= least) {
-        const int c = atomicAdd(&ps.count, 1);
-        if (c < kList) ps.keys[c] = k, ps.indexes[c] = (int)i;
+      for (int j = 0; j < kChunk; j += 32) {
+        const int64_t i = i0 + j;
+        const uint32_t k = i < D ? key_of((float)x[i]) : 0;
+        if (k >= least) {
+          const int c = atomicAdd(&ps.count, 1);
+          if (c < kList) ps.keys[c] = k, ps.indexes[c] = (int)i;
+        }
+      }
+    }
+    __syncthreads();
+    if (ps.n_hits <= kList && ps.count <= kList) {
+      const ListEntries list{ps.keys, ps.indexes, ps.count};
+      if (w.t == 0.f) {
+        const int at = index_at(sh, list, D, Border{top - 1, -1}, 1,
+                                [](uint32_t) { return (uint64_t)1; });
+        if (tid == 0) give(a, row, at, 1.f);
+      } else {
+        choose(sh, a, row, w, of, list, least, total);
+      }
+      if (tid == 0) plan.state = ROW_DONE;
+      return;
+    }
+  }
+  if (w.t == 0.f || a.stretches > kBins || !isfinite(value_of(top))) return;
+  // more of them: all of the row's entries into bins by their value
+  low = 0xFFFFFFFFu;
+  for (int i = tid; i < a.stretches; i += kThreads) {
+    const uint32_t k = a.stretch_min[(int64_t)row * a.stretches + i];
+    if (k) low = min(low, k);
+  }
+  for (int o = 32; o; o >>= 1) low = min(low, (uint32_t)__shfl_xor((int)low, o));
+  __syncthreads();
+  if (tid % 64 == 0) sh.key[tid / 64] = low;
+  __syncthreads();
+  for (int i = 0; i < kWaves; ++i) low = min(low, sh.key[i]);
+  uint64_t* bins = a.bins + (int64_t)row * kFine;
+  for (int i = tid; i < kFine; i += kThreads) bins[i] = 0;
+  if (tid == 0) {
+    // weights below e^-64 of the largest do not move the border of a sum
+    const float all = value_of(top) - value_of(low);
+    const float range = k_on ? all : fminf(all, 64.f * w.t);
+    plan.top = top;
+    plan.top_value = value_of(top);
+    plan.scale = range > 0.f && isfinite(range) ? fminf(kFine / range, 1e38f) : 0.f;
+    plan.bin = kFine;  // without top-k and top-p: no border, and no bins are needed
+    plan.blocks = plan.listed = 0;
+    plan.least = 0xFFFFFFFFu;
+    plan.most = 0;
+    plan.state = k_on ? ROW_COUNT : ROW_MASS;
+  }
+}
+
+// The entries of a row into bins by their value: the number in each (ROW_COUNT), or their
+// weight (ROW_MASS), added up as integers.  The row's last block finds the bin of the border.
+template <class T>
+__global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a, const T* logits) {
+  __shared__ uint64_t bins[kFine];
+  __shared__ Shared sh;
+  __shared__ bool is_last;
+  const int row = blockIdx.y, tid = threadIdx.x;
+  RowPlan& plan = a.plan[row];
+  const int state = plan.state;
+  if (state != ROW_MASS && state != ROW_COUNT) return;
+  const RowPlan p = plan;
+  const Wish w = wish_of(a, row);
+  if (state == ROW_MASS && w.p >= 1.f) return;
+  const T* x = logits + row * a.ldx;
+  fill_roots(sh.roots);
+  for (int i = tid; i < kFine; i += kThreads) bins[i] = 0;
+  __syncthreads();
+  const Weights of = weights_of(a, sh.roots, p.top, w.t);
+  const int64_t base = (int64_t)blockIdx.x * kSegment + 4 * tid;
+  for (int s = 0; s < kSegment; s += 4 * kThreads) {
+    const int64_t i = base + s;
+    if (i >= a.D) break;
+    T v[4];
+    if (i + 4 <= a.D) {
+      load_vec(x + i, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = i + j < a.D ? x[i + j] : (T)-INFINITY;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t k = key_of((float)v[j]);
+      const uint64_t n = k == 0 ? 0 : state == ROW_COUNT ? 1 : of.whole(k);
+      if (n) atomicAdd((unsigned long long*)&bins[bin_of(p, k)], (unsigned long long)n);
+    }
+  }
+  __syncthreads();
+  unsigned long long* sums = (unsigned long long*)a.bins + (int64_t)row * kFine;
+  for (int i = tid; i < kFine; i += kThreads)
+    if (bins[i]) atomicAdd(&sums[i], (unsigned long long)bins[i]);
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) is_last = atomicAdd(&plan.blocks, 1u) == gridDim.x - 1;
+  __syncthreads();
+  if (!is_last) return;
+  __threadfence();
+  // two halves of the row's bins, one after the other in the shared ones
+  uint64_t half[2], all = 0;
+  for (int i = tid; i < kFine; i += kThreads)
+    bins[i] = __hip_atomic_load(&sums[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  for (int h = 0; h < 2; ++h) {
+    clear_bins(sh);
+    for (int i = tid; i < kBins; i += kThreads) sh.bin[i] = bins[h * kBins + i];
+    half[h] = sum_bins(sh);
+    all += half[h];
+  }
+  uint64_t target = w.k;
+  bool fits = state == ROW_COUNT ? all > target : true;
+  if (state == ROW_MASS) {
+    const double want = ceil((double)w.p * (double)all);
+    target = want > 1.0 ? (uint64_t)want : 1;
+  } else if (!fits) {
+    target = all;  // fewer entries than top-k: all of them
+  }
+  const int h = target > half[0];
+  if (h) target -= half[0];
+  clear_bins(sh);
+  for (int i = tid; i < kBins; i += kThreads) sh.bin[i] = bins[h * kBins + i];
+  find_bin(sh, target);
+  if (tid == 0) {
+    plan.bin = h * kBins + sh.found;
+    plan.left = target - sh.above;
+  }
+}
+
+// The entries of the border's bin into the row's list (ROW_COUNT: of the bins before it too),
+// and for each stretch the weight of those in the bins before and the number of those in it.
+template <class T>
+__global__ __launch_bounds__(256) void sample_list_kernel(SampleArgs a, const T* logits) {
+  __shared__ double roots[64];
+  __shared__ uint64_t wave_mass[4];
+  __shared__ int wave_count[4];
+  const int row = blockIdx.y, stretch = blockIdx.x, tid = threadIdx.x, l = tid % 64;
+  RowPlan& plan = a.plan[row];
+  const int state = plan.state;
+  if (state != ROW_MASS && state != ROW_COUNT) return;
+  const RowPlan p = plan;
+  const Wish w = wish_of(a, row);
+  const T* x = logits + row * a.ldx;
+  const int64_t base = (int64_t)stretch * kStretch + 4 * tid;
+  constexpr int kSteps = kStretch / 1024;
+  fill_roots(roots);
+  __syncthreads();
+  const Weights of = weights_of(a, roots, p.top, w.t);
+  const double q = w.q;
+  uint64_t mass = 0;
+  int count = 0;
+  uint32_t least = 0xFFFFFFFFu, most = 0;
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const int64_t i = base + s * 1024;
+    T v[4];
+    if (i + 4 <= a.D) {
+      load_vec(x + i, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = i + j < a.D ? x[i + j] : (T)-INFINITY;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t k = key_of((float)v[j]);
+      const int b = k ? bin_of(p, k) : kFine;
+      if (state == ROW_MASS && b < p.bin && (k == p.top || q <= 0.0 || of.of(k) >= q))
+        mass += of.whole(k);
+      const bool listed = b == p.bin || (state == ROW_COUNT && b < p.bin);
+      const uint64_t who = __ballot(listed);
+      if (!who) continue;
+      unsigned first = 0;
+      if (l == 0) first = atomicAdd(&plan.listed, (unsigned)__popcll(who));
+      first = __builtin_amdgcn_readfirstlane(first);
+      if (!listed) continue;
+      const unsigned at = first + __popcll(who & ((1ull << l) - 1));
+      ++count;
+      least = min(least, k);
+      most = max(most, k);
+      if (at < kLong) {
+        a.list_keys[(int64_t)row * kLong + at] = k;
+        a.list_indexes[(int64_t)row * kLong + at] = (int)(i + j);
       }
     }
   }
+  if (state != ROW_MASS) return;
+  for (int o = 32; o; o >>= 1) {
+    mass += __shfl_xor(mass, o);
+    count += __shfl_xor(count, o);
+    least = min(least, (uint32_t)__shfl_xor((int)least, o));
+    most = max(most, (uint32_t)__shfl_xor((int)most, o));
+  }
+  if (l == 0) {
+    wave_mass[tid / 64] = mass, wave_count[tid / 64] = count;
+    if (most) atomicMin(&plan.least, least), atomicMax(&plan.most, most);
+  }
   __syncthreads();
-  if (ps.count > kList) return;
-  const ListEntries list{ps.keys, ps.indexes, ps.count};
-  if (w.t == 0.f) {
-    const int at = index_at(sh, list, D, Border{top - 1, -1}, 1, [](uint32_t) { return (uint64_t)1; });
-    if (tid == 0) give(a, row, at, 1.f), a.done[row] = 1;
+  if (tid == 0) {
+    const int64_t at = (int64_t)row * a.stretches + stretch;
+    a.stretch_mass[at] = wave_mass[0] + wave_mass[1] + wave_mass[2] + wave_mass[3];
+    a.stretch_count[at] = wave_count[0] + wave_count[1] + wave_count[2] + wave_count[3];
+  }
+}
+
+// The rest of a row whose entries are in bins; false: more of them at the border than the list
+// holds, and not all alike.
+template <class T>
+__device__ bool finish_bins(Shared& sh, const SampleArgs& a, int row, const Wish& w,
+                            const T* x) {
+  const int tid = threadIdx.x, D = a.D;
+  const RowPlan p = a.plan[row];
+  const Weights of = weights_of(a, sh.roots, p.top, w.t);
+  const ListEntries list{a.list_keys + (int64_t)row * kLong, a.list_indexes + (int64_t)row * kLong,
+                         (int)p.listed};
+  if (p.state == ROW_COUNT) {
+    if (p.listed > kLong) return false;
+    choose(sh, a, row, w, of, list, 1, 0);
+    return true;
+  }
+  const uint64_t* mass = a.stretch_mass + (int64_t)row * a.stretches;
+  const int* count = a.stretch_count + (int64_t)row * a.stretches;
+  const double q = w.q;
+  auto kept = [&](uint32_t k) { return k == p.top || q <= 0.0 || of.of(k) >= q ? of.whole(k) : 0; };
+  Border b{0, D};
+  if (w.p >= 1.f) {
+    clear_bins(sh);
+    for (int i = tid; i < a.stretches; i += kThreads) sh.bin[i] = mass[i];
+  } else if (p.least == p.most) {
+    // one key: the first ones by index, by the stretches' numbers
+    const uint64_t v = of.whole(p.most), want = (p.left + v - 1) / v;
+    clear_bins(sh);
+    for (int i = tid; i < a.stretches; i += kThreads) sh.bin[i] = count[i];
+    find_bin(sh, want);
+    const int stretch = sh.found;
+    const uint64_t rest = want - sh.above;
+    const int64_t first = (int64_t)stretch * kStretch;
+    const RowEntries<T> part{x + first, (int)(first + kStretch < D ? kStretch : D - first)};
+    b = {p.most, (int)first + index_at(sh, part, part.n, Border{p.most - 1, -1}, rest,
+                                       [&](uint32_t k) { return (uint64_t)(k == p.most); })};
+    const uint64_t each = kept(p.most);
+    clear_bins(sh);
+    for (int i = tid; i < a.stretches; i += kThreads)
+      sh.bin[i] = mass[i] + each * (i < stretch ? (uint64_t)count[i] : i == stretch ? rest : 0);
+  } else {
+    if (p.listed > kLong) return false;
+    b = border_of(sh, list, D, p.most, p.least, Border{0, D}, p.left,
+                  [&](uint32_t k) { return of.whole(k); });
+    clear_bins(sh);
+    for (int i = tid; i < a.stretches; i += kThreads) sh.bin[i] = mass[i];
+    __syncthreads();
+    for (int i = tid; i < list.n; i += kThreads)
+      if (b.holds(list.keys[i], list.indexes[i]))
+        atomicAdd((unsigned long long*)&sh.bin[list.indexes[i] / kStretch],
+                  (unsigned long long)kept(list.keys[i]));
+  }
+  const uint64_t all = sum_bins(sh);
+  find_bin(sh, (uint64_t)((double)w.u * (double)all) + 1);
+  const uint64_t left = (uint64_t)((double)w.u * (double)all) + 1 - sh.above;
+  const int64_t first = (int64_t)sh.found * kStretch;
+  const RowEntries<T> part{x + first, (int)(first + kStretch < D ? kStretch : D - first)};
+  const Border here{b.key, (int)(b.last - first < -1 ? -1 : b.last - first)};
+  const int at = index_at(sh, part, part.n, here, left, kept);
+  if (tid == 0)
+    give(a, row, (int)first + at, (float)(of.of(part.key(at)) / ((double)all / a.unit)));
+  return true;
+}
+
+// One block a row, over and over the row: short rows, and those that the other launches leave.
+template <class T>
+__global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, const T* logits) {
+  __shared__ Shared sh;
+  const int row = blockIdx.x, tid = threadIdx.x, D = a.D;
+  if (a.plan && a.plan[row].state == ROW_DONE) return;
+  fill_roots(sh.roots);
+  const RowEntries<T> src{logits + row * a.ldx, D};
+  const Wish w = wish_of(a, row);
+  if (a.plan && a.plan[row].state != ROW_OPEN) {
+    __syncthreads();
+    if (finish_bins(sh, a, row, w, logits + row * a.ldx)) return;
+  }
+  // the largest key, its first index, and the smallest key
+  uint32_t top = 0, low = 0xFFFFFFFFu;
+  int at = D;
+  for (int i = tid; i < D; i += kThreads) {
+    const uint32_t k = src.key(i);
+    if (k > top) top = k, at = i;
+    if (k) low = min(low, k);
+  }
+  for (int o = 32; o; o >>= 1) {
+    const uint32_t k = __shfl_xor(top, o);
+    const int i = __shfl_xor(at, o);
+    if (k > top || (k == top && i < at)) top = k, at = i;
+    low = min(low, (uint32_t)__shfl_xor(low, o));
+  }
+  if ((tid & 63) == 0) sh.key[tid >> 6] = top, sh.idx[tid >> 6] = at, sh.wave[tid >> 6] = low;
+  __syncthreads();
+  for (int i = 0; i < kWaves; ++i) {
+    const uint32_t k = sh.key[i];
+    if (k > top || (k == top && sh.idx[i] < at)) top = k, at = sh.idx[i];
+    low = min(low, (uint32_t)sh.wave[i]);
+  }
+  if (!w.good || top == 0 || w.t == 0.f) {
+    const bool none = !w.good || top == 0;
+    if (tid == 0) give(a, row, none ? -1 : at, none ? 0.f : 1.f);
     return;
   }
-  choose(sh, a, row, w, of, list, least, total);
-  if (tid == 0) a.done[row] = 1;
+  choose(sh, a, row, w, weights_of(a, sh.roots, top, w.t), src, low, 0);
 }
 
 struct Layout {
@@ -575,6 +862,7 @@ Layout layout(int m, int D, char* p) {
   SampleArgs& a = r.args;
   a.chunks = (int)(((int64_t)D + kChunk - 1) / kChunk);
   a.stretches = (int)(((int64_t)D + kStretch - 1) / kStretch);
+  a.segments = (int)(((int64_t)D + kSegment - 1) / kSegment);
   int64_t at = 0;
   auto take = [&](auto*& q, int64_t n) {
     q = (std::remove_reference_t<decltype(q)>)(p + at);
@@ -583,7 +871,12 @@ Layout layout(int m, int D, char* p) {
   take(a.stretch_sum, (int64_t)m * a.stretches);
   take(a.stretch_min, (int64_t)m * a.stretches);
   take(a.chunk_max, (int64_t)m * a.chunks);
-  take(a.done, m);
+  take(a.stretch_mass, (int64_t)m * a.stretches);
+  take(a.stretch_count, (int64_t)m * a.stretches);
+  take(a.plan, m);
+  take(a.bins, (int64_t)m * kFine);
+  take(a.list_keys, (int64_t)m * kLong);
+  take(a.list_indexes, (int64_t)m * kLong);
   r.bytes = at;
   return r;
 }
@@ -597,7 +890,7 @@ extern "C" {
 
 int64_t lst_sample_workspace(int32_t m, int32_t D) {
   if (m < 0 || D < 1) return -1;
-  return D <= kShort ? 0 : layout(m, D, nullptr).bytes;
+  return D <= kShort ? 0 : layout(std::min(m, kBatch), D, nullptr).bytes;
 }
 
 int lst_sample(int32_t dtype, int32_t m, int32_t D, const void* logits, int64_t ldx,
@@ -607,25 +900,35 @@ int lst_sample(int32_t dtype, int32_t m, int32_t D, const void* logits, int64_t 
   if (!known_dtype(dtype) || m < 0 || D < 1) return LST_EINVAL;
   if (m == 0) return LST_OK;
   if (!logits || !u || !tokens || ldx < D) return LST_EINVAL;
-  if (D > kShort && (!workspace || ((uintptr_t)workspace & 15) || m > 65535)) return LST_EINVAL;
-  SampleArgs a{};
-  if (D > kShort) a = layout(m, D, (char*)workspace).args;
-  a.m = m, a.D = D, a.ldx = ldx;
-  a.temperature = temperature, a.top_k = top_k, a.top_p = top_p, a.min_p = min_p, a.u = u;
-  a.tokens = tokens, a.prob = prob;
+  if (D > kShort && (!workspace || ((uintptr_t)workspace & 15))) return LST_EINVAL;
   int log = 0;
   while (((int64_t)1 << log) < D) ++log;
-  a.shift = 62 - log;
-  a.unit = (double)((int64_t)1 << a.shift);
   hipStream_t s = (hipStream_t)hip_stream;
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
-    const T* x = (const T*)logits;
-    if (D > kShort) {
-      hipLaunchKernelGGL(sample_stats_kernel<T>, dim3(a.stretches, m), dim3(256), 0, s, a, x);
-      hipLaunchKernelGGL(sample_plan_kernel<T>, dim3(m), dim3(kThreads), 0, s, a, x);
+    // long rows a batch at a time: the workspace is that of a batch
+    for (int r = 0; r < m; r += kBatch) {
+      const int n = std::min(kBatch, m - r);
+      SampleArgs a{};
+      if (D > kShort) a = layout(n, D, (char*)workspace).args;
+      a.m = n, a.D = D, a.ldx = ldx, a.u = u + r, a.tokens = tokens + r;
+      if (temperature) a.temperature = temperature + r;
+      if (top_k) a.top_k = top_k + r;
+      if (top_p) a.top_p = top_p + r;
+      if (min_p) a.min_p = min_p + r;
+      if (prob) a.prob = prob + r;
+      a.shift = 62 - log;
+      a.unit = (double)((int64_t)1 << a.shift);
+      const T* x = (const T*)logits + r * ldx;
+      if (D > kShort) {
+        hipLaunchKernelGGL(sample_stats_kernel<T>, dim3(a.stretches, n), dim3(256), 0, s, a, x);
+        hipLaunchKernelGGL(sample_plan_kernel<T>, dim3(n), dim3(kThreads), 0, s, a, x);
+        hipLaunchKernelGGL(sample_bins_kernel<T>, dim3(a.segments, n), dim3(kThreads), 0, s, a,
+                           x);
+        hipLaunchKernelGGL(sample_list_kernel<T>, dim3(a.stretches, n), dim3(256), 0, s, a, x);
+      }
+      hipLaunchKernelGGL(sample_row_kernel<T>, dim3(n), dim3(kThreads), 0, s, a, x);
     }
-    hipLaunchKernelGGL(sample_row_kernel<T>, dim3(m), dim3(kThreads), 0, s, a, x);
     return launched();
   });
 }

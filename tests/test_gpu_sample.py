@@ -162,6 +162,36 @@ def test_many_rows(gpu_lib):
 
 
 @pytest.mark.gpu
+def test_many_long_rows(gpu_lib):
+    """More rows than one set of launches takes."""
+    m, D = 1030, 9000
+    x, u = _logits(m, D, torch.bfloat16, 34, spread=0.7)
+    _check(x, u, [MIX[i % len(MIX)] for i in range(m)])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_borders_among_many(gpu_lib, dtype):
+    """Borders with thousands of entries on both sides, and among thousands of equal ones."""
+    D = 120_000
+    g = torch.Generator("cuda").manual_seed(17)
+    sets = [dict(top_p=p, min_p=q, temperature=t) for p in (0.3, 0.8, 0.99)
+            for q, t in ((0.0, 1.0), (0.0, 30.0), (0.4, 1.0), (0.02, 5.0))]
+    sets += [dict(min_p=0.4), dict(min_p=0.9, temperature=2.0), dict(top_k=3000),
+             dict(top_k=7000, top_p=0.6), dict(top_k=100_000, top_p=0.9), dict(top_k=119_990)]
+    m = len(sets)
+    smooth = torch.rand((m, D), device="cuda", generator=g) * 2
+    steps = (smooth * 8).floor() / 8          # sixteen values, thousands of each
+    lone = smooth.clone()
+    lone[:, 77] = 40.0                        # one value far above all others
+    far = smooth.clone()
+    far[:, ::5] = torch.finfo(dtype).min      # and a fifth of them masked by the lowest one
+    u = torch.rand(m, device="cuda", generator=g).tolist()
+    for x in (smooth, steps, lone, far):
+        _check(x.to(dtype), [float(np.float32(v)) for v in u], sets)
+
+
+@pytest.mark.gpu
 def test_frequencies(gpu_lib):
     """Evenly spread random numbers over one row: each token as often as its probability says."""
     m, D = 4096, 20_000
