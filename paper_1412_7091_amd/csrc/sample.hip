@@ -9,8 +9,8 @@
 // the kept weights up to i exceeds u times the sum of all of them.
 //
 // Weights are computed in float64 and added as integers, multiples of 2^-shift with
-// the shift as large as D sums of at most 1 allow: sums of integers do not depend on
-// the order in which the atomics arrive, so the choice does not either.
+// the shift as large as D sums of at most 1 allow (51 at most): sums of integers do
+// not depend on the order in which the atomics arrive, so the choice does not either.
 #include <algorithm>
 
 #include "dtypes.h"
@@ -98,47 +98,39 @@ __device__ inline float value_of(uint32_t k) {
   return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xFFFFFFFFu));
 }
 
-// Weights exp((x - top) / t) = 2^(y / 64) with y = (x - top) 64 / (t ln 2): a table of the
-// 64 roots of two, and a polynomial of the rest, at most ln 2 / 128, to 4e-17.
+// Weights w = exp((x - top) / t) = 2^(y / 64) with y = (x - top) 64 / (t ln 2): a table of the
+// 64 roots of two, and a polynomial of the rest, at most ln 2 / 128, to 4e-17.  Without a
+// branch: a weight costs about 25 instructions, and the long rows' passes are bound by them.
 struct Weights {
   const double* roots;  // 2^(i / 64), in LDS
-  double c, top_value, unit;
-  uint32_t top;
+  double c, unit;       // unit = 2^shift, at most 2^51
+  float top;
   int shift;
 
-  // 2^e v with v in [0.99, 2.02); e = -4096: nothing, whatever v is
-  __device__ double parts(uint32_t key, int& e) const {
-    const double y = ((double)value_of(key) - top_value) * c;
-    const double n = rint(y);
-    const double r = (y - n) * 0.010830424696249145;  // ln 2 / 64
-    double q = fma(r, 1.0 / 120, 1.0 / 24);
-    q = fma(r, q, 1.0 / 6);
-    q = fma(r, q, 0.5);
+  // w 2^shift; 0 for -inf and what is no number
+  __device__ double scaled(float x) const {
+    const double y = ((double)x - (double)top) * c, n = rint(y), r = y - n;
+    double q = fma(r, 1.2417843701716923e-12, 5.732851688640402e-10);  // (ln 2 / 64)^k / k!
+    q = fma(r, q, 2.1173137155464774e-07);
+    q = fma(r, q, 5.864904955056169e-05);
+    q = fma(r, q, 0.010830424696249145);
     q = fma(r, q, 1.0);
-    q = fma(r, q, 1.0);
-    const bool some = y > -64.0 * 1000 && key != 0;
-    const int i = some ? (int)n : 0;
-    e = some ? i >> 6 : -4096;
-    return roots[i & 63] * q;
+    const int i = (int)n;
+    const double d = __builtin_ldexp(roots[i & 63] * q, (i >> 6) + shift);
+    return x == top ? unit : y > -64.0 * 1075 ? d : 0.0;  // (both may be infinite)
   }
-  __device__ double of(uint32_t key) const {
-    if (key == top) return 1.0;  // also where the largest is infinite
-    int e;
-    const double v = parts(key, e);
-    return e == -4096 ? 0.0 : ldexp(v, e);
+  // to the next integer: the lowest bits of a sum with 2^52
+  static __device__ uint64_t rounded(double d) {
+    return (uint64_t)__double_as_longlong(d + 0x1p52) & 0xFFFFFFFFFFFFFull;
   }
-  __device__ uint64_t whole(uint32_t key) const {
-    if (key == top) return (uint64_t)1 << shift;
-    int e;
-    const double v = parts(key, e);
-    return e < -shift - 2 ? 0 : (uint64_t)(ldexp(v, e + shift) + 0.5);
-  }
+  __device__ uint64_t whole(uint32_t key) const { return rounded(scaled(value_of(key))); }
+  __device__ double of(uint32_t key) const { return scaled(value_of(key)) / unit; }
 };
 
 __device__ inline Weights weights_of(const SampleArgs& a, const double* roots, uint32_t top,
                                      float t) {
-  return {roots, 92.332482616893656 / (double)t,  // 64 / ln 2
-          (double)value_of(top), a.unit, top, a.shift};
+  // 64 / ln 2
+  return {roots, 92.332482616893656 / (double)t, a.unit, value_of(top), a.shift};
 }
 
 __device__ inline void fill_roots(double* roots) {
@@ -146,8 +138,8 @@ __device__ inline void fill_roots(double* roots) {
 }
 
 // The bins go down from the largest value; the last one holds all that is far below.
-__device__ inline int bin_of(const RowPlan& p, uint32_t key) {
-  return min((int)((p.top_value - value_of(key)) * p.scale), kFine - 1);
+__device__ inline int bin_of(const RowPlan& p, float x) {
+  return min((int)((p.top_value - x) * p.scale), kFine - 1);
 }
 
 struct Shared {
@@ -161,9 +153,11 @@ struct Shared {
 };
 
 // The first bin at which the running sum reaches target (at most the total): sh.found, and
-// the sum before it, sh.above.
+// the sum before it, sh.above.  Bin 0 should no bin reach it: what is found is always a bin,
+// and the indexes made from it are those of entries.
 __device__ void find_bin(Shared& sh, uint64_t target) {
   const int tid = threadIdx.x, l = tid & 63, w = tid >> 6;
+  if (tid == 0) sh.found = 0, sh.above = 0;
   __syncthreads();
   const uint64_t a = sh.bin[2 * tid], b = sh.bin[2 * tid + 1];
   uint64_t sum = a + b;
@@ -322,7 +316,7 @@ template <class S>
 __device__ void choose(Shared& sh, const SampleArgs& a, int row, const Wish& w, const Weights& of,
                        const S& src, uint32_t low, uint64_t total) {
   const int D = a.D;
-  const uint32_t top = of.top;
+  const uint32_t top = key_of(of.top);
   auto mass = [&](uint32_t k) { return of.whole(k); };
   Border b{0, D};
   if (w.k > 0 && w.k < D) {
@@ -420,7 +414,8 @@ __global__ __launch_bounds__(256) void sample_stats_kernel(SampleArgs a, const T
 #pragma unroll
   for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sum += of.of(key[s][j]);
+    for (int j = 0; j < 4; ++j) sum += of.scaled(value_of(key[s][j]));
+  sum /= a.unit;
   if (top == 0) sum = 0.0;
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
   if (tid % 64 == 0) wave_sum[tid / 64] = sum;
@@ -625,11 +620,17 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a, con
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[j] = i + j < a.D ? x[i + j] : (T)-INFINITY;
     }
+    // what is not to be chosen adds nothing, to whichever bin
+    if (state == ROW_MASS) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t k = key_of((float)v[j]);
-      const uint64_t n = k == 0 ? 0 : state == ROW_COUNT ? 1 : of.whole(k);
-      if (n) atomicAdd((unsigned long long*)&bins[bin_of(p, k)], (unsigned long long)n);
+      for (int j = 0; j < 4; ++j)
+        atomicAdd((unsigned long long*)&bins[bin_of(p, (float)v[j])],
+                  (unsigned long long)Weights::rounded(of.scaled((float)v[j])));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        atomicAdd((unsigned long long*)&bins[bin_of(p, (float)v[j])],
+                  (unsigned long long)((float)v[j] > -INFINITY));
     }
   }
   __syncthreads();
@@ -678,6 +679,7 @@ __global__ __launch_bounds__(256) void sample_list_kernel(SampleArgs a, const T*
   __shared__ double roots[64];
   __shared__ uint64_t wave_mass[4];
   __shared__ int wave_count[4];
+  __shared__ unsigned first;
   const int row = blockIdx.y, stretch = blockIdx.x, tid = threadIdx.x, l = tid % 64;
   RowPlan& plan = a.plan[row];
   const int state = plan.state;
@@ -690,60 +692,83 @@ __global__ __launch_bounds__(256) void sample_list_kernel(SampleArgs a, const T*
   fill_roots(roots);
   __syncthreads();
   const Weights of = weights_of(a, roots, p.top, w.t);
-  const double q = w.q;
-  uint64_t mass = 0;
-  int count = 0;
-  uint32_t least = 0xFFFFFFFFu, most = 0;
+  const double q = (double)w.q * a.unit;
+  float v[kSteps][4];
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
     const int64_t i = base + s * 1024;
-    T v[4];
+    T r[4];
     if (i + 4 <= a.D) {
-      load_vec(x + i, v);
+      load_vec(x + i, r);
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = i + j < a.D ? x[i + j] : (T)-INFINITY;
+      for (int j = 0; j < 4; ++j) r[j] = i + j < a.D ? x[i + j] : (T)-INFINITY;
     }
 #pragma unroll
+    for (int j = 0; j < 4; ++j) v[s][j] = (float)r[j];
+  }
+  uint64_t mass = 0;
+  uint32_t listed = 0, least = 0xFFFFFFFFu, most = 0;  // listed: a bit an entry
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s)
+#pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t k = key_of((float)v[j]);
-      const int b = k ? bin_of(p, k) : kFine;
-      if (state == ROW_MASS && b < p.bin && (k == p.top || q <= 0.0 || of.of(k) >= q))
-        mass += of.whole(k);
-      const bool listed = b == p.bin || (state == ROW_COUNT && b < p.bin);
-      const uint64_t who = __ballot(listed);
-      if (!who) continue;
-      unsigned first = 0;
-      if (l == 0) first = atomicAdd(&plan.listed, (unsigned)__popcll(who));
-      first = __builtin_amdgcn_readfirstlane(first);
-      if (!listed) continue;
-      const unsigned at = first + __popcll(who & ((1ull << l) - 1));
-      ++count;
-      least = min(least, k);
-      most = max(most, k);
-      if (at < kLong) {
-        a.list_keys[(int64_t)row * kLong + at] = k;
-        a.list_indexes[(int64_t)row * kLong + at] = (int)(i + j);
+      const float f = v[s][j];
+      const int b = f > -INFINITY ? bin_of(p, f) : kFine + 1;
+      if (b == p.bin || (state == ROW_COUNT && b < p.bin)) {
+        listed |= 1u << (4 * s + j);
+        least = min(least, key_of(f));
+        most = max(most, key_of(f));
       }
     }
+  if (state == ROW_MASS) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float f = v[s][j];
+        const double d = of.scaled(f);
+        const bool before = f > -INFINITY && bin_of(p, f) < p.bin;
+        mass += before && (d >= q || f == of.top) ? Weights::rounded(d) : 0;
+      }
   }
-  if (state != ROW_MASS) return;
+  const int own = __popc(listed);
+  int upto = own;  // of the wave's lanes up to this one
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_up(upto, o);
+    if (l >= o) upto += up;
+  }
   for (int o = 32; o; o >>= 1) {
     mass += __shfl_xor(mass, o);
-    count += __shfl_xor(count, o);
     least = min(least, (uint32_t)__shfl_xor((int)least, o));
     most = max(most, (uint32_t)__shfl_xor((int)most, o));
   }
-  if (l == 0) {
-    wave_mass[tid / 64] = mass, wave_count[tid / 64] = count;
-    if (most) atomicMin(&plan.least, least), atomicMax(&plan.most, most);
+  if (l == 63) {
+    wave_mass[tid / 64] = mass, wave_count[tid / 64] = upto;
+    if (state == ROW_MASS && most) atomicMin(&plan.least, least), atomicMax(&plan.most, most);
   }
   __syncthreads();
+  const int n = wave_count[0] + wave_count[1] + wave_count[2] + wave_count[3];
   if (tid == 0) {
+    first = n ? atomicAdd(&plan.listed, (unsigned)n) : 0;
     const int64_t at = (int64_t)row * a.stretches + stretch;
     a.stretch_mass[at] = wave_mass[0] + wave_mass[1] + wave_mass[2] + wave_mass[3];
-    a.stretch_count[at] = wave_count[0] + wave_count[1] + wave_count[2] + wave_count[3];
+    a.stretch_count[at] = n;
   }
+  __syncthreads();
+  unsigned at = first + upto - own;
+  for (int k = 0; k < tid / 64; ++k) at += wave_count[k];
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (listed >> (4 * s + j) & 1) {
+        if (at < kLong) {
+          a.list_keys[(int64_t)row * kLong + at] = key_of(v[s][j]);
+          a.list_indexes[(int64_t)row * kLong + at] = (int)(base + s * 1024 + j);
+        }
+        ++at;
+      }
 }
 
 // The rest of a row whose entries are in bins; false: more of them at the border than the list
@@ -917,7 +942,7 @@ int lst_sample(int32_t dtype, int32_t m, int32_t D, const void* logits, int64_t 
       if (top_p) a.top_p = top_p + r;
       if (min_p) a.min_p = min_p + r;
       if (prob) a.prob = prob + r;
-      a.shift = 62 - log;
+      a.shift = std::min(51, 62 - log);
       a.unit = (double)((int64_t)1 << a.shift);
       const T* x = (const T*)logits + r * ldx;
       if (D > kShort) {
