@@ -33,15 +33,14 @@ constexpr int kBatch = 1024;   // rows of one set of launches
 
 // What the launches leave each other of a long row.
 enum { ROW_OPEN = 0, ROW_DONE = 1, ROW_MASS = 2, ROW_COUNT = 3 };
-struct RowPlan {
+struct alignas(128) RowPlan {
   int state;
   uint32_t top;     // the largest key
   float top_value, scale;  // bin = (top_value - x) scale
   int bin;          // the one that holds the last entry kept
-  unsigned blocks;  // that have added their bins
-  unsigned listed;  // entries of the bin (ROW_COUNT: of all up to it)
-  uint32_t least, most;  // smallest and largest key of the bin
   uint64_t left;    // ROW_MASS: what the bin's entries have to give
+  // on a line of its own, since blocks add to it while others read what is above
+  alignas(64) unsigned listed;  // entries of the bin (ROW_COUNT: of all up to it)
 };
 
 struct SampleArgs {
@@ -62,6 +61,7 @@ struct SampleArgs {
   double* stretch_sum;
   uint64_t* stretch_mass;
   int* stretch_count;
+  uint32_t *stretch_least, *stretch_most;  // of the entries in the last bin
   RowPlan* plan;
   uint64_t* bins;
   uint32_t* list_keys;
@@ -188,6 +188,20 @@ __device__ uint64_t sum_bins(Shared& sh) {
   uint64_t all = 0;
   for (int i = 0; i < kWaves; ++i) all += sh.wave[i];
   return all;
+}
+
+// The smallest `least` and the largest `most` of all threads.
+__device__ void extremes(Shared& sh, uint32_t& least, uint32_t& most) {
+  for (int o = 32; o; o >>= 1) {
+    least = min(least, (uint32_t)__shfl_xor((int)least, o));
+    most = max(most, (uint32_t)__shfl_xor((int)most, o));
+  }
+  __syncthreads();
+  if (threadIdx.x % 64 == 0)
+    sh.key[threadIdx.x / 64] = most, sh.idx[threadIdx.x / 64] = (int)least;
+  __syncthreads();
+  for (int i = 0; i < kWaves; ++i)
+    most = max(most, sh.key[i]), least = min(least, (uint32_t)sh.idx[i]);
 }
 
 __device__ void clear_bins(Shared& sh) {
@@ -423,6 +437,48 @@ __global__ __launch_bounds__(256) void sample_stats_kernel(SampleArgs a, const T
   if (tid == 0) a.stretch_sum[at] = (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]);
 }
 
+// choose() for at most kFewEntries entries and u > 0: every entry is compared with every other
+// one, four threads an entry, instead of sorted.
+constexpr int kFewEntries = kThreads / 4;
+__device__ void choose_few(Shared& sh, const SampleArgs& a, int row, const Wish& w,
+                           const Weights& of, const ListEntries& list, uint64_t total) {
+  uint64_t *order = sh.bin, *weight = sh.bin + kFewEntries, *kept = sh.bin + 2 * kFewEntries;
+  const int tid = threadIdx.x, i = tid / 4, part = tid % 4, n = list.n;
+  __syncthreads();
+  if (tid < n) {
+    order[tid] = (uint64_t)~list.keys[tid] << 32 | (uint32_t)list.indexes[tid];
+    weight[tid] = of.whole(list.keys[tid]);
+  }
+  if (tid == 0) sh.above = 0;
+  __syncthreads();
+  int rank = 0;
+  uint64_t before = 0;
+  if (i < n)
+    for (int j = part; j < n; j += 4)
+      if (order[j] < order[i]) ++rank, before += weight[j];
+  for (int o = 1; o < 4; o <<= 1) rank += __shfl_xor(rank, o), before += __shfl_xor(before, o);
+  const int most = w.k > 0 && w.k < n ? w.k : n;
+  if (i < n && part == 0 && rank == most - 1) sh.above = before + weight[i];
+  __syncthreads();
+  const double want = w.p < 1.f ? ceil((double)w.p * (double)(total ? total : sh.above)) : 0.0;
+  if (i < n && part == 0) {
+    const bool in = rank == 0 || (rank < most && (w.p >= 1.f || (double)before < want) &&
+                                  (w.q <= 0.f || of.of(list.keys[i]) >= (double)w.q));
+    kept[i] = in ? weight[i] : 0;
+  }
+  __syncthreads();
+  uint64_t upto = 0, all = 0;
+  if (i < n)
+    for (int j = part; j < n; j += 4) {
+      all += kept[j];
+      if (list.indexes[j] <= list.indexes[i]) upto += kept[j];
+    }
+  for (int o = 1; o < 4; o <<= 1) upto += __shfl_xor(upto, o), all += __shfl_xor(all, o);
+  const uint64_t target = (uint64_t)((double)w.u * (double)all) + 1;
+  if (i < n && part == 0 && upto >= target && upto - kept[i] < target)
+    give(a, row, list.indexes[i], (float)(of.of(list.keys[i]) / ((double)all / a.unit)));
+}
+
 struct PlanShared {
   Shared sh;
   uint32_t keys[kList];
@@ -450,13 +506,7 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
     top = max(top, k);
     if (k) low = min(low, k);
   }
-  for (int o = 32; o; o >>= 1) {
-    top = max(top, (uint32_t)__shfl_xor((int)top, o));
-    low = min(low, (uint32_t)__shfl_xor((int)low, o));
-  }
-  if (tid % 64 == 0) sh.key[tid / 64] = top, sh.idx[tid / 64] = (int)low;
-  __syncthreads();
-  for (int i = 0; i < kWaves; ++i) top = max(top, sh.key[i]), low = min(low, (uint32_t)sh.idx[i]);
+  extremes(sh, low, top);
   if (!w.good || top == 0) {
     if (tid == 0) give(a, row, -1, 0.f), plan.state = ROW_DONE;
     return;
@@ -535,15 +585,28 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
         if (h < kList) ps.hits[h] = i;
       }
     __syncthreads();
-    for (int h = tid / 32; h < (ps.n_hits <= kList ? ps.n_hits : 0); h += kThreads / 32) {
-      const int64_t i0 = (int64_t)ps.hits[h] * kChunk + tid % 32;
+    // a half-wave a chunk, four chunks under way
+    const int hits = ps.n_hits <= kList ? ps.n_hits : 0;
+    for (int h0 = tid / 32; h0 < hits; h0 += 4 * (kThreads / 32)) {
+      T v[4][kChunk / 32];
 #pragma unroll
-      for (int j = 0; j < kChunk; j += 32) {
-        const int64_t i = i0 + j;
-        const uint32_t k = i < D ? key_of((float)x[i]) : 0;
-        if (k >= least) {
-          const int c = atomicAdd(&ps.count, 1);
-          if (c < kList) ps.keys[c] = k, ps.indexes[c] = (int)i;
+      for (int c = 0; c < 4; ++c) {
+        const int h = min(h0 + c * (kThreads / 32), hits - 1);
+        const int64_t i = (int64_t)ps.hits[h] * kChunk + tid % 32;
+#pragma unroll
+        for (int j = 0; j < kChunk / 32; ++j) v[c][j] = x[min(i + 32 * j, (int64_t)D - 1)];
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int h = h0 + c * (kThreads / 32);
+        if (h >= hits) break;
+        const int64_t i = (int64_t)ps.hits[h] * kChunk + tid % 32;
+#pragma unroll
+        for (int j = 0; j < kChunk / 32; ++j) {
+          const uint32_t k = key_of((float)v[c][j]);
+          if (k < least || i + 32 * j >= D) continue;
+          const int at = atomicAdd(&ps.count, 1);
+          if (at < kList) ps.keys[at] = k, ps.indexes[at] = (int)(i + 32 * j);
         }
       }
     }
@@ -554,6 +617,8 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
         const int at = index_at(sh, list, D, Border{top - 1, -1}, 1,
                                 [](uint32_t) { return (uint64_t)1; });
         if (tid == 0) give(a, row, at, 1.f);
+      } else if (list.n <= kFewEntries) {
+        choose_few(sh, a, row, w, of, list, total);
       } else {
         choose(sh, a, row, w, of, list, least, total);
       }
@@ -568,11 +633,8 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
     const uint32_t k = a.stretch_min[(int64_t)row * a.stretches + i];
     if (k) low = min(low, k);
   }
-  for (int o = 32; o; o >>= 1) low = min(low, (uint32_t)__shfl_xor((int)low, o));
-  __syncthreads();
-  if (tid % 64 == 0) sh.key[tid / 64] = low;
-  __syncthreads();
-  for (int i = 0; i < kWaves; ++i) low = min(low, sh.key[i]);
+  uint32_t unused = 0;
+  extremes(sh, low, unused);
   uint64_t* bins = a.bins + (int64_t)row * kFine;
   for (int i = tid; i < kFine; i += kThreads) bins[i] = 0;
   if (tid == 0) {
@@ -583,20 +645,17 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
     plan.top_value = value_of(top);
     plan.scale = range > 0.f && isfinite(range) ? fminf(kFine / range, 1e38f) : 0.f;
     plan.bin = kFine;  // without top-k and top-p: no border, and no bins are needed
-    plan.blocks = plan.listed = 0;
-    plan.least = 0xFFFFFFFFu;
-    plan.most = 0;
+    plan.listed = 0;
     plan.state = k_on ? ROW_COUNT : ROW_MASS;
   }
 }
 
 // The entries of a row into bins by their value: the number in each (ROW_COUNT), or their
-// weight (ROW_MASS), added up as integers.  The row's last block finds the bin of the border.
+// weight (ROW_MASS), added up as integers.
 template <class T>
 __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a, const T* logits) {
   __shared__ uint64_t bins[kFine];
-  __shared__ Shared sh;
-  __shared__ bool is_last;
+  __shared__ double roots[64];
   const int row = blockIdx.y, tid = threadIdx.x;
   RowPlan& plan = a.plan[row];
   const int state = plan.state;
@@ -605,10 +664,10 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a, con
   const Wish w = wish_of(a, row);
   if (state == ROW_MASS && w.p >= 1.f) return;
   const T* x = logits + row * a.ldx;
-  fill_roots(sh.roots);
+  fill_roots(roots);
   for (int i = tid; i < kFine; i += kThreads) bins[i] = 0;
   __syncthreads();
-  const Weights of = weights_of(a, sh.roots, p.top, w.t);
+  const Weights of = weights_of(a, roots, p.top, w.t);
   const int64_t base = (int64_t)blockIdx.x * kSegment + 4 * tid;
   for (int s = 0; s < kSegment; s += 4 * kThreads) {
     const int64_t i = base + s;
@@ -637,16 +696,20 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a, con
   unsigned long long* sums = (unsigned long long*)a.bins + (int64_t)row * kFine;
   for (int i = tid; i < kFine; i += kThreads)
     if (bins[i]) atomicAdd(&sums[i], (unsigned long long)bins[i]);
-  __threadfence();
-  __syncthreads();
-  if (tid == 0) is_last = atomicAdd(&plan.blocks, 1u) == gridDim.x - 1;
-  __syncthreads();
-  if (!is_last) return;
-  __threadfence();
-  // two halves of the row's bins, one after the other in the shared ones
+}
+
+// The bin of the border, from a row's bins.
+__global__ __launch_bounds__(kThreads) void sample_border_kernel(SampleArgs a) {
+  __shared__ Shared sh;
+  const int row = blockIdx.x, tid = threadIdx.x;
+  RowPlan& plan = a.plan[row];
+  const int state = plan.state;
+  if (state != ROW_MASS && state != ROW_COUNT) return;
+  const Wish w = wish_of(a, row);
+  if (state == ROW_MASS && w.p >= 1.f) return;
+  const uint64_t* bins = a.bins + (int64_t)row * kFine;
+  // one half of them after the other
   uint64_t half[2], all = 0;
-  for (int i = tid; i < kFine; i += kThreads)
-    bins[i] = __hip_atomic_load(&sums[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   for (int h = 0; h < 2; ++h) {
     clear_bins(sh);
     for (int i = tid; i < kBins; i += kThreads) sh.bin[i] = bins[h * kBins + i];
@@ -679,6 +742,7 @@ __global__ __launch_bounds__(256) void sample_list_kernel(SampleArgs a, const T*
   __shared__ double roots[64];
   __shared__ uint64_t wave_mass[4];
   __shared__ int wave_count[4];
+  __shared__ uint32_t wave_least[4], wave_most[4];
   __shared__ unsigned first;
   const int row = blockIdx.y, stretch = blockIdx.x, tid = threadIdx.x, l = tid % 64;
   RowPlan& plan = a.plan[row];
@@ -745,16 +809,20 @@ __global__ __launch_bounds__(256) void sample_list_kernel(SampleArgs a, const T*
   }
   if (l == 63) {
     wave_mass[tid / 64] = mass, wave_count[tid / 64] = upto;
-    if (state == ROW_MASS && most) atomicMin(&plan.least, least), atomicMax(&plan.most, most);
+    wave_least[tid / 64] = least, wave_most[tid / 64] = most;
   }
   __syncthreads();
   const int n = wave_count[0] + wave_count[1] + wave_count[2] + wave_count[3];
   if (tid == 0) {
-    first = n ? atomicAdd(&plan.listed, (unsigned)n) : 0;
+    if (n) first = atomicAdd(&plan.listed, (unsigned)n);
     const int64_t at = (int64_t)row * a.stretches + stretch;
     a.stretch_mass[at] = wave_mass[0] + wave_mass[1] + wave_mass[2] + wave_mass[3];
     a.stretch_count[at] = n;
+    a.stretch_least[at] =
+        min(min(wave_least[0], wave_least[1]), min(wave_least[2], wave_least[3]));
+    a.stretch_most[at] = max(max(wave_most[0], wave_most[1]), max(wave_most[2], wave_most[3]));
   }
+  if (n == 0) return;
   __syncthreads();
   unsigned at = first + upto - own;
   for (int k = 0; k < tid / 64; ++k) at += wave_count[k];
@@ -790,13 +858,20 @@ __device__ bool finish_bins(Shared& sh, const SampleArgs& a, int row, const Wish
   const int* count = a.stretch_count + (int64_t)row * a.stretches;
   const double q = w.q;
   auto kept = [&](uint32_t k) { return k == p.top || q <= 0.0 || of.of(k) >= q ? of.whole(k) : 0; };
+  // the smallest and largest key of the last bin
+  uint32_t least = 0xFFFFFFFFu, most = 0;
+  for (int i = tid; i < a.stretches; i += kThreads) {
+    least = min(least, a.stretch_least[(int64_t)row * a.stretches + i]);
+    most = max(most, a.stretch_most[(int64_t)row * a.stretches + i]);
+  }
+  extremes(sh, least, most);
   Border b{0, D};
   if (w.p >= 1.f) {
     clear_bins(sh);
     for (int i = tid; i < a.stretches; i += kThreads) sh.bin[i] = mass[i];
-  } else if (p.least == p.most) {
+  } else if (least == most) {
     // one key: the first ones by index, by the stretches' numbers
-    const uint64_t v = of.whole(p.most), want = (p.left + v - 1) / v;
+    const uint64_t v = of.whole(most), want = (p.left + v - 1) / v;
     clear_bins(sh);
     for (int i = tid; i < a.stretches; i += kThreads) sh.bin[i] = count[i];
     find_bin(sh, want);
@@ -804,15 +879,15 @@ __device__ bool finish_bins(Shared& sh, const SampleArgs& a, int row, const Wish
     const uint64_t rest = want - sh.above;
     const int64_t first = (int64_t)stretch * kStretch;
     const RowEntries<T> part{x + first, (int)(first + kStretch < D ? kStretch : D - first)};
-    b = {p.most, (int)first + index_at(sh, part, part.n, Border{p.most - 1, -1}, rest,
-                                       [&](uint32_t k) { return (uint64_t)(k == p.most); })};
-    const uint64_t each = kept(p.most);
+    b = {most, (int)first + index_at(sh, part, part.n, Border{most - 1, -1}, rest,
+                                       [&](uint32_t k) { return (uint64_t)(k == most); })};
+    const uint64_t each = kept(most);
     clear_bins(sh);
     for (int i = tid; i < a.stretches; i += kThreads)
       sh.bin[i] = mass[i] + each * (i < stretch ? (uint64_t)count[i] : i == stretch ? rest : 0);
   } else {
     if (p.listed > kLong) return false;
-    b = border_of(sh, list, D, p.most, p.least, Border{0, D}, p.left,
+    b = border_of(sh, list, D, most, least, Border{0, D}, p.left,
                   [&](uint32_t k) { return of.whole(k); });
     clear_bins(sh);
     for (int i = tid; i < a.stretches; i += kThreads) sh.bin[i] = mass[i];
@@ -898,6 +973,8 @@ Layout layout(int m, int D, char* p) {
   take(a.chunk_max, (int64_t)m * a.chunks);
   take(a.stretch_mass, (int64_t)m * a.stretches);
   take(a.stretch_count, (int64_t)m * a.stretches);
+  take(a.stretch_least, (int64_t)m * a.stretches);
+  take(a.stretch_most, (int64_t)m * a.stretches);
   take(a.plan, m);
   take(a.bins, (int64_t)m * kFine);
   take(a.list_keys, (int64_t)m * kLong);
@@ -950,6 +1027,7 @@ int lst_sample(int32_t dtype, int32_t m, int32_t D, const void* logits, int64_t 
         hipLaunchKernelGGL(sample_plan_kernel<T>, dim3(n), dim3(kThreads), 0, s, a, x);
         hipLaunchKernelGGL(sample_bins_kernel<T>, dim3(a.segments, n), dim3(kThreads), 0, s, a,
                            x);
+        hipLaunchKernelGGL(sample_border_kernel, dim3(n), dim3(kThreads), 0, s, a);
         hipLaunchKernelGGL(sample_list_kernel<T>, dim3(a.stretches, n), dim3(256), 0, s, a, x);
       }
       hipLaunchKernelGGL(sample_row_kernel<T>, dim3(n), dim3(kThreads), 0, s, a, x);
