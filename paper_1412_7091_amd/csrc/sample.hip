@@ -150,6 +150,10 @@ struct Shared {
   int found;
   uint32_t key[kWaves];
   int idx[kWaves];
+  // the entries among which a search ends, and what it ends with
+  int few, few_at;
+  uint32_t few_keys[64], few_key;
+  int few_indexes[64];
 };
 
 // The first bin at which the running sum reaches target (at most the total): sh.found, and
@@ -227,6 +231,7 @@ struct RowEntries {
   __device__ int to(int64_t end) const { return (int)end; }
   __device__ int index(int p) const { return p; }
   __device__ uint32_t key(int p) const { return key_of((float)x[p]); }
+  __device__ uint64_t count(Shared& sh) const;  // of those that may be chosen
 };
 
 struct ListEntries {
@@ -237,6 +242,7 @@ struct ListEntries {
   __device__ int to(int64_t) const { return n; }
   __device__ int index(int p) const { return indexes[p]; }
   __device__ uint32_t key(int p) const { return keys[p]; }
+  __device__ uint64_t count(Shared&) const { return n; }
 };
 
 // The largest keys of a row's chunks.
@@ -246,6 +252,39 @@ struct Maxima {
   __device__ int index(int p) const { return p; }
   __device__ uint32_t key(int p) const { return k[p]; }
 };
+
+// The end of a search: sh.few entries, at most 64, among which the sum of value(key) in the
+// order of before(a key, its index, another key, its index) reaches target: sh.few_key and
+// sh.few_at.  One wave compares every entry with every other.
+template <class V, class B>
+__device__ void settle(Shared& sh, uint64_t target, V value, B before) {
+  const int l = threadIdx.x, n = sh.few;
+  if (l < 64 && l < n) {
+    const uint32_t key = sh.few_keys[l];
+    const int index = sh.few_indexes[l];
+    uint64_t sum = 0;
+    for (int j = 0; j < n; ++j)
+      if (before(sh.few_keys[j], sh.few_indexes[j], key, index)) sum += value(sh.few_keys[j]);
+    if (sum < target && target <= sum + value(key)) sh.few_key = key, sh.few_at = index;
+  }
+  __syncthreads();
+}
+
+// Collects the entries p in [from, to) that `wanted` for it; true when they are at most 64.
+template <class S, class W>
+__device__ bool collect(Shared& sh, const S& src, int from, int to, W wanted) {
+  if (threadIdx.x == 0) sh.few = sh.few_at = 0, sh.few_key = 0;
+  __syncthreads();
+  for (int p = from + threadIdx.x; p < to; p += kThreads) {
+    const uint32_t k = src.key(p);
+    const int i = src.index(p);
+    if (!wanted(k, i)) continue;
+    const int at = atomicAdd(&sh.few, 1);
+    if (at < 64) sh.few_keys[at] = k, sh.few_indexes[at] = i;
+  }
+  __syncthreads();
+  return sh.few <= 64;
+}
 
 // The index at which the sum by index of value(key) over those entries that `in` holds reaches
 // target, which it does.
@@ -262,43 +301,60 @@ __device__ int index_at(Shared& sh, const S& src, int D, Border in, uint64_t tar
       const uint32_t k = src.key(p);
       if (i < first || i >= end || !k || !in.holds(k, i)) continue;
       const uint64_t v = value(k);
-      if (v) atomicAdd((unsigned long long*)&sh.bin[(uint32_t)(i - first) / step], (unsigned long long)v);
+      if (v) atomicAdd((unsigned long long*)&sh.bin[(uint32_t)(i - first) / step],
+                       (unsigned long long)v);
     }
     find_bin(sh, target);
     target -= sh.above;
     first += (int64_t)sh.found * step;
     size = step;
+    if (size == 1) break;
+    const int64_t last = first + size < D ? first + size : D;
+    if (collect(sh, src, src.from(first), src.to(last), [&](uint32_t k, int i) {
+          return i >= first && i < last && k && in.holds(k, i);
+        })) {
+      settle(sh, target, value, [](uint32_t, int i, uint32_t, int j) { return i < j; });
+      return sh.few_at;
+    }
   }
   return (int)first;
 }
 
-// The key at which the sum from the largest key down, of value(key) over those entries that
-// `in` holds, reaches target, which it does; of target is left what equal keys have to give.
-// enough > 0: or a smaller key, when the sum of the keys between is at most that.
+// One digit of the distance from the largest key at which the sum of value(key), from there
+// down over those entries that `in` holds, reaches target: of target is left what the
+// entries with this prefix have to give, of bits the ones behind it.
 template <class S, class V>
-__device__ uint32_t key_at(Shared& sh, const S& src, uint32_t top, uint32_t low, Border in,
-                           uint64_t& target, V value, uint64_t enough = 0) {
-  // by the distance of the keys from the largest one, from its leading digit down
+__device__ void search_digit(Shared& sh, const S& src, uint32_t top, Border in, uint64_t& target,
+                             V value, int& bits, uint32_t& prefix) {
+  const int shift = max(bits - kDigit, 0);
+  clear_bins(sh);
+  for (int p = threadIdx.x; p < src.n; p += kThreads) {
+    const uint32_t k = src.key(p);
+    if (!k || !in.holds(k, src.index(p))) continue;
+    const uint32_t d = top - k;
+    if (bits < 32 && (d >> bits) != prefix) continue;
+    atomicAdd((unsigned long long*)&sh.bin[(d >> shift) & ((1u << (bits - shift)) - 1)],
+              (unsigned long long)value(k));
+  }
+  find_bin(sh, target);
+  target -= sh.above;
+  prefix = (prefix << (bits - shift)) | (uint32_t)sh.found;
+  bits = shift;
+}
+
+// A key that at least `count` of the entries reach, and hardly more than that: at most
+// `spare` of them are as near to it as the search tells.
+template <class S>
+__device__ uint32_t key_near(Shared& sh, const S& src, uint32_t top, uint32_t low,
+                             uint64_t count, uint64_t spare) {
   int bits = 32 - __clz((int)(top - low) | 1);
   uint32_t prefix = 0;
   while (bits > 0) {
-    const int shift = max(bits - kDigit, 0);
-    clear_bins(sh);
-    for (int p = threadIdx.x; p < src.n; p += kThreads) {
-      const uint32_t k = src.key(p);
-      if (!k || !in.holds(k, src.index(p))) continue;
-      const uint32_t d = top - k;
-      if (bits < 32 && (d >> bits) != prefix) continue;
-      atomicAdd((unsigned long long*)&sh.bin[(d >> shift) & ((1u << (bits - shift)) - 1)],
-                (unsigned long long)value(k));
-    }
-    find_bin(sh, target);
-    target -= sh.above;
-    prefix = (prefix << (bits - shift)) | (uint32_t)sh.found;
-    bits = shift;
-    if (bits && sh.bin[sh.found] <= enough) return top - min(top, (prefix << bits) + ((1u << bits) - 1));
+    search_digit(sh, src, top, Border{0, src.n}, count, [](uint32_t) { return (uint64_t)1; },
+                 bits, prefix);
+    if (sh.bin[sh.found] <= spare) break;
   }
-  return top - prefix;
+  return top - min(top, (uint32_t)((((uint64_t)prefix + 1) << bits) - 1));
 }
 
 // The beginning of those that `in` holds whose values (value(key), an integer) reach target:
@@ -306,7 +362,21 @@ __device__ uint32_t key_at(Shared& sh, const S& src, uint32_t top, uint32_t low,
 template <class S, class V>
 __device__ Border border_of(Shared& sh, const S& src, int D, uint32_t top, uint32_t low,
                             Border in, uint64_t target, V value) {
-  const uint32_t key = key_at(sh, src, top, low, in, target, value);
+  int bits = 32 - __clz((int)(top - low) | 1);
+  uint32_t prefix = 0;
+  while (bits > 0) {
+    search_digit(sh, src, top, in, target, value, bits, prefix);
+    const int left = bits;
+    if (collect(sh, src, 0, src.n, [&](uint32_t k, int i) {
+          return k && (top - k) >> left == prefix && in.holds(k, i);
+        })) {
+      settle(sh, target, value, [](uint32_t k, int i, uint32_t l, int j) {
+        return k > l || (k == l && i < j);
+      });
+      return {sh.few_key, sh.few_at};
+    }
+  }
+  const uint32_t key = top - prefix;
   const uint64_t v = value(key), want = (target + v - 1) / v;
   return {key, index_at(sh, src, D, in, want, [&](uint32_t k) { return (uint64_t)(k == key); })};
 }
@@ -324,6 +394,11 @@ __device__ uint64_t sum_of(Shared& sh, const S& src, Border in, V value) {
   return sum_bins(sh);
 }
 
+template <class T>
+__device__ uint64_t RowEntries<T>::count(Shared& sh) const {
+  return sum_of(sh, *this, Border{0, n}, [](uint32_t) { return (uint64_t)1; });
+}
+
 // The three filters and the choice.  total: the sum of the row's weights where the entries are
 // not all of them and top-k is off; 0: the sum of these is it.
 template <class S>
@@ -335,7 +410,7 @@ __device__ void choose(Shared& sh, const SampleArgs& a, int row, const Wish& w, 
   Border b{0, D};
   if (w.k > 0 && w.k < D) {
     auto one = [](uint32_t) { return (uint64_t)1; };
-    if (sum_of(sh, src, b, one) > (uint64_t)w.k)
+    if (src.count(sh) > (uint64_t)w.k)
       b = border_of(sh, src, D, top, low, b, (uint64_t)w.k, one);
   }
   if (w.p < 1.f) {
@@ -560,11 +635,10 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
     if (k_on && w.k <= n) {
       // the k-th largest of the chunks' largest keys, or a little less: k entries are at
       // least as large
-      auto one = [](uint32_t) { return (uint64_t)1; };
       const Maxima maxima{cmax, n};
-      uint64_t left = w.k;
+      auto one = [](uint32_t) { return (uint64_t)1; };
       if (sum_of(sh, maxima, Border{0, n}, one) >= (uint64_t)w.k)
-        least = key_at(sh, maxima, top, low, Border{0, n}, left, one, kList / 8);
+        least = key_near(sh, maxima, top, low, (uint64_t)w.k, kList / 16);
     }
     // (not where top-p asks for the weight of all that top-k leaves)
     if (w.q > 0.f && (w.p >= 1.f || total)) {
