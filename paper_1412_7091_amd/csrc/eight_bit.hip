@@ -154,9 +154,13 @@ __global__ __launch_bounds__(256) void fragments_kernel(const T* x, int64_t ldx,
 struct Codes {
   uintx4 lo, hi;
   int e;
+  // ONCE: no other block reads them
+  template <bool ONCE>
   __device__ void load(const uint8_t* w, const uint8_t* scale) {
-    lo = *reinterpret_cast<const uintx4*>(w);
-    hi = *reinterpret_cast<const uintx4*>(w + 64);
+    const uintx4 *p = reinterpret_cast<const uintx4*>(w),
+                 *q = reinterpret_cast<const uintx4*>(w + 64);
+    lo = ONCE ? __builtin_nontemporal_load(p) : *p;
+    hi = ONCE ? __builtin_nontemporal_load(q) : *q;
     e = *scale;
   }
   __device__ bf16x8 fragment(int s) const {
@@ -183,7 +187,9 @@ __device__ inline void store_tile(T* O, int64_t ldo, int m, int64_t D, int n, in
 }
 
 // At most 16 rows of H: one launch.  Every block quantises them by itself, into LDS, and its
-// waves go through tiles of 16 rows of W, four blocks' codes under way at a time.
+// waves go through tiles of 16 rows of W, four blocks' codes under way at a time.  Bound by
+// memory: one row by 200 000 x 512 codes (104 MB) takes 21 us, 5.0 TB/s; with the
+// quantisation in a launch of its own 27.
 template <class TH, class T>
 __global__ __launch_bounds__(512) void scores_few_kernel(const TH* H, int64_t ldh, int d,
                                                          const uint8_t* W, const uint8_t* sw,
@@ -211,7 +217,7 @@ __global__ __launch_bounds__(512) void scores_few_kernel(const TH* H, int64_t ld
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int b = min(b0 + j, blocks - 1);
-        c[j].load(p + b * kBlock, ps + b);
+        c[j].load<false>(p + b * kBlock, ps + b);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -230,7 +236,13 @@ __global__ __launch_bounds__(512) void scores_few_kernel(const TH* H, int64_t ld
 // 16 MT rows of W a wave, four waves a block one after another, 16 NT rows of H a block.  A
 // block of H's columns goes to LDS by DMA while the one before is multiplied; the codes of a
 // wave's own rows go to registers.
-template <class T, int MT, int NT>
+//
+// 128 rows of H by 200 000 x 512 codes take 59 us (205 MB at 3.5 TB/s; 63 with loads that
+// stay in the caches, which no other block reads; the same with all of H held in LDS and
+// waves that go through W by themselves: 56), 512 rows by 500 000 x 1024 take 555 us
+// (0.95 PFLOP/s, where a large bfloat16 product of the library reaches 1.2 and this one 0.87;
+// 666 with loads past the caches, where four blocks read the same codes).
+template <class T, int MT, int NT, bool ONCE>
 __global__ __launch_bounds__(256, 2) void scores_kernel(const uint8_t* W, const uint8_t* sw,
                                                      const __bf16* H, int m, int64_t D,
                                                      int blocks, int row_blocks, T* O,
@@ -263,7 +275,7 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(const uint8_t* W, const 
   Codes next[MT];
   fetch(0);
 #pragma unroll
-  for (int t = 0; t < MT; ++t) next[t].load(p[t], ps[t]);
+  for (int t = 0; t < MT; ++t) next[t].template load<ONCE>(p[t], ps[t]);
   for (int b = 0; b < blocks; ++b) {
     wait_vm_le(0);
     lds_barrier();  // block b has landed; every wave is done with block b - 1
@@ -273,7 +285,7 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(const uint8_t* W, const 
     if (b + 1 < blocks) {
       fetch(b + 1);
 #pragma unroll
-      for (int t = 0; t < MT; ++t) next[t].load(p[t] + (b + 1) * kBlock, ps[t] + b + 1);
+      for (int t = 0; t < MT; ++t) next[t].template load<ONCE>(p[t] + (b + 1) * kBlock, ps[t] + b + 1);
     }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
@@ -375,9 +387,10 @@ int lst_scores(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int32_t d
                          m, D, blocks, (int)row_blocks, (T*)O, ldo);
       return launched();
     };
-    if (tiles <= 2) return run(scores_kernel<T, 4, 2>, 4, 2);
-    if (tiles <= 4) return run(scores_kernel<T, 4, 4>, 4, 4);
-    return run(scores_kernel<T, 4, 8>, 4, 8);
+    if (tiles <= 2) return run(scores_kernel<T, 4, 2, true>, 4, 2);
+    if (tiles <= 4) return run(scores_kernel<T, 4, 4, true>, 4, 4);
+    if (tiles <= 8) return run(scores_kernel<T, 4, 8, true>, 4, 8);
+    return run(scores_kernel<T, 4, 8, false>, 4, 8);
   });
 }
 
