@@ -15,6 +15,7 @@ are tensors of their own for each call.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Tuple
 
@@ -465,7 +466,7 @@ def lst_dropout(x, p, seed, offset=0, *, residual=None, counter=None, out=None):
     px, ldx = _matrix(x, "x")
     code = _dtype_code(x, "x")
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = x.new_empty(x.shape)
     pr, ldr = _matrix(residual, "residual", x, x.shape)
     py, ldy = _matrix(out, "out", x, x.shape)
     _enqueue("lst_dropout", x.device, code, x.shape[0], x.shape[1], px, ldx, pr, ldr, py, ldy,
@@ -474,10 +475,12 @@ def lst_dropout(x, p, seed, offset=0, *, residual=None, counter=None, out=None):
     return out
 
 
+@functools.lru_cache(maxsize=256)
 def lst_recur_saved(rows: int, d: int) -> int:
     return int(load_library().lst_recur_saved(rows, d))
 
 
+@functools.lru_cache(maxsize=256)
 def lst_recur_workspace(rows: int, d: int) -> int:
     return int(load_library().lst_recur_workspace(rows, d))
 
@@ -509,11 +512,11 @@ def _recur_inputs(x, g, offsets, h0, n_seq):
                    _vector(h0, torch.float32, "h0", x.device)))
 
 
-def _recur_work(rows, d, device):
+def _work(like, n: int):
+    """n bytes of workspace beside a tensor, for one call (None for none)."""
     import torch
 
-    n = lst_recur_workspace(rows, d)
-    return torch.empty(n, dtype=torch.uint8, device=device) if n > 0 else None
+    return like.new_empty(n, dtype=torch.uint8) if n > 0 else None
 
 
 def lst_recur_forward(x, g, offsets=None, h0=None, *, n_seq=None, out=None, h_last=None,
@@ -524,13 +527,13 @@ def lst_recur_forward(x, g, offsets=None, h0=None, *, n_seq=None, out=None, h_la
     have, args = _recur_inputs(x, g, offsets, h0, n_seq)
     rows, d, dev = x.shape[0], x.shape[1], x.device
     if out is None:
-        out = torch.empty((rows, d), dtype=x.dtype, device=dev)
+        out = x.new_empty((rows, d))
     if h_last is None:
-        h_last = torch.empty((have, d), dtype=torch.float32, device=dev)
+        h_last = x.new_empty((have, d), dtype=torch.float32)
     saved = None
     if save:
-        saved = torch.empty((lst_recur_saved(rows, d) // d, d), dtype=torch.float32, device=dev)
-    work = _recur_work(rows, d, dev)
+        saved = x.new_empty((lst_recur_saved(rows, d) // d, d), dtype=torch.float32)
+    work = _work(x, lst_recur_workspace(rows, d))
     _enqueue("lst_recur_forward", dev, *args, *_matrix(out, "out", x, x.shape),
              _vector(h_last, torch.float32, "h_last", dev, have * d),
              None if saved is None else saved.data_ptr(),
@@ -547,9 +550,9 @@ def lst_recur_backward(x, g, grad_y, saved, offsets=None, h0=None, grad_last=Non
     have, args = _recur_inputs(x, g, offsets, h0, n_seq)
     rows, d, dev = x.shape[0], x.shape[1], x.device
     if out is None:
-        out = tuple(torch.empty((rows, d), dtype=x.dtype, device=dev) for _ in range(2))
-    grad_h0 = torch.empty((have, d), dtype=torch.float32, device=dev)
-    work = _recur_work(rows, d, dev)
+        out = x.new_empty((rows, d)), x.new_empty((rows, d))
+    grad_h0 = x.new_empty((have, d), dtype=torch.float32)
+    work = _work(x, lst_recur_workspace(rows, d))
     _enqueue("lst_recur_backward", dev, *args, *_matrix(grad_y, "grad_y", x, x.shape),
              _vector(grad_last, torch.float32, "grad_last", dev, have * d),
              _vector(saved, torch.float32, "saved", dev, lst_recur_saved(rows, d)),
@@ -570,7 +573,7 @@ def lst_recur_step(x, g, h, slots=None, *, out=None, status=None):
     if h.dim() != 2 or h.shape[1] != d:
         raise ValueError("h must be (n_slots, d)")
     if out is None:
-        out = torch.empty((rows, d), dtype=x.dtype, device=dev)
+        out = x.new_empty((rows, d))
     _enqueue("lst_recur_step", dev, code, rows, h.shape[0], d, px, ldx, pg, ldg,
              _vector(slots, torch.int32, "slots", dev, rows),
              _vector(h, torch.float32, "h", dev), *_matrix(out, "out", x, x.shape),
@@ -587,15 +590,16 @@ def lst_quantize(x, *, codes=None, scales=None):
     rows, cols = x.shape
     blocks = (cols + 127) // 128
     if codes is None:
-        codes = torch.empty((rows, 128 * blocks), dtype=torch.uint8, device=x.device)
+        codes = x.new_empty((rows, 128 * blocks), dtype=torch.uint8)
     if scales is None:
-        scales = torch.empty((rows, blocks), dtype=torch.uint8, device=x.device)
+        scales = x.new_empty((rows, blocks), dtype=torch.uint8)
     _enqueue("lst_quantize", x.device, code, rows, cols, px, ldx,
              _vector(codes, torch.uint8, "codes", x.device, rows * 128 * blocks),
              _vector(scales, torch.uint8, "scales", x.device, rows * blocks))
     return codes, scales
 
 
+@functools.lru_cache(maxsize=256)
 def lst_scores_workspace(m: int, d: int) -> int:
     return int(load_library().lst_scores_workspace(m, d))
 
@@ -612,19 +616,21 @@ def lst_scores(H, codes, scales, *, dtype=None, out=None):
     if scales.dim() != 2 or scales.shape[1] != blocks or codes.shape != (D, 128 * blocks):
         raise ValueError(f"codes and scales must be those of a matrix with {d} columns")
     if out is None:
-        out = torch.empty((m, D), dtype=dtype or H.dtype, device=dev)
+        out = H.new_empty((m, D), dtype=dtype or H.dtype)
     elif dtype is not None and out.dtype != dtype:
         raise TypeError(f"out must be {dtype}, got {out.dtype}")
     po, ldo = _matrix(out, "out", shape=(m, D))
     if out.device != dev:
         raise TypeError(f"out must be on {dev}")
-    work = torch.empty(max(0, lst_scores_workspace(m, d)), dtype=torch.uint8, device=dev)
+    work = _work(H, lst_scores_workspace(m, d))
     _enqueue("lst_scores", dev, code, _dtype_code(out, "out"), m, D, d, ph, ldh,
              _vector(codes, torch.uint8, "codes", dev),
-             _vector(scales, torch.uint8, "scales", dev), po, ldo, work.data_ptr())
+             _vector(scales, torch.uint8, "scales", dev), po, ldo,
+             None if work is None else work.data_ptr())
     return out
 
 
+@functools.lru_cache(maxsize=256)
 def lst_sample_workspace(m: int, D: int) -> int:
     return int(load_library().lst_sample_workspace(m, D))
 
@@ -639,11 +645,10 @@ def lst_sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=Non
     code = _dtype_code(logits, "logits")
     (m, D), dev = logits.shape, logits.device
     if tokens is None:
-        tokens = torch.empty(m, dtype=torch.int32, device=dev)
+        tokens = logits.new_empty(m, dtype=torch.int32)
     if prob is None:
-        prob = torch.empty(m, dtype=torch.float32, device=dev)
-    n = lst_sample_workspace(m, D)
-    work = torch.empty(n, dtype=torch.uint8, device=dev) if n > 0 else None
+        prob = logits.new_empty(m, dtype=torch.float32)
+    work = _work(logits, lst_sample_workspace(m, D))
     f32 = torch.float32
     if u is None:
         raise TypeError("u must be a device vector of float32")

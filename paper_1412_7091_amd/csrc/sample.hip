@@ -22,7 +22,7 @@ constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 2048;
 constexpr int kDigit = 11;     // bits of a pass: kBins = 2^kDigit
-constexpr int kChunk = 128;    // entries whose largest key is kept
+constexpr int kChunk = 64;     // entries whose largest key is kept
 constexpr int kStretch = 4096; // entries of one block of the first launch
 constexpr int kList = 4096;    // entries that one block lists, at most
 constexpr int kFine = 4096;    // bins of a row's values
@@ -53,11 +53,11 @@ struct SampleArgs {
   int shift;    // weights are multiples of 2^-shift
   double unit;  // 2^shift
   // the workspace, for rows longer than kShort: the largest key of each chunk; of each stretch
-  // the smallest key and the sum of its weights, relative to its largest, then the weight of
-  // its entries in the bins before the last and the number of those in it; per row its plan,
-  // bins, and a list
+  // the smallest and the largest key and the sum of its weights, relative to the largest, then
+  // the weight of its entries in the bins before the last and the number of those in it; per
+  // row its plan, bins, and a list
   int chunks, stretches, segments;
-  uint32_t *chunk_max, *stretch_min;
+  uint32_t *chunk_max, *stretch_min, *stretch_max;
   double* stretch_sum;
   uint64_t* stretch_mass;
   int* stretch_count;
@@ -154,6 +154,7 @@ struct Shared {
   int few, few_at;
   uint32_t few_keys[64], few_key;
   int few_indexes[64];
+  uint64_t few_values[64];
 };
 
 // The first bin at which the running sum reaches target (at most the total): sh.found, and
@@ -262,10 +263,13 @@ __device__ void settle(Shared& sh, uint64_t target, V value, B before) {
   if (l < 64 && l < n) {
     const uint32_t key = sh.few_keys[l];
     const int index = sh.few_indexes[l];
+    const uint64_t own = value(key);
+    sh.few_values[l] = own;
+    __builtin_amdgcn_wave_barrier();
     uint64_t sum = 0;
     for (int j = 0; j < n; ++j)
-      if (before(sh.few_keys[j], sh.few_indexes[j], key, index)) sum += value(sh.few_keys[j]);
-    if (sum < target && target <= sum + value(key)) sh.few_key = key, sh.few_at = index;
+      if (before(sh.few_keys[j], sh.few_indexes[j], key, index)) sum += sh.few_values[j];
+    if (sum < target && target <= sum + own) sh.few_key = key, sh.few_at = index;
   }
   __syncthreads();
 }
@@ -452,7 +456,7 @@ __device__ inline bool wants_sum(const Wish& w, int D) {
 }
 
 // The largest key of every chunk, and the smallest key and the sum of every stretch: one read
-// of the row.  A block has one stretch, a half-wave a chunk at a time.
+// of the row.  A block has one stretch, 16 lanes a chunk at a time.
 template <class T>
 __global__ __launch_bounds__(256) void sample_stats_kernel(SampleArgs a, const T* logits) {
   __shared__ double roots[64];
@@ -483,19 +487,21 @@ __global__ __launch_bounds__(256) void sample_stats_kernel(SampleArgs a, const T
 #pragma unroll
     for (int j = 0; j < 4; ++j) low = min(low, key[s][j] - 1);  // 0, none, becomes the largest
 #pragma unroll
-    for (int o = 16; o; o >>= 1) k = max(k, (uint32_t)__shfl_xor((int)k, o));
+    for (int o = kChunk / 8; o; o >>= 1) k = max(k, (uint32_t)__shfl_xor((int)k, o));
     const int64_t chunk = (base + s * 1024) / kChunk;
-    if (tid % 32 == 0 && chunk < a.chunks) a.chunk_max[(int64_t)row * a.chunks + chunk] = k;
+    if (tid % (kChunk / 4) == 0 && chunk < a.chunks) a.chunk_max[(int64_t)row * a.chunks + chunk] = k;
     top = max(top, k);
   }
-  top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+  for (int o = 32; o >= kChunk / 4; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
   for (int o = 32; o; o >>= 1) low = min(low, (uint32_t)__shfl_xor((int)low, o));
   if (tid % 64 == 0) wave_max[tid / 64] = top, wave_min[tid / 64] = low;
   __syncthreads();
   top = max(max(wave_max[0], wave_max[1]), max(wave_max[2], wave_max[3]));
   const int64_t at = (int64_t)row * a.stretches + stretch;
-  if (tid == 0)
+  if (tid == 0) {
     a.stretch_min[at] = min(min(wave_min[0], wave_min[1]), min(wave_min[2], wave_min[3])) + 1;
+    a.stretch_max[at] = top;
+  }
   const Wish w = wish_of(a, row);
   if (!wants_sum(w, a.D)) return;
   const Weights of = weights_of(a, roots, top, w.t);
@@ -592,11 +598,7 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
   if (wants_sum(w, D) && w.u > 0.f && a.stretches <= kBins) {
     clear_bins(sh);
     for (int i = tid; i < a.stretches; i += kThreads) {
-      uint32_t k = 0;
-      for (int j = 0; j < kStretch / kChunk; ++j) {
-        const int c = i * (kStretch / kChunk) + j;
-        if (c < n) k = max(k, cmax[c]);
-      }
+      const uint32_t k = a.stretch_max[(int64_t)row * a.stretches + i];
       const double sum = a.stretch_sum[(int64_t)row * a.stretches + i] * of.of(k);
       sh.bin[i] = k ? (uint64_t)(sum * a.unit + 0.5) : 0;
     }
@@ -659,7 +661,8 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
         if (h < kList) ps.hits[h] = i;
       }
     __syncthreads();
-    // a half-wave a chunk, four chunks under way
+    // a half-wave a chunk, four chunks under way: bound by what one block can fetch (chunks of
+    // 128 took twice the time)
     const int hits = ps.n_hits <= kList ? ps.n_hits : 0;
     for (int h0 = tid / 32; h0 < hits; h0 += 4 * (kThreads / 32)) {
       T v[4][kChunk / 32];
@@ -1044,6 +1047,7 @@ Layout layout(int m, int D, char* p) {
   };
   take(a.stretch_sum, (int64_t)m * a.stretches);
   take(a.stretch_min, (int64_t)m * a.stretches);
+  take(a.stretch_max, (int64_t)m * a.stretches);
   take(a.chunk_max, (int64_t)m * a.chunks);
   take(a.stretch_mass, (int64_t)m * a.stretches);
   take(a.stretch_count, (int64_t)m * a.stretches);
