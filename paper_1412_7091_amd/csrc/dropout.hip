@@ -68,17 +68,10 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(DropoutArgs a, const 
     group[j] = (int)(at - row[j] * (I)a.groups);
     if (at >= total) continue;
     const int col = group[j] * kGroup;
-    const T *px = x + (int64_t)row[j] * a.ldx + col, *pr = res + (int64_t)row[j] * a.ldr + col;
-    if (WHOLE || col + kGroup <= a.cols) {
-      load_vec(px, v[j]);
-      if (RES) load_vec(pr, r[j]);
-    } else {
-      for (int i = 0; i < kGroup; ++i) {
-        const bool in = col + i < a.cols;
-        v[j][i] = in ? px[i] : (T)0.f;
-        if (RES) r[j][i] = in ? pr[i] : (T)0.f;
-      }
-    }
+    const T *px = x + (int64_t)row[j] * a.ldx, *pr = res + (int64_t)row[j] * a.ldr;
+    const int cols = WHOLE ? col + kGroup : a.cols;
+    load_part(px, col, cols, v[j]);
+    if (RES) load_part(pr, col, cols, r[j]);
   }
 #pragma unroll
   for (int j = 0; j < kItems; ++j) {

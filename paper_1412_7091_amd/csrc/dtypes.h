@@ -29,6 +29,24 @@ __device__ inline void load_vec(const T* p, T (&v)[N]) {
   }
 }
 
+// N elements of a row of `cols`, from column `col`; zeros behind the last.  The loads at the
+// end do not depend on each other: with a branch for each they wait for one another.
+template <class T, int N>
+__device__ inline void load_part(const T* row, int col, int cols, T (&v)[N]) {
+  if (col + N <= cols) {
+    load_vec(row + col, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = (T)0.f;
+    if (col < cols) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = row[min(col + i, cols - 1)];
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = col + i < cols ? v[i] : (T)0.f;
+    }
+  }
+}
+
 template <class T, int N>
 __device__ inline void store_vec(T* p, const T (&v)[N]) {
   if constexpr (N == 1) {

@@ -74,12 +74,7 @@ __device__ inline bf16x8 widen(uintx2 q, float scale) {
 template <class T>
 __device__ inline void block_codes(const T* row, int col, int cols, uint32_t (&q)[2], int& e) {
   T raw[8];
-  if (col + 8 <= cols) {
-    load_vec(row + col, raw);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) raw[i] = col + i < cols ? row[col + i] : (T)0.f;
-  }
+  load_part(row, col, cols, raw);
   float v[8];
   uint32_t big = 0;  // largest magnitude, by its bits
 #pragma unroll
