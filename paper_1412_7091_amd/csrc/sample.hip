@@ -11,6 +11,20 @@
 // Weights are computed in float64 and added as integers, multiples of 2^-shift with
 // the shift as large as D sums of at most 1 allow (51 at most): sums of integers do
 // not depend on the order in which the atomics arrive, so the choice does not either.
+//
+// Rows of up to 8192 entries take one block each.  Longer ones are read by many blocks,
+// once for the largest key of every 64 entries.  From those a bound follows that few
+// entries reach where top-k or min-p is on, and one block a row ends it.  Without either,
+// the row's weights go into 4096 bins by value (a second read), and the bin that top-p's
+// border falls into is listed while the weights before it are added up by stretches of
+// 4096 entries (a third).  A row whose border lies among more than 8192 unequal entries
+// of one bin is left to one block that goes over it digit by digit.
+//
+// Measured: one row of 200 000 floats with top-k 27 us, six launches that wait for each
+// other; 128 such rows with all kinds of settings 131 us (24 for the read of 102 MB), 64
+// rows of 793 471 bfloat16 with top-p alone 210 us (29 for the read).  The second and
+// third pass are bound by the weights' arithmetic (64 and 96 us), the rest by the latency
+// of blocks that search.  One block a row alone took 438, 938 and 3500 us.
 #include <algorithm>
 
 #include "dtypes.h"
@@ -901,6 +915,7 @@ __global__ __launch_bounds__(256) void sample_list_kernel(SampleArgs a, const T*
   }
   if (n == 0) return;
   __syncthreads();
+  if (first >= kLong) return;  // the list is full: its row goes by the numbers or by itself
   unsigned at = first + upto - own;
   for (int k = 0; k < tid / 64; ++k) at += wave_count[k];
 #pragma unroll
