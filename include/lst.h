@@ -411,7 +411,7 @@ enum { LST_F32 = 0, LST_BF16 = 1, LST_F16 = 2 };
 /*
  * lst_dropout -- y = residual + x * keep / (1 - p), the mask drawn by a
  * counter-based generator and never stored.
- *   rows, cols      0 <= rows <= 2^32, cols >= 1.
+ *   rows, cols      0 <= rows <= 2^32, 1 <= cols <= 2^30.
  *   x, residual, y  rows x cols; residual may be NULL; y may be x or residual.
  *   p               probability that an element is dropped, in [0, 1], rounded to a
  *                   multiple of 2^-16; the factor is that of the rounded p.  A
@@ -433,8 +433,8 @@ int lst_dropout(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_
 /*
  * lst_recur_forward -- a gated linear recurrence over packed sequences:
  *   f_t = sigmoid(g_t),  h_t = f_t h_{t-1} + (1 - f_t) x_t,  y_t = h_t,
- * for each of the d channels (1..4096) by itself.
- *   x, g, y          rows x d, the sequences' rows one after another.
+ * for each of the d channels (1..4096) by itself; at most 2^30 rows and sequences.
+ *   x, g, y          rows x d, the sequences' rows one after another; y may be x or g.
  *   offsets (device) n_seq + 1 ints, ascending: sequence s has the rows offsets[s] ..
  *                    offsets[s + 1] - 1, possibly none.  NULL: n_seq sequences of
  *                    rows / n_seq rows each.  Rows of y in no sequence are left as
@@ -456,7 +456,8 @@ int lst_recur_forward(int32_t dtype, int32_t rows, int32_t n_seq, int32_t d, con
  * lst_recur_backward -- gradients of lst_recur_forward.  x, g, offsets and h0 as
  * there, saved from that call; grad_y (rows x d) and grad_last (n_seq x d floats, or
  * NULL) are dL/dy and dL/dh_last.  grad_x and grad_g receive dL/dx and dL/dg (rows in
- * no sequence are left as they were), grad_h0 (or NULL) dL/dh0.
+ * no sequence are left as they were), grad_h0 (or NULL) dL/dh0.  grad_x and grad_g
+ * may each be one of x, g and grad_y.
  */
 int lst_recur_backward(int32_t dtype, int32_t rows, int32_t n_seq, int32_t d, const void* x,
                        int64_t ldx, const void* g, int64_t ldg, const int32_t* offsets,
@@ -476,7 +477,8 @@ int64_t lst_recur_workspace(int32_t rows, int32_t d);
  *   slots (device)  rows ints: the state that row i continues; -1: none, its row of y
  *                   is left as it was.  NULL: row i continues state i.  An index
  *                   outside [-1, n_slots), and one that an earlier row names already,
- *                   sets the status LST_EINDEX and counts as -1.
+ *                   sets the status LST_EINDEX and counts as -1.  At most 65 536 rows
+ *                   with slots, since each is compared with those before it.
  */
 int lst_recur_step(int32_t dtype, int32_t rows, int32_t n_slots, int32_t d, const void* x,
                    int64_t ldx, const void* g, int64_t ldg, const int32_t* slots, float* h,
@@ -485,7 +487,7 @@ int lst_recur_step(int32_t dtype, int32_t rows, int32_t n_slots, int32_t d, cons
 /*
  * lst_quantize -- a matrix (the weights of a trained layer: lst_materialize_W) into
  * 8 bits, with one scale for each block of 128 columns of a row.
- *   x       rows x cols, 1 <= cols <= 4096.
+ *   x       rows x cols, 1 <= cols <= 4096; rows x b below 2^28 - 15.
  *   codes  (device)  rows x 128 b bytes, b = (cols + 127) / 128, 16-byte aligned:
  *                    receives e4m3 values, zeros behind the last column.
  *   scales (device)  rows x b bytes: receives biased exponents; a value of the block
@@ -502,7 +504,9 @@ int lst_quantize(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64
  *   H                m x d of type dtype, quantised by the call as lst_quantize does.
  *   codes, scales    W (D x d) as lst_quantize leaves it.
  *   O                m x D of type out_dtype.
- * The quantised values are multiplied exactly and summed in float32.
+ *   m <= 2^20, D <= 2^36; for m > 16 or d > 2048, D <= 2^31 and m D <= 2^37.
+ * The quantised values are multiplied exactly and summed in float32 (those below
+ * 2^-126 may count as zero).
  */
 int lst_scores(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int32_t d, const void* H,
                int64_t ldh, const uint8_t* codes, const uint8_t* scales, void* O, int64_t ldo,
@@ -511,7 +515,7 @@ int64_t lst_scores_workspace(int32_t m, int32_t d); /* bytes; -1 for a bad size 
 
 /*
  * lst_sample -- a token from each row of outputs.
- *   logits            m x D, D >= 1.  Entries that are -inf or no number are never
+ *   logits            m x D, 1 <= D <= 2^30.  Entries that are -inf or no number are never
  *                     chosen; when some are +inf, the choice is among those.
  *   temperature, top_k, top_p, min_p, u (device, m values each; the first four may
  *                     be NULL: 1, 0, 1, 0).

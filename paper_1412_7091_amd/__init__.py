@@ -502,6 +502,8 @@ def _recur_inputs(x, g, offsets, h0, n_seq):
         have = h0.shape[0] if h0 is not None else 1
     if n_seq is not None and n_seq != have:
         raise ValueError("n_seq and offsets disagree")
+    if have > 1 << 30:
+        raise ValueError("at most 2^30 sequences")
     rows, d = x.shape
     if h0 is not None and tuple(h0.shape) != (have, d):
         raise ValueError("h0 must be (n_seq, d)")
@@ -532,7 +534,8 @@ def lst_recur_forward(x, g, offsets=None, h0=None, *, n_seq=None, out=None, h_la
         h_last = x.new_empty((have, d), dtype=torch.float32)
     saved = None
     if save:
-        saved = x.new_empty((lst_recur_saved(rows, d) // d, d), dtype=torch.float32)
+        saved = x.new_empty((max(lst_recur_saved(rows, d), 0) // max(d, 1), d),
+                            dtype=torch.float32)
     work = _work(x, lst_recur_workspace(rows, d))
     _enqueue("lst_recur_forward", dev, *args, *_matrix(out, "out", x, x.shape),
              _vector(h_last, torch.float32, "h_last", dev, have * d),
@@ -570,7 +573,7 @@ def lst_recur_step(x, g, h, slots=None, *, out=None, status=None):
     code = _dtype_code(x, "x")
     pg, ldg = _matrix(g, "g", x, x.shape)
     rows, d, dev = x.shape[0], x.shape[1], x.device
-    if h.dim() != 2 or h.shape[1] != d:
+    if h.dim() != 2 or h.shape[1] != d or h.shape[0] > 0x7FFFFFFF:
         raise ValueError("h must be (n_slots, d)")
     if out is None:
         out = x.new_empty((rows, d))

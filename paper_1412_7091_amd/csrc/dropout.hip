@@ -108,7 +108,8 @@ extern "C" int lst_dropout(int32_t dtype, int64_t rows, int32_t cols, const void
                            const void* residual, int64_t ldr, void* y, int64_t ldy, double p,
                            uint64_t seed, uint64_t offset, const uint64_t* counter,
                            void* hip_stream) {
-  if (!known_dtype(dtype) || rows < 0 || rows > (int64_t)1 << 32 || cols < 1) return LST_EINVAL;
+  if (!known_dtype(dtype) || rows < 0 || rows > (int64_t)1 << 32 || cols < 1 || cols > 1 << 30)
+    return LST_EINVAL;
   if (!(p >= 0.0) || !(p <= 1.0)) return LST_EINVAL;
   if (rows == 0) return LST_OK;
   if (!x || !y || ldx < cols || ldy < cols || (residual && ldr < cols)) return LST_EINVAL;
@@ -125,7 +126,7 @@ extern "C" int lst_dropout(int32_t dtype, int64_t rows, int32_t cols, const void
   a.offset = offset;
   a.counter = counter;
   const int64_t total = rows * a.groups, per = kThreads * kItems;
-  if ((total + per - 1) / per > 0x7FFFFFFF) return LST_EINVAL;
+  if ((total + per - 1) / per > 0xFFFFFF) return LST_EINVAL;  // a launch has 2^32 threads at most
   const unsigned blocks = (unsigned)((total + per - 1) / per);
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);

@@ -106,14 +106,14 @@ __device__ inline void block_codes(const T* row, int col, int cols, uint32_t (&q
 // 16 lanes a block, eight columns a lane.  Bound by memory: 793 471 x 300 floats (1.26 GB
 // with the codes) take 213 us, 5.9 TB/s; 32 lanes a block, four columns a lane with an access
 // for each, took 305 us.
-template <class T, class I>
+template <class T>
 __global__ __launch_bounds__(256) void quantize_kernel(const T* x, int64_t ldx, int64_t rows,
                                                        int cols, int blocks, uint8_t* codes,
                                                        uint8_t* scales) {
-  const I at = (I)blockIdx.x * 16 + threadIdx.x / 16;  // the block
-  if (at >= (I)(rows * blocks)) return;
-  const I row = at / (I)blocks;
-  const int l = threadIdx.x % 16, col = (int)(at - row * (I)blocks) * kBlock + 8 * l;
+  const unsigned at = blockIdx.x * 16 + threadIdx.x / 16;  // the block
+  if (at >= (unsigned)(rows * blocks)) return;
+  const unsigned row = at / (unsigned)blocks;
+  const int l = threadIdx.x % 16, col = (int)(at - row * (unsigned)blocks) * kBlock + 8 * l;
   uint32_t q[2];
   int e;
   block_codes(x + (int64_t)row * ldx, col, cols, q, e);
@@ -307,6 +307,7 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(const uint8_t* W, const 
 constexpr int kFew = 16;          // rows of H that one launch takes
 constexpr int kFewColumns = 2048;  // that fit 64 KB of LDS in bfloat16
 constexpr int kFewBlocks = 512;   // blocks of that launch, two a compute unit
+constexpr int64_t kMostBlocks = (1 << 28) - 16;  // of a matrix: 2^32 threads
 
 int64_t blocks_of(int32_t cols) { return ((int64_t)cols + kBlock - 1) / kBlock; }
 
@@ -322,15 +323,13 @@ int lst_quantize(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64
   if (!known_dtype(dtype) || rows < 0 || cols < 1 || cols > 4096) return LST_EINVAL;
   if (rows == 0) return LST_OK;
   if (!x || !codes || !scales || ldx < cols || ((uintptr_t)codes & 15)) return LST_EINVAL;
-  const int64_t blocks = rows * blocks_of(cols), n = (blocks + 15) / 16;
-  if (n > 0x7FFFFFFF) return LST_EINVAL;
+  if (rows > kMostBlocks / blocks_of(cols)) return LST_EINVAL;
+  const int64_t n = (rows * blocks_of(cols) + 15) / 16;
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
-    auto run = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)n), dim3(256), 0, (hipStream_t)hip_stream,
-                         (const T*)x, ldx, rows, cols, (int)blocks_of(cols), codes, scales);
-    };
-    blocks <= 0x7FFFFFFF ? run(quantize_kernel<T, uint32_t>) : run(quantize_kernel<T, int64_t>);
+    hipLaunchKernelGGL(quantize_kernel<T>, dim3((unsigned)n), dim3(256), 0,
+                       (hipStream_t)hip_stream, (const T*)x, ldx, rows, cols,
+                       (int)blocks_of(cols), codes, scales);
     return launched();
   });
 }
@@ -364,6 +363,11 @@ int lst_scores(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int32_t d
         return launched();
       });
     });
+  // 256 rows of W and up to 8 tiles of H a block
+  const int nt = tiles <= 2 ? 2 : tiles <= 4 ? 4 : 8;
+  const int64_t row_blocks = (D + 255) / 256;
+  const int64_t grid = (row_blocks + 7) / 8 * 8 * ((tiles + nt - 1) / nt);
+  if (grid > 0xFFFFFF) return LST_EINVAL;  // a launch has 2^32 threads at most
   __bf16* fragments = (__bf16*)workspace;
   int rc = with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
@@ -374,18 +378,14 @@ int lst_scores(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int32_t d
   if (rc != LST_OK) return rc;
   return with_dtype(out_dtype, [&](auto t) {
     using T = decltype(t);
-    auto run = [&](auto kernel, int mt, int nt) {
-      const int64_t row_blocks = (D + 64 * mt - 1) / (64 * mt), cols = (tiles + nt - 1) / nt;
-      const int64_t grid = (row_blocks + 7) / 8 * 8 * cols;
-      if (row_blocks > 0x7FFFFFF0 || grid > 0x7FFFFFFF) return (int)LST_EINVAL;
+    auto run = [&](auto kernel) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, s, codes, scales, fragments,
                          m, D, blocks, (int)row_blocks, (T*)O, ldo);
       return launched();
     };
-    if (tiles <= 2) return run(scores_kernel<T, 4, 2, true>, 4, 2);
-    if (tiles <= 4) return run(scores_kernel<T, 4, 4, true>, 4, 4);
-    if (tiles <= 8) return run(scores_kernel<T, 4, 8, true>, 4, 8);
-    return run(scores_kernel<T, 4, 8, false>, 4, 8);
+    if (nt == 2) return run(scores_kernel<T, 4, 2, true>);
+    if (nt == 4) return run(scores_kernel<T, 4, 4, true>);
+    return tiles <= 8 ? run(scores_kernel<T, 4, 8, true>) : run(scores_kernel<T, 4, 8, false>);
   });
 }
 

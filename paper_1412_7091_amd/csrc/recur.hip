@@ -109,12 +109,11 @@ __device__ inline Pair unpack(unsigned long long v) {
 }
 
 // ------------------------------------------------------------- the workspace
-constexpr int kRows = 16;                     // rows a wave
-constexpr int kWaves = kChunk / kRows;       // waves a block
-constexpr int kThreads = 64 * kWaves;
 constexpr int kGroupChunks = 16;             // chunks whose pair is published together
 constexpr int kHead = 64;                    // bytes before the words: the ticket
 constexpr int kPolls = 1 << 22;              // several seconds: never reached
+constexpr int kMost = 1 << 30;               // rows, sequences: with a block's step below 2^31
+constexpr int kMostSlots = 1 << 16;          // of a step: each is compared with those before it
 
 struct Shape {
   int chunks, tiles, width;  // width: channels of all tiles
@@ -654,7 +653,7 @@ __global__ __launch_bounds__(256) void recur_step_kernel(int n_slots, int d, con
     return;
   }
   if (slot < 0) return;
-  for (int c = blockIdx.y * 256 + threadIdx.x; c < d; c += gridDim.y * 256) {
+  for (int c = threadIdx.x; c < d; c += 256) {
     float f, i;
     gate<T>((float)g[row * ldg + c], f, i);
     float* p = h + (int64_t)slot * d + c;
@@ -667,6 +666,7 @@ __global__ __launch_bounds__(256) void recur_step_kernel(int n_slots, int d, con
 int check_recur(int dtype, int rows, int n_seq, int d, const void* x, int64_t ldx, const void* g,
                 int64_t ldg, const int32_t* offsets) {
   if (!known_dtype(dtype) || rows < 0 || n_seq < 0 || d < 1 || d > 4096) return LST_EINVAL;
+  if (rows > kMost || n_seq > kMost) return LST_EINVAL;
   if (n_seq == 0 && rows != 0 && !offsets) return LST_EINVAL;
   if (!offsets && n_seq && rows % n_seq) return LST_EINVAL;
   if (rows && (!x || !g || ldx < d || ldg < d)) return LST_EINVAL;
@@ -707,11 +707,11 @@ using namespace lst;
 extern "C" {
 
 int64_t lst_recur_saved(int32_t rows, int32_t d) {
-  return rows < 0 || d < 1 ? -1 : ((int64_t)rows + kChunk - 1) / kChunk * d;
+  return rows < 0 || rows > kMost || d < 1 || d > 4096 ? -1 : ((int64_t)rows + kChunk - 1) / kChunk * d;
 }
 
 int64_t lst_recur_workspace(int32_t rows, int32_t d) {
-  if (rows < 0 || d < 1) return -1;
+  if (rows < 0 || rows > kMost || d < 1 || d > 4096) return -1;
   const Shape s = shape_of(rows, d, 2);  // as wide as with one channel a lane, or wider
   return s.joined() ? kHead + s.words() * (int64_t)sizeof(unsigned long long) : 0;
 }
@@ -770,7 +770,7 @@ int lst_recur_step(int32_t dtype, int32_t rows, int32_t n_slots, int32_t d, cons
                    int64_t ldx, const void* g, int64_t ldg, const int32_t* slots, float* h,
                    void* y, int64_t ldy, int32_t* status, void* hip_stream) {
   if (!known_dtype(dtype) || rows < 0 || n_slots < 0 || d < 1 || d > 4096) return LST_EINVAL;
-  if (!slots && rows > n_slots) return LST_EINVAL;
+  if (slots ? rows > kMostSlots : rows > n_slots || rows > 0xFFFFFF) return LST_EINVAL;
   if (rows == 0) return LST_OK;
   if (!x || !g || !h || !y || ldx < d || ldg < d || ldy < d) return LST_EINVAL;
   return with_dtype(dtype, [&](auto t) {

@@ -44,17 +44,21 @@ constexpr int kSegment = 32768; // entries of one block that sorts them into bin
 constexpr int kLong = 8192;    // entries of a row's list in memory, at most
 constexpr int kShort = 8192;   // rows up to this length take one launch
 constexpr int kBatch = 1024;   // rows of one set of launches
+constexpr int kMostRows = 1 << 20;     // of short rows' one launch
+constexpr int kMostEntries = 1 << 30;  // of a row: an index and a block's step stay below 2^31
 
 // What the launches leave each other of a long row.
 enum { ROW_OPEN = 0, ROW_DONE = 1, ROW_MASS = 2, ROW_COUNT = 3 };
-struct alignas(128) RowPlan {
+struct RowPlan {
   int state;
   uint32_t top;     // the largest key
   float top_value, scale;  // bin = (top_value - x) scale
   int bin;          // the one that holds the last entry kept
   uint64_t left;    // ROW_MASS: what the bin's entries have to give
   // on a line of its own, since blocks add to it while others read what is above
-  alignas(64) unsigned listed;  // entries of the bin (ROW_COUNT: of all up to it)
+  int apart[24];
+  unsigned listed;  // entries of the bin (ROW_COUNT: of all up to it)
+  int behind[31];
 };
 
 struct SampleArgs {
@@ -221,6 +225,7 @@ __device__ void extremes(Shared& sh, uint32_t& least, uint32_t& most) {
   __syncthreads();
   for (int i = 0; i < kWaves; ++i)
     most = max(most, sh.key[i]), least = min(least, (uint32_t)sh.idx[i]);
+  __syncthreads();  // the row's own search writes them again
 }
 
 __device__ void clear_bins(Shared& sh) {
@@ -1058,7 +1063,7 @@ Layout layout(int m, int D, char* p) {
   int64_t at = 0;
   auto take = [&](auto*& q, int64_t n) {
     q = (std::remove_reference_t<decltype(q)>)(p + at);
-    at += (n * (int64_t)sizeof(*q) + 15) / 16 * 16;
+    at += (n * (int64_t)sizeof(*q) + 127) / 128 * 128;
   };
   take(a.stretch_sum, (int64_t)m * a.stretches);
   take(a.stretch_min, (int64_t)m * a.stretches);
@@ -1084,7 +1089,7 @@ using namespace lst;
 extern "C" {
 
 int64_t lst_sample_workspace(int32_t m, int32_t D) {
-  if (m < 0 || D < 1) return -1;
+  if (m < 0 || D < 1 || D > kMostEntries) return -1;
   return D <= kShort ? 0 : layout(std::min(m, kBatch), D, nullptr).bytes;
 }
 
@@ -1092,7 +1097,7 @@ int lst_sample(int32_t dtype, int32_t m, int32_t D, const void* logits, int64_t 
                const float* temperature, const int32_t* top_k, const float* top_p,
                const float* min_p, const float* u, int32_t* tokens, float* prob, void* workspace,
                void* hip_stream) {
-  if (!known_dtype(dtype) || m < 0 || D < 1) return LST_EINVAL;
+  if (!known_dtype(dtype) || m < 0 || D < 1 || D > kMostEntries) return LST_EINVAL;
   if (m == 0) return LST_OK;
   if (!logits || !u || !tokens || ldx < D) return LST_EINVAL;
   if (D > kShort && (!workspace || ((uintptr_t)workspace & 15))) return LST_EINVAL;
@@ -1102,8 +1107,9 @@ int lst_sample(int32_t dtype, int32_t m, int32_t D, const void* logits, int64_t 
   return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
     // long rows a batch at a time: the workspace is that of a batch
-    for (int r = 0; r < m; r += kBatch) {
-      const int n = std::min(kBatch, m - r);
+    const int batch = D > kShort ? kBatch : kMostRows;
+    for (int64_t r = 0; r < m; r += batch) {
+      const int n = (int)std::min<int64_t>(batch, m - r);
       SampleArgs a{};
       if (D > kShort) a = layout(n, D, (char*)workspace).args;
       a.m = n, a.D = D, a.ldx = ldx, a.u = u + r, a.tokens = tokens + r;

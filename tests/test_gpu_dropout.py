@@ -162,3 +162,16 @@ def test_refusals_on_host():
         lst.Dropout(1.5)
     with pytest.raises(TypeError):
         lst.lst_dropout(torch.zeros(2, 8), 0.5, 1)
+
+
+def test_sizes_behind_the_limits():
+    """Refused on the host: columns counted in 32 bits with a block's step behind the last one,
+    and launches of more than 2^32 threads."""
+    lib = lst.load_library()
+    P = 16  # never dereferenced
+
+    def call(rows, cols):
+        return lib.lst_dropout(1, rows, cols, P, cols, None, 0, P, cols, 0.5, 1, 0, None, None)
+
+    for rows, cols in ((1, (1 << 30) + 1), (1, 0x7FFFFFFF), (1 << 32, 64)):
+        assert call(rows, cols) == lst.LST_EINVAL, (rows, cols)

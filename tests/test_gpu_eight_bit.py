@@ -259,3 +259,13 @@ def test_refusals_on_host():
             == lst.LST_EINVAL, kw
     assert scores(m=0, H=None) == lst.LST_OK
     assert lst.lst_scores_workspace(3, 129) >= 3 * 258 and lst.lst_scores_workspace(1, 5000) == -1
+
+
+def test_sizes_behind_the_limits():
+    """Refused on the host: launches of more than 2^32 threads."""
+    lib = lst.load_library()
+    P = 64  # never dereferenced
+    for rows, cols in (((1 << 28) - 15, 128), (1 << 27, 129), (1 << 40, 1)):
+        assert lib.lst_quantize(0, rows, cols, P, cols, P, P, None) == lst.LST_EINVAL
+    for m, D in (((1 << 20) + 1, 5), (1 << 20, 1 << 20), (17, 1 << 36)):
+        assert lib.lst_scores(0, 0, m, D, 8, P, 8, P, P, P, D, P, None) == lst.LST_EINVAL

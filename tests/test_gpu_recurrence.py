@@ -359,3 +359,47 @@ def test_refusals_on_host():
     assert step(rows=0) == lst.LST_OK
     assert lst.lst_recur_saved(129, 5) == 10 and lst.lst_recur_saved(-1, 5) == -1
     assert lst.lst_recur_workspace(-1, 5) == -1
+
+
+def test_sizes_behind_the_limits():
+    """Refused on the host: more than 2^30 rows or sequences, whose counts with a block's step
+    leave 32 bits, and more slots than each can be compared with."""
+    lib = lst.load_library()
+    P = 16  # never dereferenced
+    for rows, n in (((1 << 30) + 1, 1), (0x7FFFFFFF, 1), (4, (1 << 30) + 1), (4, 0x7FFFFFFF)):
+        assert lib.lst_recur_forward(1, rows, n, 1, P, 1, P, 1, P, None, P, 1, None, None, P,
+                                     None, None) == lst.LST_EINVAL
+        assert lib.lst_recur_backward(1, rows, n, 1, P, 1, P, 1, P, None, P, 1, None, P, P, 1, P,
+                                      1, None, P, None, None) == lst.LST_EINVAL
+    assert lst.lst_recur_saved((1 << 30) + 1, 1) == lst.lst_recur_saved(1, 4097) == -1
+    assert lst.lst_recur_workspace((1 << 30) + 1, 1) == lst.lst_recur_workspace(1, 4097) == -1
+    assert lst.lst_recur_saved(1 << 30, 1) == 1 << 23
+    for rows, slots in (((1 << 16) + 1, P), (1 << 24, None)):
+        assert lib.lst_recur_step(0, rows, 1 << 25, 8, P, 8, P, 8, slots, P, P, 8, None,
+                                  None) == lst.LST_EINVAL
+
+
+@pytest.mark.gpu
+def test_widths_refused_with_save(gpu_lib):
+    for d in (0, 4097):
+        x = torch.zeros(4, d, device="cuda")
+        with pytest.raises(lst.LstError):
+            lst.lst_recur_forward(x, x, save=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradients_in_place(gpu_lib, dtype):
+    """grad_x and grad_g over the rows of x and g, y over those of x."""
+    torch.manual_seed(8)
+    rows, d = 700, 66
+    x, g, dy = (torch.randn(rows, d, device="cuda").to(dtype) for _ in range(3))
+    off = torch.tensor([0, 5, 300, 301, 700], dtype=torch.int32, device="cuda")
+    y, _, saved = lst.lst_recur_forward(x, g, off, save=True)
+    dx, dg, _ = lst.lst_recur_backward(x, g, dy, saved, off)
+    a, b = x.clone(), g.clone()
+    lst.lst_recur_backward(a, b, dy, saved, off, out=(a, b))
+    assert torch.equal(a, dx) and torch.equal(b, dg)
+    a = x.clone()
+    lst.lst_recur_forward(a, g, off, out=a)
+    assert torch.equal(a, y)

@@ -272,3 +272,21 @@ def test_refusals_on_host():
         assert call(**kw) == lst.LST_EINVAL, kw
     assert call(m=0, x=None) == lst.LST_OK
     assert lst.lst_sample_workspace(-1, 5) == -1 and lst.lst_sample_workspace(1, 0) == -1
+
+
+def test_sizes_behind_the_limits():
+    """Refused on the host: rows whose indexes with a block's step leave 32 bits."""
+    lib = lst.load_library()
+    P = 64  # never dereferenced
+    for D in ((1 << 30) + 1, 0x7FFFFFFF):
+        assert lib.lst_sample(0, 1, D, P, D, None, None, None, None, P, P, None, P,
+                              None) == lst.LST_EINVAL
+        assert lst.lst_sample_workspace(1, D) == -1
+    assert lst.lst_sample_workspace(1, 1 << 30) > 0
+
+
+@pytest.mark.gpu
+def test_many_short_rows(gpu_lib):
+    m, D = 3100, 9
+    x, u = _logits(m, D, torch.float32, 35)
+    _check(x, u, [MIX[i % len(MIX)] for i in range(m)])
