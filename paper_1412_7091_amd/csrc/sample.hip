@@ -21,9 +21,9 @@
 // of one bin is left to one block that goes over it digit by digit.
 //
 // Measured: one row of 200 000 floats with top-k 27 us, six launches that wait for each
-// other; 128 such rows with all kinds of settings 131 us (24 for the read of 102 MB), 64
-// rows of 793 471 bfloat16 with top-p alone 210 us (29 for the read).  The second and
-// third pass are bound by the weights' arithmetic (64 and 96 us), the rest by the latency
+// other; 128 such rows with all kinds of settings 112 us (22 for the read of 102 MB), 64
+// rows of 793 471 bfloat16 with top-p alone 181 us (27 for the read).  The second and
+// third pass are bound by the weights' arithmetic (56 and 76 us), the rest by the latency
 // of blocks that search.  One block a row alone took 438, 938 and 3500 us.
 #include <algorithm>
 
@@ -40,7 +40,9 @@ constexpr int kChunk = 64;     // entries whose largest key is kept
 constexpr int kStretch = 4096; // entries of one block of the first launch
 constexpr int kList = 4096;    // entries that one block lists, at most
 constexpr int kFine = 4096;    // bins of a row's values
-constexpr int kSegment = 32768; // entries of one block that sorts them into bins
+constexpr int kSegment = 16384; // entries of one block that sorts them into bins (128 rows of
+                                // 200 000: 11 us, with 32768 17; 64 of 793 471: 57 with either,
+                                // with 8192 89)
 constexpr int kLong = 8192;    // entries of a row's list in memory, at most
 constexpr int kShort = 8192;   // rows up to this length take one launch
 constexpr int kBatch = 1024;   // rows of one set of launches
@@ -68,8 +70,7 @@ struct SampleArgs {
   const int32_t* top_k;
   int32_t* tokens;
   float* prob;
-  int shift;    // weights are multiples of 2^-shift
-  double unit;  // 2^shift
+  double unit;  // 2^shift: weights are multiples of 2^-shift
   // the workspace, for rows longer than kShort: the largest key of each chunk; of each stretch
   // the smallest and the largest key and the sum of its weights, relative to the largest, then
   // the weight of its entries in the bins before the last and the number of those in it; per
@@ -117,47 +118,71 @@ __device__ inline float value_of(uint32_t k) {
 }
 
 // Weights w = exp((x - top) / t) = 2^(y / 64) with y = (x - top) 64 / (t ln 2): a table of the
-// 64 roots of two, and a polynomial of the rest, at most ln 2 / 128, to 4e-17.  Without a
-// branch: a weight costs about 25 instructions, and the long rows' passes are bound by them.
-struct Weights {
-  const double* roots;  // 2^(i / 64), in LDS
-  double c, unit;       // unit = 2^shift, at most 2^51
-  float top;
-  int shift;
+// 64 roots of two, and a polynomial of the rest, at most ln 2 / 128, to 4e-17.  The long rows'
+// passes are bound by this arithmetic (each operation in 64 bits is 2 us of 64 rows of 793 471
+// entries).
+struct Weight {
+  double power, rest;  // the weight 2^shift is their product
+  __device__ double value() const { return power * rest; }
+  // to the next integer, in one rounding: the lowest 52 bits of a sum with 2^52
+  __device__ uint64_t bits() const { return __double_as_longlong(fma(power, rest, 0x1p52)); }
+  __device__ uint64_t whole() const { return bits() & 0xFFFFFFFFFFFFFull; }
+};
 
-  // w 2^shift; 0 for -inf and what is no number
-  __device__ double scaled(float x) const {
-    const double y = ((double)x - (double)top) * c, n = rint(y), r = y - n;
+struct Weights {
+  const double* roots;  // 2^(shift + i / 64), in LDS, less i 2^14 in the upper word
+  double c, unit;       // unit = 2^shift, at most 2^51
+  double floor;         // x - top at which w = 2^-200
+  float top;
+
+  // 2^(shift + i / 64): one sum of the upper word and i 2^14
+  __device__ double power(int i) const {
+    const double d = roots[i & 63];
+    return __hiloint2double(__double2hiint(d) + (i << 14), __double2loint(d));
+  }
+  __device__ static double rest(double r) {
     double q = fma(r, 1.2417843701716923e-12, 5.732851688640402e-10);  // (ln 2 / 64)^k / k!
     q = fma(r, q, 2.1173137155464774e-07);
     q = fma(r, q, 5.864904955056169e-05);
     q = fma(r, q, 0.010830424696249145);
-    q = fma(r, q, 1.0);
+    return fma(r, q, 1.0);
+  }
+  // w 2^shift where w is at least 2^-200 and the top is finite; 2^-200 2^shift, less than any
+  // sum of weights can tell, for all that is less, -inf and what is no number.  The integer of
+  // y is in the lowest bits of its sum with 1.5 2^52 (rint, the conversion and ldexp are slower).
+  __device__ Weight near(float x) const {
+    const double dx = fmax((double)x - (double)top, floor), t = fma(dx, c, 0x1.8p52);
+    return {power(__double2loint(t)), rest(fma(dx, c, 0x1.8p52 - t))};
+  }
+  __device__ Weight weight(float x) const { return x == top ? Weight{unit, 1.0} : near(x); }
+  // the same however small it is
+  __device__ double scaled(float x) const {
+    const double y = ((double)x - (double)top) * c, n = rint(y);
+    if (x == top || y > -64.0 * 199) return weight(x).value();
     const int i = (int)n;
-    const double d = __builtin_ldexp(roots[i & 63] * q, (i >> 6) + shift);
-    return x == top ? unit : y > -64.0 * 1075 ? d : 0.0;  // (both may be infinite)
+    return y > -64.0 * 1200 ? __builtin_ldexp(power(i & 63) * rest(y - n), i >> 6) : 0.0;
   }
-  // to the next integer: the lowest bits of a sum with 2^52
-  static __device__ uint64_t rounded(double d) {
-    return (uint64_t)__double_as_longlong(d + 0x1p52) & 0xFFFFFFFFFFFFFull;
-  }
-  __device__ uint64_t whole(uint32_t key) const { return rounded(scaled(value_of(key))); }
+  __device__ uint64_t whole(uint32_t key) const { return weight(value_of(key)).whole(); }
   __device__ double of(uint32_t key) const { return scaled(value_of(key)) / unit; }
 };
 
 __device__ inline Weights weights_of(const SampleArgs& a, const double* roots, uint32_t top,
                                      float t) {
-  // 64 / ln 2
-  return {roots, 92.332482616893656 / (double)t, a.unit, value_of(top), a.shift};
+  const double c = 92.332482616893656 / (double)t;  // 64 / ln 2
+  return {roots, c, a.unit, -64.0 * 200 / c, value_of(top)};
 }
 
-__device__ inline void fill_roots(double* roots) {
-  if (threadIdx.x < 64) roots[threadIdx.x] = exp2(threadIdx.x / 64.0);
+__device__ inline void fill_roots(double* roots, double unit) {
+  const int i = threadIdx.x;
+  if (i >= 64) return;
+  const double d = exp2(i / 64.0) * unit;
+  roots[i] = __hiloint2double(__double2hiint(d) - (i << 14), __double2loint(d));
 }
 
-// The bins go down from the largest value; the last one holds all that is far below.
-__device__ inline int bin_of(const RowPlan& p, float x) {
-  return min((int)((p.top_value - x) * p.scale), kFine - 1);
+// The bins go down from the largest value; the last one holds all that is far below.  An
+// entry's bin is the whole part of this.
+__device__ inline float bin_value(const RowPlan& p, float x) {
+  return fminf((p.top_value - x) * p.scale, kFine - 0.5f);
 }
 
 struct Shared {
@@ -474,51 +499,67 @@ __device__ inline bool wants_sum(const Wish& w, int D) {
   return w.good && w.t > 0.f && !k && (w.p < 1.f) == (w.q > 0.f);
 }
 
+// A thread's entries of a stretch, which 256 of them have: kWide neighbours at a time.  -inf
+// behind the row's end.
+constexpr int kWide = 8, kSteps = kStretch / (256 * kWide);
+template <class T>
+__device__ inline void load_stretch(const T* x, int64_t base, int D, float (&v)[kSteps][kWide]) {
+  T r[kSteps][kWide];
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const int64_t i = base + s * 256 * kWide;
+    if (i + kWide <= D) {
+      load_vec(x + i, r[s]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kWide; ++j) r[s][j] = i + j < D ? x[i + j] : (T)-INFINITY;
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+    for (int j = 0; j < kWide; ++j) v[s][j] = (float)r[s][j];
+}
+
 // The largest key of every chunk, and the smallest key and the sum of every stretch: one read
-// of the row.  A block has one stretch, 16 lanes a chunk at a time.
+// of the row.  A block has one stretch, eight lanes a chunk at a time.
 template <class T>
 __global__ __launch_bounds__(256) void sample_stats_kernel(SampleArgs a, const T* logits) {
   __shared__ double roots[64];
-  __shared__ uint32_t wave_max[4], wave_min[4];
+  __shared__ float wave_max[4], wave_min[4];
   __shared__ double wave_sum[4];
   const int row = blockIdx.y, stretch = blockIdx.x, tid = threadIdx.x;
   const T* x = logits + row * a.ldx;
-  const int64_t base = (int64_t)stretch * kStretch + 4 * tid;
-  constexpr int kSteps = kStretch / 1024;
-  fill_roots(roots);
-  uint32_t key[kSteps][4], top = 0, low = 0xFFFFFFFFu;
+  const int64_t base = (int64_t)stretch * kStretch + kWide * tid;
+  float v[kSteps][kWide];
+  load_stretch(x, base, a.D, v);
+  fill_roots(roots, a.unit);
+  float high = -INFINITY, low = INFINITY;  // of those that may be chosen
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
-    const int64_t i = base + s * 1024;
-    T v[4];
-    if (i + 4 <= a.D) {
-      load_vec(x + i, v);
-    } else {
+    float h = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = i + j < a.D ? x[i + j] : (T)-INFINITY;
+    for (int j = 0; j < kWide; ++j) {
+      h = v[s][j] > h ? v[s][j] : h;
+      low = v[s][j] < low && v[s][j] > -INFINITY ? v[s][j] : low;
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) key[s][j] = key_of((float)v[j]);
+    for (int o = kChunk / kWide / 2; o; o >>= 1) h = fmaxf(h, __shfl_xor(h, o));
+    const int64_t chunk = (base + s * 256 * kWide) / kChunk;
+    if (tid % (kChunk / kWide) == 0 && chunk < a.chunks)
+      a.chunk_max[(int64_t)row * a.chunks + chunk] = key_of(h);
+    high = fmaxf(high, h);
   }
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
-    uint32_t k = max(max(key[s][0], key[s][1]), max(key[s][2], key[s][3]));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) low = min(low, key[s][j] - 1);  // 0, none, becomes the largest
-#pragma unroll
-    for (int o = kChunk / 8; o; o >>= 1) k = max(k, (uint32_t)__shfl_xor((int)k, o));
-    const int64_t chunk = (base + s * 1024) / kChunk;
-    if (tid % (kChunk / 4) == 0 && chunk < a.chunks) a.chunk_max[(int64_t)row * a.chunks + chunk] = k;
-    top = max(top, k);
-  }
-  for (int o = 32; o >= kChunk / 4; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-  for (int o = 32; o; o >>= 1) low = min(low, (uint32_t)__shfl_xor((int)low, o));
-  if (tid % 64 == 0) wave_max[tid / 64] = top, wave_min[tid / 64] = low;
+  for (int o = 32; o >= kChunk / kWide; o >>= 1) high = fmaxf(high, __shfl_xor(high, o));
+  for (int o = 32; o; o >>= 1) low = fminf(low, __shfl_xor(low, o));
+  if (tid % 64 == 0) wave_max[tid / 64] = high, wave_min[tid / 64] = low;
   __syncthreads();
-  top = max(max(wave_max[0], wave_max[1]), max(wave_max[2], wave_max[3]));
+  high = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
+  const uint32_t top = key_of(high);
   const int64_t at = (int64_t)row * a.stretches + stretch;
   if (tid == 0) {
-    a.stretch_min[at] = min(min(wave_min[0], wave_min[1]), min(wave_min[2], wave_min[3])) + 1;
+    low = fminf(fminf(wave_min[0], wave_min[1]), fminf(wave_min[2], wave_min[3]));
+    a.stretch_min[at] = top ? key_of(low) : 0;
     a.stretch_max[at] = top;
   }
   const Wish w = wish_of(a, row);
@@ -528,7 +569,10 @@ __global__ __launch_bounds__(256) void sample_stats_kernel(SampleArgs a, const T
 #pragma unroll
   for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sum += of.scaled(value_of(key[s][j]));
+    for (int j = 0; j < kWide; ++j) {
+      sum += of.weight(v[s][j]).value();
+      if (j % 2) asm volatile("" : "+v"(sum));  // 16 weights at once: 82 registers, 34 us for 27
+    }
   sum /= a.unit;
   if (top == 0) sum = 0.0;
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
@@ -599,7 +643,7 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
   const Wish w = wish_of(a, row);
   RowPlan& plan = a.plan[row];
   if (tid == 0) plan.state = ROW_OPEN, ps.count = ps.n_hits = 0;
-  fill_roots(sh.roots);
+  fill_roots(sh.roots, a.unit);
   uint32_t top = 0, low = 0xFFFFFFFFu;
   for (int i = tid; i < n; i += kThreads) {
     const uint32_t k = cmax[i];
@@ -760,31 +804,38 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a, con
   const Wish w = wish_of(a, row);
   if (state == ROW_MASS && w.p >= 1.f) return;
   const T* x = logits + row * a.ldx;
-  fill_roots(roots);
+  fill_roots(roots, a.unit);
   for (int i = tid; i < kFine; i += kThreads) bins[i] = 0;
   __syncthreads();
   const Weights of = weights_of(a, roots, p.top, w.t);
   const int64_t base = (int64_t)blockIdx.x * kSegment + 4 * tid;
+  T next[4];
+  auto fetch = [&](int64_t i) {
+    if (i + 4 <= a.D) {
+      load_vec(x + i, next);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) next[j] = i + j < a.D ? x[i + j] : (T)-INFINITY;
+    }
+  };
+  fetch(base);
   for (int s = 0; s < kSegment; s += 4 * kThreads) {
     const int64_t i = base + s;
     if (i >= a.D) break;
     T v[4];
-    if (i + 4 <= a.D) {
-      load_vec(x + i, v);
-    } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = i + j < a.D ? x[i + j] : (T)-INFINITY;
-    }
+    for (int j = 0; j < 4; ++j) v[j] = next[j];
+    if (s + 4 * kThreads < kSegment) fetch(i + 4 * kThreads);
     // what is not to be chosen adds nothing, to whichever bin
     if (state == ROW_MASS) {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        atomicAdd((unsigned long long*)&bins[bin_of(p, (float)v[j])],
-                  (unsigned long long)Weights::rounded(of.scaled((float)v[j])));
+        atomicAdd((unsigned long long*)&bins[(int)bin_value(p, (float)v[j])],
+                  (unsigned long long)of.near((float)v[j]).whole());
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        atomicAdd((unsigned long long*)&bins[bin_of(p, (float)v[j])],
+        atomicAdd((unsigned long long*)&bins[(int)bin_value(p, (float)v[j])],
                   (unsigned long long)((float)v[j] > -INFINITY));
     }
   }
@@ -794,41 +845,43 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a, con
     if (bins[i]) atomicAdd(&sums[i], (unsigned long long)bins[i]);
 }
 
-// The bin of the border, from a row's bins.
+// The bin of the border, from a row's bins: four of them a thread.
 __global__ __launch_bounds__(kThreads) void sample_border_kernel(SampleArgs a) {
-  __shared__ Shared sh;
-  const int row = blockIdx.x, tid = threadIdx.x;
+  static_assert(kFine == 4 * kThreads, "");
+  __shared__ uint64_t wave[kWaves];
+  const int row = blockIdx.x, tid = threadIdx.x, l = tid % 64, w = tid / 64;
   RowPlan& plan = a.plan[row];
   const int state = plan.state;
   if (state != ROW_MASS && state != ROW_COUNT) return;
-  const Wish w = wish_of(a, row);
-  if (state == ROW_MASS && w.p >= 1.f) return;
-  const uint64_t* bins = a.bins + (int64_t)row * kFine;
-  // one half of them after the other
-  uint64_t half[2], all = 0;
-  for (int h = 0; h < 2; ++h) {
-    clear_bins(sh);
-    for (int i = tid; i < kBins; i += kThreads) sh.bin[i] = bins[h * kBins + i];
-    half[h] = sum_bins(sh);
-    all += half[h];
+  const Wish wish = wish_of(a, row);
+  if (state == ROW_MASS && wish.p >= 1.f) return;
+  uint64_t v[4], upto = 0;
+  load_vec(a.bins + (int64_t)row * kFine + 4 * tid, v);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) upto += v[j];
+  const uint64_t own = upto;
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint64_t up = __shfl_up(upto, o);
+    if (l >= o) upto += up;
   }
-  uint64_t target = w.k;
-  bool fits = state == ROW_COUNT ? all > target : true;
+  if (l == 63) wave[w] = upto;
+  __syncthreads();
+  uint64_t all = 0;
+  for (int i = 0; i < kWaves; ++i) {
+    if (i == w) upto += all;
+    all += wave[i];
+  }
+  uint64_t target = min((uint64_t)max(wish.k, 1), all);  // fewer entries than top-k: all of them
   if (state == ROW_MASS) {
-    const double want = ceil((double)w.p * (double)all);
+    const double want = ceil((double)wish.p * (double)all);
     target = want > 1.0 ? (uint64_t)want : 1;
-  } else if (!fits) {
-    target = all;  // fewer entries than top-k: all of them
   }
-  const int h = target > half[0];
-  if (h) target -= half[0];
-  clear_bins(sh);
-  for (int i = tid; i < kBins; i += kThreads) sh.bin[i] = bins[h * kBins + i];
-  find_bin(sh, target);
-  if (tid == 0) {
-    plan.bin = h * kBins + sh.found;
-    plan.left = target - sh.above;
-  }
+  uint64_t before = upto - own;
+  if (before >= target || upto < target) return;
+  int bin = 0;
+  while (bin < 3 && before + v[bin] < target) before += v[bin++];
+  plan.bin = 4 * tid + bin;
+  plan.left = target - before;
 }
 
 // The entries of the border's bin into the row's list (ROW_COUNT: of the bins before it too),
@@ -847,50 +900,49 @@ __global__ __launch_bounds__(256) void sample_list_kernel(SampleArgs a, const T*
   const RowPlan p = plan;
   const Wish w = wish_of(a, row);
   const T* x = logits + row * a.ldx;
-  const int64_t base = (int64_t)stretch * kStretch + 4 * tid;
-  constexpr int kSteps = kStretch / 1024;
-  fill_roots(roots);
+  const int64_t base = (int64_t)stretch * kStretch + kWide * tid;
+  float v[kSteps][kWide];
+  load_stretch(x, base, a.D, v);
+  fill_roots(roots, a.unit);
   __syncthreads();
   const Weights of = weights_of(a, roots, p.top, w.t);
-  const double q = (double)w.q * a.unit;
-  float v[kSteps][4];
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
-    const int64_t i = base + s * 1024;
-    T r[4];
-    if (i + 4 <= a.D) {
-      load_vec(x + i, r);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) r[j] = i + j < a.D ? x[i + j] : (T)-INFINITY;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[s][j] = (float)r[j];
-  }
+  const double q = fmin((double)w.q, 1.0) * a.unit;  // (the largest are kept in any case)
+  const float below = p.bin, from = state == ROW_COUNT ? -1.f : below, upto_bin = below + 1.f;
   uint64_t mass = 0;
   uint32_t listed = 0, least = 0xFFFFFFFFu, most = 0;  // listed: a bit an entry
-#pragma unroll
-  for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float f = v[s][j];
-      const int b = f > -INFINITY ? bin_of(p, f) : kFine + 1;
-      if (b == p.bin || (state == ROW_COUNT && b < p.bin)) {
-        listed |= 1u << (4 * s + j);
-        least = min(least, key_of(f));
-        most = max(most, key_of(f));
-      }
+  auto mark = [&](int i, float f, float b) {
+    if (b >= from && b < upto_bin && f > -INFINITY) {
+      listed |= 1u << i;
+      least = min(least, key_of(f));
+      most = max(most, key_of(f));
     }
-  if (state == ROW_MASS) {
+  };
+  auto weigh = [&](auto limited) {
 #pragma unroll
     for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float f = v[s][j];
-        const double d = of.scaled(f);
-        const bool before = f > -INFINITY && bin_of(p, f) < p.bin;
-        mass += before && (d >= q || f == of.top) ? Weights::rounded(d) : 0;
+      for (int j = 0; j < kWide; ++j) {
+        // (-inf and what is no number has no weight, and counts for nothing)
+        const float f = v[s][j], b = bin_value(p, f);
+        Weight d = of.near(f);
+        const bool kept = b < below && (!limited.value || d.value() >= q);
+        // (without the upper word: less than any sum can tell)
+        d.power = __hiloint2double(kept ? __double2hiint(d.power) : 0, __double2loint(d.power));
+        mass += d.bits();
+        // (here, not behind all of the marks: that takes 142 registers and 109 us for 77)
+        if (j % 2) asm volatile("" : "+v"(mass));
+        mark(kWide * s + j, f, b);
       }
+    // what each sum with 2^52 holds beside the integer (all of it modulo 2^64)
+    mass -= kSteps * kWide * Weight{0.0, 0.0}.bits();
+  };
+  if (state == ROW_MASS) {
+    w.q > 0.f ? weigh(std::true_type{}) : weigh(std::false_type{});
+  } else {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int j = 0; j < kWide; ++j) mark(kWide * s + j, v[s][j], bin_value(p, v[s][j]));
   }
   const int own = __popc(listed);
   int upto = own;  // of the wave's lanes up to this one
@@ -926,11 +978,11 @@ __global__ __launch_bounds__(256) void sample_list_kernel(SampleArgs a, const T*
 #pragma unroll
   for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (listed >> (4 * s + j) & 1) {
+    for (int j = 0; j < kWide; ++j)
+      if (listed >> (kWide * s + j) & 1) {
         if (at < kLong) {
           a.list_keys[(int64_t)row * kLong + at] = key_of(v[s][j]);
-          a.list_indexes[(int64_t)row * kLong + at] = (int)(base + s * 1024 + j);
+          a.list_indexes[(int64_t)row * kLong + at] = (int)(base + s * 256 * kWide + j);
         }
         ++at;
       }
@@ -1012,7 +1064,7 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, cons
   __shared__ Shared sh;
   const int row = blockIdx.x, tid = threadIdx.x, D = a.D;
   if (a.plan && a.plan[row].state == ROW_DONE) return;
-  fill_roots(sh.roots);
+  fill_roots(sh.roots, a.unit);
   const RowEntries<T> src{logits + row * a.ldx, D};
   const Wish w = wish_of(a, row);
   if (a.plan && a.plan[row].state != ROW_OPEN) {
@@ -1118,8 +1170,7 @@ int lst_sample(int32_t dtype, int32_t m, int32_t D, const void* logits, int64_t 
       if (top_p) a.top_p = top_p + r;
       if (min_p) a.min_p = min_p + r;
       if (prob) a.prob = prob + r;
-      a.shift = std::min(51, 62 - log);
-      a.unit = (double)((int64_t)1 << a.shift);
+      a.unit = (double)((int64_t)1 << std::min(51, 62 - log));
       const T* x = (const T*)logits + r * ldx;
       if (D > kShort) {
         hipLaunchKernelGGL(sample_stats_kernel<T>, dim3(a.stretches, n), dim3(256), 0, s, a, x);
