@@ -304,7 +304,8 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(const uint8_t* W, const 
       store_tile(O, ldo, m, D, (t0 + n) * 16 + i16, r0 + 16 * t + 4 * q4, acc[t][n]);
 }
 
-constexpr int kFew = 16;          // rows of H that one launch takes
+constexpr int kFew = 16;          // rows of H that one launch takes: 23 us (16 by 200 000 x
+                                  // 512 codes), by fragments and tiles 33
 constexpr int kFewColumns = 2048;  // that fit 64 KB of LDS in bfloat16
 constexpr int kFewBlocks = 512;   // blocks of that launch, two a compute unit
 constexpr int64_t kMostBlocks = (1 << 28) - 16;  // of a matrix: 2^32 threads
@@ -363,7 +364,8 @@ int lst_scores(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int32_t d
         return launched();
       });
     });
-  // 256 rows of W and up to 8 tiles of H a block
+  // 256 rows of W and up to 8 tiles of H a block; no more than there are: 32 rows of H by
+  // 200 000 x 512 codes take 37 us with 2 tiles and 47 with 8, 64 take 44 with 4 and 52 with 8
   const int nt = tiles <= 2 ? 2 : tiles <= 4 ? 4 : 8;
   const int64_t row_blocks = (D + 255) / 256;
   const int64_t grid = (row_blocks + 7) / 8 * 8 * ((tiles + nt - 1) / nt);

@@ -18,7 +18,8 @@
 // the row's weights go into 4096 bins by value (a second read), and the bin that top-p's
 // border falls into is listed while the weights before it are added up by stretches of
 // 4096 entries (a third).  A row whose border lies among more than 8192 unequal entries
-// of one bin is left to one block that goes over it digit by digit.
+// of one bin, or that keeps more than 8192 by top-k, is left to one block that goes over it
+// digit by digit (128 rows of 200 000 with top-k 20 000 take 774 us, with 3000 167).
 //
 // Measured: one row of 200 000 floats with top-k 27 us, six launches that wait for each
 // other; 128 such rows with all kinds of settings 112 us (22 for the read of 102 MB), 64
@@ -44,7 +45,10 @@ constexpr int kSegment = 16384; // entries of one block that sorts them into bin
                                 // 200 000: 11 us, with 32768 17; 64 of 793 471: 57 with either,
                                 // with 8192 89)
 constexpr int kLong = 8192;    // entries of a row's list in memory, at most
-constexpr int kShort = 8192;   // rows up to this length take one launch
+// Rows up to this length take one launch.  128 rows with top-k 50 and top-p, top-p alone, and
+// neither: 35, 27 and 15 us in one launch and 25, 43 and 24 in six at 4096 entries, 43, 38 and
+// 19 against 25, 45 and 25 at 8000, 58, 58 and 29 against 26, 45 and 26 at 16 000.
+constexpr int kShort = 8192;
 constexpr int kBatch = 1024;   // rows of one set of launches
 constexpr int kMostRows = 1 << 20;     // of short rows' one launch
 constexpr int kMostEntries = 1 << 30;  // of a row: an index and a block's step stay below 2^31
