@@ -106,6 +106,9 @@ __device__ inline Wish wish_of(const SampleArgs& a, int row) {
   w.q = a.min_p ? a.min_p[row] : 0.f;
   w.u = a.u[row];
   w.good = w.t >= 0.f && isfinite(w.t) && !isnan(w.p) && !isnan(w.q) && w.u >= 0.f && w.u < 1.f;
+  // no weight is more than 1: the first of the largest entries is left, as with top-k 1, and
+  // further on min-p keeps every entry that is as large as the largest
+  if (w.q > 1.f) w.k = 1, w.q = 0.f;
   return w;
 }
 
@@ -910,7 +913,7 @@ __global__ __launch_bounds__(256) void sample_list_kernel(SampleArgs a, const T*
   fill_roots(roots, a.unit);
   __syncthreads();
   const Weights of = weights_of(a, roots, p.top, w.t);
-  const double q = fmin((double)w.q, 1.0) * a.unit;  // (the largest are kept in any case)
+  const double q = (double)w.q * a.unit;
   const float below = p.bin, from = state == ROW_COUNT ? -1.f : below, upto_bin = below + 1.f;
   uint64_t mass = 0;
   uint32_t listed = 0, least = 0xFFFFFFFFu, most = 0;  // listed: a bit an entry

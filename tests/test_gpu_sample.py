@@ -290,3 +290,23 @@ def test_many_short_rows(gpu_lib):
     m, D = 3100, 9
     x, u = _logits(m, D, torch.float32, 35)
     _check(x, u, [MIX[i % len(MIX)] for i in range(m)])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [2, 100, 3000, 5000, 9000, 150_000])
+def test_min_p_above_one(gpu_lib, dtype, D):
+    """No weight reaches it: the first of the largest entries alone, however many are equal."""
+    inf = float("inf")
+    up = float(np.nextafter(np.float32(1), np.float32(2)))
+    sets = [dict(min_p=q, **s) for q in (up, 1.5, inf)
+            for s in (dict(), dict(top_k=2), dict(top_p=0.9), dict(top_k=7000, top_p=0.999),
+                      dict(temperature=30.0), dict(temperature=0.0))]
+    equal = torch.zeros((len(sets), D), device="cuda")
+    two = (torch.arange(D, device="cuda") % 2 == 1).float().repeat(len(sets), 1)
+    stairs = -(torch.arange(D, device="cuda") % 7 - 3).abs().float().repeat(len(sets), 1)
+    infinite = torch.where(two > 0, inf, 0.0)
+    for x, first in ((equal, 0), (two, 1), (stairs, min(3, D - 1)), (infinite, 1)):
+        for u in (0.0, 0.9):
+            tokens = _check(x.to(dtype), [float(np.float32(u))] * len(sets), sets)
+            assert (tokens == first).all()
