@@ -530,9 +530,11 @@ int64_t lst_scores_workspace(int32_t m, int32_t d); /* bytes; -1 for a bad size 
  *   3. min_p > 0 keeps those with w_i >= min_p, at least the first;
  *   4. the token is the first, by index, at which the sum of the kept weights exceeds
  *      u times their total.
- * temperature 0 takes the first entry of the order.  Weights have 64 bits.  A row
- * without an entry to choose from, with a negative or infinite temperature, u outside
- * [0, 1) or a parameter that is no number gets the token -1 and the probability 0.
+ * temperature 0 takes the first entry of the order.  Weights are computed in 64 bits and
+ * summed in integers of 64 bits, so that the choice does not depend on timing; a sum is off
+ * by at most 2^-27 of the row's total (2^-52 D where D is above 2^25).  A row without an
+ * entry to choose from, with a negative or infinite temperature, u outside [0, 1) or a
+ * parameter that is no number gets the token -1 and the probability 0.
  */
 int lst_sample(int32_t dtype, int32_t m, int32_t D, const void* logits, int64_t ldx,
                const float* temperature, const int32_t* top_k, const float* top_p,

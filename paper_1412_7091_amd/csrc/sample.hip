@@ -9,8 +9,10 @@
 // the kept weights up to i exceeds u times the sum of all of them.
 //
 // Weights are computed in float64 and added as integers, multiples of 2^-shift with
-// the shift as large as D sums of at most 1 allow (51 at most): sums of integers do
+// the shift as large as their sum allows in 64 bits (51 at most): sums of integers do
 // not depend on the order in which the atomics arrive, so the choice does not either.
+// A sum is off by at most 2^-52 D of the row's total (2^-27 where D says what the sum is
+// at most, kFixedUnit): by half a step for each of D weights, of which one is 1.
 //
 // Rows of up to 8192 entries take one block each.  Longer ones are read by many blocks,
 // once for the largest key of every 64 entries.  From those a bound follows that few
@@ -50,6 +52,9 @@ constexpr int kLong = 8192;    // entries of a row's list in memory, at most
 // 19 against 25, 45 and 25 at 8000, 58, 58 and 29 against 26, 45 and 26 at 16 000.
 constexpr int kShort = 8192;
 constexpr int kBatch = 1024;   // rows of one set of launches
+// Rows up to this length have the step that D weights of 1 leave, which is 2^-27 of the total
+// for all D weights together; longer ones each have their own.
+constexpr int kFixedUnit = 1 << 18;
 constexpr int kMostRows = 1 << 20;     // of short rows' one launch
 constexpr int kMostEntries = 1 << 30;  // of a row: an index and a block's step stay below 2^31
 
@@ -61,8 +66,9 @@ struct RowPlan {
   float top_value, scale;  // bin = (top_value - x) scale
   int bin;          // the one that holds the last entry kept
   uint64_t left;    // ROW_MASS: what the bin's entries have to give
+  double unit;      // 2^shift of the row's weights
   // on a line of its own, since blocks add to it while others read what is above
-  int apart[24];
+  int apart[22];
   unsigned listed;  // entries of the bin (ROW_COUNT: of all up to it)
   int behind[31];
 };
@@ -74,7 +80,7 @@ struct SampleArgs {
   const int32_t* top_k;
   int32_t* tokens;
   float* prob;
-  double unit;  // 2^shift: weights are multiples of 2^-shift
+  double unit;  // 2^shift where D alone says what the weights' sum is at most
   // the workspace, for rows longer than kShort: the largest key of each chunk; of each stretch
   // the smallest and the largest key and the sum of its weights, relative to the largest, then
   // the weight of its entries in the bins before the last and the number of those in it; per
@@ -173,10 +179,10 @@ struct Weights {
   __device__ double of(uint32_t key) const { return scaled(value_of(key)) / unit; }
 };
 
-__device__ inline Weights weights_of(const SampleArgs& a, const double* roots, uint32_t top,
-                                     float t) {
+// roots: filled for the unit.
+__device__ inline Weights weights_of(const double* roots, double unit, uint32_t top, float t) {
   const double c = 92.332482616893656 / (double)t;  // 64 / ln 2
-  return {roots, c, a.unit, -64.0 * 200 / c, value_of(top)};
+  return {roots, c, unit, -64.0 * 200 / c, value_of(top)};
 }
 
 __device__ inline void fill_roots(double* roots, double unit) {
@@ -490,7 +496,7 @@ __device__ void choose(Shared& sh, const SampleArgs& a, int row, const Wish& w, 
   for (int p = src.from(at) + threadIdx.x; p < src.to(at + 1); p += kThreads)
     if (src.index(p) == at) {
       a.tokens[row] = at;
-      if (a.prob) a.prob[row] = (float)(of.of(src.key(p)) / ((double)all / a.unit));
+      if (a.prob) a.prob[row] = (float)(of.of(src.key(p)) / ((double)all / of.unit));
     }
 }
 
@@ -571,7 +577,7 @@ __global__ __launch_bounds__(256) void sample_stats_kernel(SampleArgs a, const T
   }
   const Wish w = wish_of(a, row);
   if (!wants_sum(w, a.D)) return;
-  const Weights of = weights_of(a, roots, top, w.t);
+  const Weights of = weights_of(roots, a.unit, top, w.t);  // no weight is rounded here
   double sum = 0.0;
 #pragma unroll
   for (int s = 0; s < kSteps; ++s)
@@ -627,7 +633,31 @@ __device__ void choose_few(Shared& sh, const SampleArgs& a, int row, const Wish&
   for (int o = 1; o < 4; o <<= 1) upto += __shfl_xor(upto, o), all += __shfl_xor(all, o);
   const uint64_t target = (uint64_t)((double)w.u * (double)all) + 1;
   if (i < n && part == 0 && upto >= target && upto - kept[i] < target)
-    give(a, row, list.indexes[i], (float)(of.of(list.keys[i]) / ((double)all / a.unit)));
+    give(a, row, list.indexes[i], (float)(of.of(list.keys[i]) / ((double)all / of.unit)));
+}
+
+// 2^shift for a row of more than kFixedUnit entries: its weights' sum is at most 64 times that
+// of the chunks' largest ones, and that times 2^shift stays below 2^62 (the float32 sum is near
+// enough: 2^64 is where the integers end).  3 us of 64 rows of 793 471 entries.
+__device__ double unit_of(Shared& sh, const SampleArgs& a, const uint32_t* cmax, uint32_t top,
+                          float t) {
+  // halves: the difference of two finite values may have no float
+  const float high = 0.5f * value_of(top), c = 2.88539008f / t;
+  float sum = 0.f;
+  for (int i = threadIdx.x; i < a.chunks; i += kThreads) {
+    const uint32_t k = cmax[i];
+    sum += k == top ? 1.f : k ? __builtin_amdgcn_exp2f((0.5f * value_of(k) - high) * c) : 0.f;
+  }
+  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  if (threadIdx.x % 64 == 0) sh.key[threadIdx.x / 64] = __float_as_uint(sum);
+  __syncthreads();
+  float all = 0.f;
+  for (int i = 0; i < kWaves; ++i) all += __uint_as_float(sh.key[i]);
+  __syncthreads();
+  // kChunk all is less than 2^(the biased exponent of all - 126) kChunk
+  const int log = (int)(__float_as_uint(all) >> 23) - 126 + 6;
+  static_assert(kChunk == 1 << 6, "");
+  return fmax(a.unit, __hiloint2double((1023 + min(51, 62 - log)) << 20, 0));
 }
 
 struct PlanShared {
@@ -663,14 +693,21 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
     return;
   }
   const bool k_on = w.k > 0 && w.k < D;
-  const Weights of = weights_of(a, sh.roots, top, w.t);
+  double unit = a.unit;
+  if (D > kFixedUnit && w.t > 0.f) {
+    unit = unit_of(sh, a, cmax, top, w.t);
+    if (tid < 64) sh.roots[tid] *= unit / a.unit;
+    __syncthreads();
+  }
+  if (tid == 0) plan.unit = unit;
+  const Weights of = weights_of(sh.roots, unit, top, w.t);
   uint64_t total = 0;
   if (wants_sum(w, D) && w.u > 0.f && a.stretches <= kBins) {
     clear_bins(sh);
     for (int i = tid; i < a.stretches; i += kThreads) {
       const uint32_t k = a.stretch_max[(int64_t)row * a.stretches + i];
       const double sum = a.stretch_sum[(int64_t)row * a.stretches + i] * of.of(k);
-      sh.bin[i] = k ? (uint64_t)(sum * a.unit + 0.5) : 0;
+      sh.bin[i] = k ? (uint64_t)(sum * unit + 0.5) : 0;
     }
     total = sum_bins(sh);
     if (w.q <= 0.f) {
@@ -690,7 +727,7 @@ __global__ __launch_bounds__(kThreads) void sample_plan_kernel(SampleArgs a, con
           find_bin(sh, left);
           if (tid == 0) {
             const int i = (int)(first + half * kBins) + sh.found;
-            give(a, row, i, (float)(of.of(key_of((float)x[i])) / ((double)total / a.unit)));
+            give(a, row, i, (float)(of.of(key_of((float)x[i])) / ((double)total / unit)));
             plan.state = ROW_DONE;
           }
           return;
@@ -811,10 +848,10 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a, con
   const Wish w = wish_of(a, row);
   if (state == ROW_MASS && w.p >= 1.f) return;
   const T* x = logits + row * a.ldx;
-  fill_roots(roots, a.unit);
+  fill_roots(roots, p.unit);
   for (int i = tid; i < kFine; i += kThreads) bins[i] = 0;
   __syncthreads();
-  const Weights of = weights_of(a, roots, p.top, w.t);
+  const Weights of = weights_of(roots, p.unit, p.top, w.t);
   const int64_t base = (int64_t)blockIdx.x * kSegment + 4 * tid;
   T next[4];
   auto fetch = [&](int64_t i) {
@@ -910,10 +947,10 @@ __global__ __launch_bounds__(256) void sample_list_kernel(SampleArgs a, const T*
   const int64_t base = (int64_t)stretch * kStretch + kWide * tid;
   float v[kSteps][kWide];
   load_stretch(x, base, a.D, v);
-  fill_roots(roots, a.unit);
+  fill_roots(roots, p.unit);
   __syncthreads();
-  const Weights of = weights_of(a, roots, p.top, w.t);
-  const double q = (double)w.q * a.unit;
+  const Weights of = weights_of(roots, p.unit, p.top, w.t);
+  const double q = (double)w.q * p.unit;
   const float below = p.bin, from = state == ROW_COUNT ? -1.f : below, upto_bin = below + 1.f;
   uint64_t mass = 0;
   uint32_t listed = 0, least = 0xFFFFFFFFu, most = 0;  // listed: a bit an entry
@@ -1002,7 +1039,7 @@ __device__ bool finish_bins(Shared& sh, const SampleArgs& a, int row, const Wish
                             const T* x) {
   const int tid = threadIdx.x, D = a.D;
   const RowPlan p = a.plan[row];
-  const Weights of = weights_of(a, sh.roots, p.top, w.t);
+  const Weights of = weights_of(sh.roots, p.unit, p.top, w.t);
   const ListEntries list{a.list_keys + (int64_t)row * kLong, a.list_indexes + (int64_t)row * kLong,
                          (int)p.listed};
   if (p.state == ROW_COUNT) {
@@ -1061,7 +1098,7 @@ __device__ bool finish_bins(Shared& sh, const SampleArgs& a, int row, const Wish
   const Border here{b.key, (int)(b.last - first < -1 ? -1 : b.last - first)};
   const int at = index_at(sh, part, part.n, here, left, kept);
   if (tid == 0)
-    give(a, row, (int)first + at, (float)(of.of(part.key(at)) / ((double)all / a.unit)));
+    give(a, row, (int)first + at, (float)(of.of(part.key(at)) / ((double)all / p.unit)));
   return true;
 }
 
@@ -1071,7 +1108,8 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, cons
   __shared__ Shared sh;
   const int row = blockIdx.x, tid = threadIdx.x, D = a.D;
   if (a.plan && a.plan[row].state == ROW_DONE) return;
-  fill_roots(sh.roots, a.unit);
+  const double unit = a.plan ? a.plan[row].unit : a.unit;
+  fill_roots(sh.roots, unit);
   const RowEntries<T> src{logits + row * a.ldx, D};
   const Wish w = wish_of(a, row);
   if (a.plan && a.plan[row].state != ROW_OPEN) {
@@ -1104,7 +1142,7 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, cons
     if (tid == 0) give(a, row, none ? -1 : at, none ? 0.f : 1.f);
     return;
   }
-  choose(sh, a, row, w, weights_of(a, sh.roots, top, w.t), src, low, 0);
+  choose(sh, a, row, w, weights_of(sh.roots, unit, top, w.t), src, low, 0);
 }
 
 struct Layout {

@@ -310,3 +310,97 @@ def test_min_p_above_one(gpu_lib, dtype, D):
         for u in (0.0, 0.9):
             tokens = _check(x.to(dtype), [float(np.float32(u))] * len(sets), sets)
             assert (tokens == first).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D,x,dtype", [(1 << 20, -29.83, torch.float32),
+                                       (793_471, -29.5, torch.float16),
+                                       (1 << 24, -28.0, torch.float32),
+                                       (1 << 27, -25.0, torch.bfloat16)])
+def test_long_tails_of_small_weights(gpu_lib, D, x, dtype):
+    """One entry of weight 1 behind n = D - 1 equal ones of weight w, each of which is less than
+    2^-62 D / 2 (half the step that D sums of at most 1 leave in 64 bits) or little more.  Sums
+    are off by at most e = 2^-52 D of the total: both sums of a comparison, and with top-p the
+    two of its border too, make 4 e / w entries."""
+    n, w = D - 1, float(np.exp(float(torch.tensor(x, dtype=dtype))))
+    T = 1 + n * w
+    half = float(np.float32(1 - n * w / 2))  # top-p that keeps about half of the tail
+    low = float(np.float32(w / 2))
+    share = n * w / T
+    rows = [(share * s, k) for s in (1 / 8, 3 / 8, 3 / 4)
+            for k in (dict(), dict(top_p=half), dict(min_p=low), dict(top_k=D - D // 8),
+                      dict(top_p=half, min_p=low))]
+    rows += [(0.5, dict()), (0.0, dict()), (share / 2, dict(min_p=4 * low))]
+    default = dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0)
+    kw = {name: _device(name, [{**default, **s}[name] for _, s in rows]) for name in NAMES}
+    u = [float(np.float32(v)) for v, _ in rows]
+    logits = torch.full((len(rows), D), x, device="cuda", dtype=dtype)
+    logits[:, n] = 0.0
+    tokens, prob = lst.lst_sample(logits, _device("u", u), **kw)
+    tokens, prob = tokens.tolist(), prob.tolist()
+    slack = 4 * D * 2.0 ** -52 * T / w + 2
+    for i, (_, s) in enumerate(rows):
+        kept = n
+        if "top_p" in s:
+            kept = int(np.ceil((float(np.float32(s["top_p"])) * T - 1) / w))
+        if "top_k" in s:
+            kept = s["top_k"] - 1
+        if s.get("min_p", 0.0) > w:
+            kept = 0
+        total = 1 + kept * w
+        want = int(u[i] * total / w)
+        assert abs(want - kept) > slack, i  # on one side of the tail's end
+        want = want if want < kept else n
+        assert abs(tokens[i] - want) <= (slack if want < n else 0), (i, s, tokens[i], want)
+        p = (w if want < n else 1.0) / total
+        assert abs(prob[i] - p) <= (2.0 ** -23 + D * 2.0 ** -51) * p, (i, s, prob[i], p)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_more_than_eight_million_entries(gpu_lib, dtype):
+    """Rows whose stretches are more than one block's bins."""
+    D = 8_500_003
+    x, u = _logits(1, D, dtype, 12, spread=1.5)
+    x[0, ::7] = -float("inf")
+    sets = [dict(temperature=0.0), dict(top_k=50, top_p=0.9), dict(top_k=4000),
+            dict(top_k=20_000, min_p=1e-4), dict(min_p=0.3)]
+    us = [float(np.float32((u[0] + 0.19 * i) % 1)) for i in range(len(sets) + 3)]
+    xs = x[0].double().cpu().numpy()
+    order = np.argsort(-xs, kind="stable")
+    order = order[xs[order] > -np.inf]
+    some = np.where(np.isin(np.arange(D), order[:30_000]), xs, -np.inf)  # what these settings keep
+    rows = x.repeat(len(sets) + 3, 1)
+    more = [dict(), dict(top_p=0.8), dict(top_p=0.7, min_p=0.002, temperature=1.5)]
+    default = dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0)
+    kw = {n: _device(n, [{**default, **s}[n] for s in sets + more]) for n in NAMES}
+    tokens, prob = (t.tolist() for t in lst.lst_sample(rows, _device("u", us), **kw))
+    for i, s in enumerate(sets):
+        want, p = answers.sample(some, us[i], **s)
+        assert tokens[i] == want and abs(prob[i] - p) <= 2.0 ** -23 * p + 2.0 ** -40, (i, s)
+    for i, s in enumerate(more, len(sets)):  # the same choice, all entries at once
+        s = {**default, **s}
+        w = np.exp((xs[order] - xs[order[0]]) / float(np.float32(s["temperature"])))
+        before = np.concatenate([[0.0], np.cumsum(w)])
+        p, q = float(np.float32(s["top_p"])), float(np.float32(s["min_p"]))
+        keep = len(w) if p >= 1 else int((before[:-1] < p * before[-1]).sum())
+        keep = max(1, min(keep, int((w >= q).sum())))
+        by = np.argsort(order[:keep])
+        sums = np.cumsum(w[by])
+        j = int(np.searchsorted(sums, us[i] * sums[-1], side="right"))
+        p = w[by[j]] / sums[-1]
+        assert tokens[i] == order[by[j]], (i, s)
+        assert abs(prob[i] - p) <= 2.0 ** -23 * p + 2.0 ** -40, (i, s)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [9000, 300_000])
+def test_hot_rows_between_the_ends_of_float32(gpu_lib, D):
+    """Differences that float32 does not hold, at temperatures that make weights of them."""
+    big = torch.finfo(torch.float32).max
+    x = torch.full((6, D), -big, device="cuda")
+    x[:, 5::1000] = big
+    x[:, 3] = 0.0
+    sets = [dict(temperature=t, **s) for t in (3e38, 1e38)
+            for s in (dict(), dict(top_p=0.6), dict(min_p=0.02, top_p=0.9))]
+    _check(x, [float(np.float32(0.1 + 0.17 * i)) for i in range(6)], sets)
