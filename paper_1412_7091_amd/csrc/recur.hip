@@ -44,6 +44,8 @@
 // registers (one block a compute unit) instead of 105 the backward pass took 248 us, and
 // with gates computed again in each phase instead of held 179.  8191 rows of 500 bfloat16
 // in 311 sequences are 256 blocks, one a compute unit: 17 and 22 us, a block's own latency.
+#include <algorithm>
+
 #include "dtypes.h"
 
 namespace lst {
@@ -133,9 +135,9 @@ Shape shape_of(int rows, int d, int vec) {
 
 __global__ __launch_bounds__(256) void recur_clear_kernel(unsigned long long* words, int64_t n,
                                                           unsigned* ticket) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i == 0) *ticket = 0;
-  if (i < n) words[i] = kNone;
+  for (; i < n; i += (int64_t)gridDim.x * 256) words[i] = kNone;
 }
 
 struct Workspace {
@@ -673,6 +675,14 @@ int check_recur(int dtype, int rows, int n_seq, int d, const void* x, int64_t ld
   return LST_OK;
 }
 
+// A launch has fewer than 2^32 threads, and blocks take their chunks by a ticket that goes on
+// from one launch to the next: a pass of more threads comes in several launches.
+template <class F>
+void in_launches(int64_t blocks, int threads, F launch) {
+  const int64_t most = 0xFFFFFFFFu / threads;
+  for (; blocks > 0; blocks -= most) launch(dim3((unsigned)std::min(blocks, most)), dim3(threads));
+}
+
 // Calls run with the element type, the channels a lane, the shape and the workspace, cleared.
 template <class F>
 int with_shape(int dtype, int rows, int d, void* workspace, hipStream_t stream, F run) {
@@ -686,8 +696,9 @@ int with_shape(int dtype, int rows, int d, void* workspace, hipStream_t stream, 
         ws.ticket = (unsigned*)workspace;
         ws.chunk = (unsigned long long*)((char*)workspace + kHead);
         ws.group = ws.chunk + (int64_t)z.chunks * z.width;
-        hipLaunchKernelGGL(recur_clear_kernel, dim3((unsigned)((z.words() + 255) / 256)),
-                           dim3(256), 0, stream, ws.chunk, z.words(), ws.ticket);
+        const int64_t blocks = std::min<int64_t>((z.words() + 255) / 256, 1 << 22);
+        hipLaunchKernelGGL(recur_clear_kernel, dim3((unsigned)blocks), dim3(256), 0, stream,
+                           ws.chunk, z.words(), ws.ticket);
       }
       run(t, vec, z, ws);
       return launched();
@@ -732,9 +743,10 @@ int lst_recur_forward(int32_t dtype, int32_t rows, int32_t n_seq, int32_t d, con
                     [&](auto t, auto vec, const Shape& z, const Workspace& ws) {
     using T = decltype(t);
     constexpr int VEC = decltype(vec)::value, ROWS = 16;
-    hipLaunchKernelGGL((recur_forward_kernel<T, VEC, ROWS>),
-                       dim3((unsigned)(z.chunks * z.tiles)), dim3(64 * kChunk / ROWS), 0,
-                       (hipStream_t)hip_stream, a, z, ws, (const T*)x, (const T*)g, (T*)y);
+    in_launches((int64_t)z.chunks * z.tiles, 64 * kChunk / ROWS, [&](dim3 grid, dim3 block) {
+      hipLaunchKernelGGL((recur_forward_kernel<T, VEC, ROWS>), grid, block, 0,
+                         (hipStream_t)hip_stream, a, z, ws, (const T*)x, (const T*)g, (T*)y);
+    });
   });
 }
 
@@ -759,10 +771,11 @@ int lst_recur_backward(int32_t dtype, int32_t rows, int32_t n_seq, int32_t d, co
     using T = decltype(t);
     // 8 rows a wave with two channels a lane: 16 would take all registers
     constexpr int VEC = decltype(vec)::value, ROWS = 16 / VEC;
-    hipLaunchKernelGGL((recur_backward_kernel<T, VEC, ROWS>),
-                       dim3((unsigned)(z.chunks * z.tiles)), dim3(64 * kChunk / ROWS), 0,
-                       (hipStream_t)hip_stream, a, z, ws, (const T*)x, (const T*)g,
-                       (const T*)grad_y, (T*)grad_x, (T*)grad_g);
+    in_launches((int64_t)z.chunks * z.tiles, 64 * kChunk / ROWS, [&](dim3 grid, dim3 block) {
+      hipLaunchKernelGGL((recur_backward_kernel<T, VEC, ROWS>), grid, block, 0,
+                         (hipStream_t)hip_stream, a, z, ws, (const T*)x, (const T*)g,
+                         (const T*)grad_y, (T*)grad_x, (T*)grad_g);
+    });
   });
 }
 

@@ -403,3 +403,28 @@ def test_gradients_in_place(gpu_lib, dtype):
     a = x.clone()
     lst.lst_recur_forward(a, g, off, out=a)
     assert torch.equal(a, y)
+
+
+@pytest.mark.gpu
+def test_the_most_rows(gpu_lib):
+    """2^30 rows, which no single launch has threads for; the rows repeat, and so do the results.
+    Sequences of two chunks: one of them lies across the launches' border in each pass."""
+    rows, part, d, length = 1 << 30, 1 << 20, 2, 256
+    g = torch.Generator("cuda").manual_seed(19)
+    x, gate, dy = (torch.randn((part, d), device="cuda", generator=g).bfloat16() for _ in range(3))
+    h0, dlast = (torch.randn((part // length, d), device="cuda", generator=g) for _ in range(2))
+    many = rows // part
+    n = part // length
+    y, last, saved = lst.lst_recur_forward(x, gate, None, h0, n_seq=n, save=True)
+    want = (y, last, *lst.lst_recur_backward(x, gate, dy, saved, None, h0, dlast, n_seq=n))
+    off = np.arange(3) * length
+    wy, wl, ey, el, _ = between.recur(_np(x[:512]), _np(gate[:512]), off, _np(h0[:2]))
+    _check(y[:512], wy, ey, torch.bfloat16)
+    _check(last[:2], wl, el)
+    x, gate, dy, h0, dlast = (t.repeat(many, 1) for t in (x, gate, dy, h0, dlast))
+    layer = lst.GatedRecurrence(d)
+    y, last, saved = layer.forward(x, gate, None, h0, n_seq=many * n, save=True)
+    got = (y, last, *layer.backward(x, gate, dy, saved, None, h0, dlast, n_seq=many * n))
+    assert layer.sync() == 0
+    for a, b in zip(got, want):
+        assert bool((a.view(many, *b.shape) == b).all())
