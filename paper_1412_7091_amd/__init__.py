@@ -921,8 +921,12 @@ class EightBitOutputLayer:
             return W
         import torch
 
-        W = W.materialize_W()
-        torch.cuda.synchronize(W.device)  # a layer works on the stream of its own
+        # a layer works on the stream of its own: it must not write before the current stream is
+        # done with what was in the new tensor's memory, nor be read before it has written
+        out = torch.empty((W.D, W.d), dtype=torch.float32, device=W.device)
+        torch.cuda.synchronize(out.device)
+        W = W.materialize_W(out)
+        torch.cuda.synchronize(out.device)
         return W
 
     def load(self, W) -> None:

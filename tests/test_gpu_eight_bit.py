@@ -269,3 +269,30 @@ def test_sizes_behind_the_limits():
         assert lib.lst_quantize(0, rows, cols, P, cols, P, P, None) == lst.LST_EINVAL
     for m, D in (((1 << 20) + 1, 5), (1 << 20, 1 << 20), (17, 1 << 36)):
         assert lib.lst_scores(0, 0, m, D, 8, P, 8, P, P, P, D, P, None) == lst.LST_EINVAL
+
+
+@pytest.mark.gpu
+def test_of_a_layer_on_another_stream(gpu_lib):
+    """The tensor that takes the layer's weights may get memory that the current stream has still
+    to write to (it was freed there, with work under way); the layer's own stream must wait."""
+    D, d = 4000, 96
+    g = torch.Generator("cuda").manual_seed(15)
+    V = torch.randn((D, d), device="cuda", generator=g)
+    want = lst.lst_quantize(V)
+    busy = torch.randn((4096, 4096), device="cuda", generator=g)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    layer = lst.FactoredOutputLayer(V, m_max=4, K_max=2, stream=side)
+    held = lst.EightBitOutputLayer(layer)
+    torch.cuda.synchronize()
+    assert torch.equal(held.codes, want[0]) and torch.equal(held.scales, want[1])
+    for _ in range(3):
+        a = busy
+        for _ in range(10):
+            a = a @ busy * 2.0 ** -6  # some milliseconds
+        late = torch.empty((D, d), device="cuda")
+        late.copy_(a[0, 0].expand(D, d))
+        del late
+        held.load(layer)
+        assert torch.equal(held.codes, want[0]) and torch.equal(held.scales, want[1])
+    layer.close()
