@@ -296,3 +296,50 @@ def test_of_a_layer_on_another_stream(gpu_lib):
         held.load(layer)
         assert torch.equal(held.codes, want[0]) and torch.equal(held.scales, want[1])
     layer.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [128, 500])
+@pytest.mark.parametrize("m", [3, 40, 150])
+def test_small_products_beside_large_ones(gpu_lib, m, d):
+    """Two products of 2^16 that cancel beside products of 2^-4 to 4: all codes and all partial
+    sums are multiples of 2^-4 below 2^17 and exact in float32 in any order, so the sum is too.
+    (A unit that drops what is 2^-14 of the largest product beside it does not pass.)"""
+    rng = np.random.default_rng(m + d)
+    D = 77
+    W = rng.choice([0.25, 0.5, 1.0, 2.0, -0.25, -0.5, -1.0, -2.0], (D, d))
+    H = rng.choice([0.25, 0.5, 1.0, 2.0, -0.25, -0.5, -1.0, -2.0], (m, d))
+    blocks = -(-d // 128)
+    big = np.concatenate([b * 128 + rng.choice(min(128, d - b * 128), 8, replace=False)
+                          for b in range(blocks)]).reshape(blocks, 8)
+    H[:, big.ravel()] = 256.0
+    W[:, big.ravel()] = 0.0
+    for r in range(D):
+        for b in range(blocks):
+            i, j = rng.choice(8, 2, replace=False)
+            W[r, big[b, i]], W[r, big[b, j]] = 256.0, -256.0
+    layer = lst.EightBitOutputLayer(torch.tensor(W, dtype=torch.float32, device="cuda"))
+    got = layer.scores(torch.tensor(H, dtype=torch.float32, device="cuda"))
+    assert np.array_equal(_np(got), H @ W.T)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m", [3, 40])
+def test_scores_at_the_ends_of_the_scales(gpu_lib, m):
+    """Blocks with the smallest scale (2^-127) and with the largest ones, against rows that bring
+    the products back."""
+    D, d = 100, 300
+    g = torch.Generator("cuda").manual_seed(m)
+    for size in (-127, -122, -119, -110, 100, 110):
+        W = torch.randn((D, d), device="cuda", generator=g).double()
+        H = torch.randn((m, d), device="cuda", generator=g).double()
+        W, H = (W * 2.0 ** size).float(), (H * 2.0 ** (-size // 2)).float()
+        for a, b in ((W, H), (H, W)):
+            layer = lst.EightBitOutputLayer(a)
+            got = layer.scores(b)
+            hq = answers.values(*answers.quantize(_np(b)))
+            wq = answers.values(layer.codes.cpu().numpy(), layer.scales.cpu().numpy())
+            want, bar = answers.scores(hq, wq)
+            # values and sums below 2^-126 may count as zero
+            tiny = 2.0 ** -126 * (np.abs(hq).sum(1)[:, None] + np.abs(wq).sum(1)[None] + 1)
+            assert (np.abs(_np(got) - want) <= bar + tiny).all(), size
