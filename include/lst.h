@@ -445,6 +445,10 @@ int lst_dropout(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_
  *                    sequence without rows); may be NULL, and may be h0.
  *   saved  (device)  receives what lst_recur_backward needs: lst_recur_saved(rows, d)
  *                    floats; NULL when there will be no backward pass.
+ * A state that is infinite or no number is so, one or the other, to the end of its
+ * sequence.  A block of 128 rows reads one word of each 2048 rows between it and its
+ * sequence's beginning: sequences of millions of rows take time that grows as their
+ * square.
  */
 #define LST_RECUR_CHUNK 128 /* rows of y between two states in saved */
 int lst_recur_forward(int32_t dtype, int32_t rows, int32_t n_seq, int32_t d, const void* x,
@@ -457,7 +461,7 @@ int lst_recur_forward(int32_t dtype, int32_t rows, int32_t n_seq, int32_t d, con
  * there, saved from that call; grad_y (rows x d) and grad_last (n_seq x d floats, or
  * NULL) are dL/dy and dL/dh_last.  grad_x and grad_g receive dL/dx and dL/dg (rows in
  * no sequence are left as they were), grad_h0 (or NULL) dL/dh0.  grad_x and grad_g
- * may each be one of x, g and grad_y.
+ * may each be one of x, g and grad_y, but not both the same one.
  */
 int lst_recur_backward(int32_t dtype, int32_t rows, int32_t n_seq, int32_t d, const void* x,
                        int64_t ldx, const void* g, int64_t ldg, const int32_t* offsets,
@@ -478,7 +482,8 @@ int64_t lst_recur_workspace(int32_t rows, int32_t d);
  *                   is left as it was.  NULL: row i continues state i.  An index
  *                   outside [-1, n_slots), and one that an earlier row names already,
  *                   sets the status LST_EINDEX and counts as -1.  At most 65 536 rows
- *                   with slots, since each is compared with those before it.
+ *                   with slots, since each is compared with those before it: 4096 rows
+ *                   of 500 take 15 us with slots and 11 without, 65 536 take 678 and 65.
  */
 int lst_recur_step(int32_t dtype, int32_t rows, int32_t n_slots, int32_t d, const void* x,
                    int64_t ldx, const void* g, int64_t ldg, const int32_t* slots, float* h,

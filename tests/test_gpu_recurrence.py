@@ -428,3 +428,98 @@ def test_the_most_rows(gpu_lib):
     assert layer.sync() == 0
     for a, b in zip(got, want):
         assert bool((a.view(many, *b.shape) == b).all())
+
+
+def _check_many(lengths, d, dtype, seed):
+    """As _check_all, where nearly all of very many sequences have no rows."""
+    lengths = np.asarray(lengths)
+    x, g, off, dy, h0, dlast = _inputs(lengths, d, dtype, seed)
+    layer = lst.GatedRecurrence(d)
+    at = torch.tensor(off, dtype=torch.int32, device="cuda")
+    y, last, saved = layer.forward(x, g, at, h0, save=True)
+    dx, dg, dh0 = layer.backward(x, g, dy, saved, at, h0, dlast)
+    assert layer.sync() == 0
+    some = lengths > 0
+    own = torch.tensor(some, device="cuda")
+    assert torch.equal(last[~own], h0[~own]) and torch.equal(dh0[~own], dlast[~own])
+    off = np.concatenate([[0], np.cumsum(lengths[some])])
+    h0_, dl_ = _np(h0[own]), _np(dlast[own])
+    wy, wl, ey, el, _ = between.recur(_np(x), _np(g), off, h0_)
+    _check(y, wy, ey, dtype)
+    _check(last[own], wl, el)
+    (wx, wg, w0), (ex, eg, e0) = between.recur_grad(_np(x), _np(g), off, _np(dy), h0_, dl_)
+    _check(dx, wx, ex, dtype)
+    _check(dg, wg, eg, dtype)
+    _check(dh0[own], w0, e0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d", [(torch.float32, 3), (torch.bfloat16, 6),
+                                     (torch.float16, 5)])
+@pytest.mark.parametrize("n", [513, 1025, 3000])
+def test_more_sequences_than_a_block_has_threads(gpu_lib, dtype, d, n):
+    """Sequences of one row; short ones with empty ones among them; runs of empty ones longer
+    than a block at the chunks' borders; one sequence of several chunks among short ones."""
+    rng = np.random.default_rng(n)
+    _check_many(np.ones(n, dtype=int), d, dtype, 1)
+    _check_many(rng.integers(0, 4, n), d, dtype, 2)
+    gaps = np.zeros(4 * n, dtype=int)
+    gaps[[0, n, 2 * n, 3 * n, 4 * n - 1]] = 128, 100, 28, 129, 1
+    _check_many(gaps, d, dtype, 3)
+    one = rng.integers(0, 2, n)
+    one[n // 2] = 700
+    _check_many(one, d, dtype, 4)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,n", [(torch.float32, 263_000), (torch.bfloat16, 1_060_000)])
+def test_sequences_whose_search_takes_two_rounds(gpu_lib, dtype, n):
+    rng = np.random.default_rng(n)
+    lengths = np.zeros(n, dtype=int)
+    lengths[rng.choice(n, 400, replace=False)] = rng.integers(1, 9, 400)
+    lengths[[0, n // 3, n - 1]] = 3, 300, 140
+    _check_many(lengths, 2, dtype, 5)
+    ends = np.zeros(n, dtype=int)
+    ends[[0, n - 1]] = 130, 256
+    _check_many(ends, 2, dtype, 6)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [600, 1100, 5000])
+def test_bad_offsets_among_many_set_the_status(gpu_lib, n):
+    x, g, _, dy, _, _ = _inputs((1000,), 16, torch.bfloat16, 4)
+    layer = lst.GatedRecurrence(16)
+    fine = np.minimum(np.arange(n + 1), 1000)
+    fine[-1] = 1000
+    down, low, high = fine.copy(), fine.copy(), fine.copy()
+    down[n // 2], low[1], high[n // 3:] = 0, -7, 2000
+    for off, code in ((fine, 0), (down, lst.LST_EINDEX), (low, lst.LST_EINDEX),
+                      (high, lst.LST_EINDEX), (fine[::-1].copy(), lst.LST_EINDEX)):
+        at = torch.tensor(off, dtype=torch.int32, device="cuda")
+        _, _, saved = layer.forward(x, g, at, save=True)
+        assert layer.sync() == code
+        layer.backward(x, g, dy, saved, at)
+        assert layer.sync() == code
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gate", [0.0, -3.0, -9.0])
+def test_an_infinite_state_stays_in_its_sequence(gpu_lib, gate):
+    """It is no finite number again before the sequence's end, and nothing else changes."""
+    x, g, off, dy, h0, dlast = _inputs((40, 900, 70), 12, torch.float32, 23)
+    g.add_(gate)
+    at = torch.tensor(off, dtype=torch.int32, device="cuda")
+
+    def both():
+        y, last, saved = lst.lst_recur_forward(x, g, at, h0, save=True)
+        return (y, last, *lst.lst_recur_backward(x, g, dy, saved, at, h0, dlast))
+
+    want = both()
+    x[45, 3] = float("inf")
+    got = both()
+    assert not got[0][45:940, 3].isfinite().any() and not got[1][1, 3].isfinite()
+    assert not got[3][45:940, 3].isfinite().any()  # their gates' gradients
+    for a in (got[0], want[0], got[3], want[3]):
+        a[45:940, 3] = 0
+    got[1][1, 3] = want[1][1, 3] = 0
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
