@@ -411,7 +411,8 @@ enum { LST_F32 = 0, LST_BF16 = 1, LST_F16 = 2 };
 /*
  * lst_dropout -- y = residual + x * keep / (1 - p), the mask drawn by a
  * counter-based generator and never stored.
- *   rows, cols      0 <= rows <= 2^32, 1 <= cols <= 2^30.
+ *   rows, cols      0 <= rows <= 2^32, 1 <= cols <= 2^30, and rows times (cols + 7) / 8
+ *                   at most 2^34 - 2^10.
  *   x, residual, y  rows x cols; residual may be NULL; y may be x or residual.
  *   p               probability that an element is dropped, in [0, 1], rounded to a
  *                   multiple of 2^-16; the factor is that of the rounded p.  A
@@ -499,14 +500,16 @@ int lst_recur_step(int32_t dtype, int32_t rows, int32_t n_slots, int32_t d, cons
  *                    is its code times 2^(scale - 127), the smallest power of two
  *                    with no value of the block above 448 times it (at least 2^-127).
  * Codes are rounded to nearest, ties to even.  A value that is not finite gives a
- * code that is no number and does not count for the scale.
+ * code that is no number and does not count for the scale.  A row takes 129 b bytes: a
+ * quarter of float32's at 512 columns, as many as float32's at 32.
  */
 int lst_quantize(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t ldx,
                  uint8_t* codes, uint8_t* scales, void* hip_stream);
 
 /*
  * lst_scores -- outputs of a layer held in 8 bits: O = H W^T.
- *   H                m x d of type dtype, quantised by the call as lst_quantize does.
+ *   H                m x d of type dtype, quantised by the call as lst_quantize does (each
+ *                    value to four binary digits).
  *   codes, scales    W (D x d) as lst_quantize leaves it.
  *   O                m x D of type out_dtype.
  *   m <= 2^20, D <= 2^36; for m > 16 or d > 2048, D <= 2^31 and m D <= 2^37.
@@ -523,7 +526,8 @@ int64_t lst_scores_workspace(int32_t m, int32_t d); /* bytes; -1 for a bad size 
  *   logits            m x D, 1 <= D <= 2^30.  Entries that are -inf or no number are never
  *                     chosen; when some are +inf, the choice is among those.
  *   temperature, top_k, top_p, min_p, u (device, m values each; the first four may
- *                     be NULL: 1, 0, 1, 0).
+ *                     be NULL: 1, 0, 1, 0).  Mask entries with -inf: a finite low value
+ *                     can make long rows take twenty times as long.
  *   tokens (device)   m ints: receives the tokens.
  *   prob   (device)   m floats, or NULL: receives each token's probability among the
  *                     entries that were kept.

@@ -10,7 +10,9 @@ built, load_library() raises instead of falling back to anything.
 Classes FactoredOutputLayer and NaiveOutputLayer wrap a state handle.  The
 operators around the layers (dropout, the gated recurrence, ...) hold no handle:
 they run on torch's current stream of their tensors' device, and their workspaces
-are tensors of their own for each call.
+are tensors of their own for each call.  Like the layers they take no part in
+torch's autograd: forward and backward passes are called by name, and what comes
+back from a tensor that requires a gradient has no graph.
 """
 from __future__ import annotations
 
@@ -850,7 +852,8 @@ class NaiveOutputLayer(_Layer):
 
 class Dropout:
     """Dropout whose mask is drawn from (seed, offset, row, column) and never stored: the
-    backward pass takes the offset of its forward pass."""
+    backward pass takes the offset of its forward pass.  It is called by name: torch's autograd
+    does not see either."""
 
     def __init__(self, p: float, seed: int = 0):
         if not 0.0 <= p <= 1.0:
@@ -866,7 +869,10 @@ class Dropout:
 
 
 class GatedRecurrence:
-    """h_t = f_t h_{t-1} + (1 - f_t) x_t with f = sigmoid(g), over packed sequences."""
+    """h_t = f_t h_{t-1} + (1 - f_t) x_t with f = sigmoid(g), over packed sequences.
+
+    The backward pass is called by name: torch's autograd does not see either.  Rows that belong
+    to no sequence are not written: in outputs of the call's own they hold what the memory held."""
 
     def __init__(self, d: int, device="cuda"):
         import torch
@@ -907,8 +913,11 @@ class GatedRecurrence:
 
 
 class EightBitOutputLayer:
-    """The outputs O = H W^T of a trained layer, its weights held in 8 bits (a quarter of the
-    bytes): W is any D x d matrix, or an output layer, whose materialize_W gives one."""
+    """The outputs O = H W^T of a trained layer, its weights held in 8 bits: W is any D x d matrix,
+    or an output layer, whose materialize_W gives one.
+
+    A row takes 129 bytes for each 128 columns begun: a quarter of float32's at d = 512, as many
+    at d = 32.  H is rounded to 8 bits in the same way, in each call."""
 
     def __init__(self, W):
         W = self._weights(W)

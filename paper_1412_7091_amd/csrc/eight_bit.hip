@@ -14,7 +14,8 @@
 // of the largest product that is summed with it (measured: a product of 2^2 beside
 // one of 2^16), which is an error of 1.2e-5 in the sums of 128 ordinary products.
 //
-// The rows of H are quantised in the same way and left in bfloat16, in the order in
+// The rows of H are quantised in the same way, by the operator's definition (this instruction
+// would take eight binary digits at the same rate, where e4m3 has four), and left in bfloat16, in the order in
 // which the matrix instruction takes them: a fragment, 16 rows by 32 columns, is 64
 // lanes of 16 bytes.
 #include <algorithm>
@@ -104,7 +105,7 @@ __device__ inline void block_codes(const T* row, int col, int cols, uint32_t (&q
 }
 
 // 16 lanes a block, eight columns a lane.  Bound by memory: 793 471 x 300 floats (1.26 GB
-// with the codes) take 213 us, 5.9 TB/s; 32 lanes a block, four columns a lane with an access
+// with the codes) take 222 us, 5.7 TB/s; 32 lanes a block, four columns a lane with an access
 // for each, took 305 us.
 template <class T>
 __global__ __launch_bounds__(256) void quantize_kernel(const T* x, int64_t ldx, int64_t rows,

@@ -19,7 +19,8 @@
 // A row's map h -> f h + (1 - f) x, and so every stretch of rows, is a pair (A, B) with
 // h -> A h + B.  The block publishes the pair of its chunk, gathers those of the chunks
 // before it, back to the one in which the sequence of its first row begins, and only then
-// runs over its rows.
+// runs over its rows: the one-pass scan with look-back of Merrill and Garland ("Single-pass
+// parallel prefix scan with decoupled look-back", 2016), on pairs and by whole sequences.
 //
 //  - Blocks take their chunks by a ticket, so the chunks that a block waits for have
 //    blocks that run already, and a block publishes before it waits: no wait is
@@ -27,12 +28,14 @@
 //  - A pair is one 64-bit word, written and read by one atomic access, and no fence is
 //    needed; the workspace starts out as words that no pair has.
 //  - Every sixteenth block publishes the pair of its sixteen chunks too, so a block
-//    reads at most 31 pairs and one for each sixteen chunks farther back.  Which pairs
-//    it reads and how it joins them depends on the chunk alone: the result does not
-//    depend on which block was faster.
+//    reads at most 31 pairs and one for each sixteen chunks farther back (one sequence of
+//    1 048 576 rows of 64 floats takes 285 us forward, of 4 194 304 1860; as sequences of
+//    1024 rows 193 and 694).  Which pairs it reads and how it joins them depends on the
+//    chunk alone: the result does not depend on which block was faster.
 //  - The first row of a sequence forgets what comes in.  Its pair has A = -0, which no
 //    product of gates has (they are not negative): h -> B then, also where h is no
-//    number.
+//    number.  (A product of small gates may be 0, and 0 times an infinite state no number,
+//    where row after row it would stay infinite: it is not finite either way.)
 //
 // The backward pass runs the same way from the last chunk to the first on
 // (f L)_t = f_t (dL/dy_t + (f L)_{t+1}), and computes the states within a chunk again
@@ -63,7 +66,9 @@ struct RecurArgs {
 };
 
 // exp(-|g|) = 2^t (1 + r ln 2) with -|g| log2(e) = t + r, r the product's rounding: the rounded
-// product alone would cost |g| 2^-24 of the result, which gates of 16 bits cannot tell.
+// product alone would cost |g| 2^-24 of the smaller of f and 1 - f.  Gates of 16 bits go without
+// (also where the states that come of them are kept in float32): they are themselves off by
+// up to |g| 2^-8 (bfloat16) or |g| 2^-11 of it.
 template <class T>
 __device__ inline void gate(float g, float& f, float& i) {
   const float kLog2e = 1.44269504f, kLog2eLow = 1.925963033e-8f, kLn2 = 0.693147181f;

@@ -25,9 +25,14 @@
 //
 // Measured: one row of 200 000 floats with top-k 27 us, six launches that wait for each
 // other; 128 such rows with all kinds of settings 112 us (22 for the read of 102 MB), 64
-// rows of 793 471 bfloat16 with top-p alone 181 us (27 for the read).  The second and
+// rows of 793 471 bfloat16 with top-p alone 182 us (27 for the read).  The second and
 // third pass are bound by the weights' arithmetic (56 and 76 us), the rest by the latency
 // of blocks that search.  One block a row alone took 438, 938 and 3500 us.
+//
+// A row's bins share out the distance from its largest entry to its smallest one.  Entries
+// masked by a finite low value instead of -inf make them wide (64 t at most, without top-k),
+// and then the border's bin may hold more than 8192 entries: of 64 rows of 793 471 floats, one
+// entry in a hundred at -1e4, with top-p 0.9 all are left to one block each, 3.3 ms for 0.21.
 #include <algorithm>
 
 #include "dtypes.h"
@@ -49,7 +54,9 @@ constexpr int kSegment = 16384; // entries of one block that sorts them into bin
 constexpr int kLong = 8192;    // entries of a row's list in memory, at most
 // Rows up to this length take one launch.  128 rows with top-k 50 and top-p, top-p alone, and
 // neither: 35, 27 and 15 us in one launch and 25, 43 and 24 in six at 4096 entries, 43, 38 and
-// 19 against 25, 45 and 25 at 8000, 58, 58 and 29 against 26, 45 and 26 at 16 000.
+// 19 against 25, 45 and 25 at 8000, 58, 58 and 29 against 26, 45 and 26 at 16 000.  With top-k
+// six launches are the faster ones from 4096 entries on, without it not before 8192; which rows
+// have it is known on the device alone, and the line is the latter one.
 constexpr int kShort = 8192;
 constexpr int kBatch = 1024;   // rows of one set of launches
 // Rows up to this length have the step that D weights of 1 leave, which is 2^-27 of the total
