@@ -65,20 +65,33 @@ struct RecurArgs {
   int32_t* status;
 };
 
-// exp(-|g|) = 2^t (1 + r ln 2) with -|g| log2(e) = t + r, r the product's rounding: the rounded
-// product alone would cost |g| 2^-24 of the smaller of f and 1 - f.  Gates of 16 bits go without
-// (also where the states that come of them are kept in float32): they are themselves off by
-// up to |g| 2^-8 (bfloat16) or |g| 2^-11 of it.
+// exp(-|g|), whose relative error is that of f or 1 - f, whichever is smaller: to float32's
+// digits for all types, since the states are float32.  A product m log2(e) that is rounded would
+// cost |m| 2^-24.  The first 24 bits less a 16-bit type's own (8, 11) of log2(e) make one that is
+// exact, 2^(m hi), and the rest is exp(q) with q = m (1 - hi ln 2): at least -5e-4 and -5e-3
+// where the result is a normal number, so that one term and two are enough.
+template <class T>
+__device__ inline float exp_of(float m) {
+  constexpr bool bf16 = std::is_same_v<T, __bf16>;
+  const float kHi = bf16 ? 47274.f / 32768 : 5909.f / 4096;
+  const float kRest = bf16 ? 4.8884953e-06f : 4.719484e-05f;
+  const float q = fmaxf(m * kRest, -0.01f);  // finite for m = -inf
+  const float e = __builtin_amdgcn_exp2f(m * kHi);
+  return fmaf(e, bf16 ? q : q * fmaf(q, 0.5f, 1.f), e);
+}
+
+// 2^t (1 + r ln 2) with m log2(e) = t + r, r the product's rounding
+template <>
+__device__ inline float exp_of<float>(float m) {
+  const float kLog2e = 1.44269504f, kLog2eLow = 1.925963033e-8f, kLn2 = 0.693147181f;
+  const float t = m * kLog2e, r = fmaf(m, kLog2eLow, fmaf(m, kLog2e, -t));
+  const float e = __builtin_amdgcn_exp2f(t);
+  return m < -150.f ? 0.f : fmaf(e, r * kLn2, e);  // -inf: t + r is not a number
+}
+
 template <class T>
 __device__ inline void gate(float g, float& f, float& i) {
-  const float kLog2e = 1.44269504f, kLog2eLow = 1.925963033e-8f, kLn2 = 0.693147181f;
-  const float m = -fabsf(g), t = m * kLog2e;
-  float e = __builtin_amdgcn_exp2f(t);
-  if constexpr (sizeof(T) == 4) {
-    const float r = fmaf(m, kLog2eLow, fmaf(m, kLog2e, -t));
-    e = fmaf(e, r * kLn2, e);
-    e = m < -150.f ? 0.f : e;  // -inf: t + r is not a number
-  }
+  const float e = exp_of<T>(-fabsf(g));
   const float big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
   f = g < 0.f ? small : big;
   i = g < 0.f ? big : small;

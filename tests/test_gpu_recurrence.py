@@ -523,3 +523,25 @@ def test_an_infinite_state_stays_in_its_sequence(gpu_lib, gate):
         a[45:940, 3] = 0
     got[1][1, 3] = want[1][1, 3] = 0
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_shut_gates_of_any_type(gpu_lib, dtype):
+    """Gates that let next to nothing in, or out: what does pass has float32's digits in the
+    states, which are float32 whatever the rows' type."""
+    n, d = 300, 64
+    torch.manual_seed(31)
+    size = torch.linspace(9, 85, d, device="cuda")
+    x, dy = (torch.randn((n, d), device="cuda").to(dtype) for _ in range(2))
+    for sign in (1.0, -1.0):
+        g = (sign * size * (1 + 0.01 * torch.rand((n, d), device="cuda"))).to(dtype)
+        for h0 in (None, torch.randn((1, d), device="cuda")):
+            _check_all(x, g, np.array([0, n]), dy, h0, None)
+            layer = lst.GatedRecurrence(d)
+            h = torch.zeros((n, d), device="cuda")
+            y = layer.step(x, g, h)
+            off = np.arange(n + 1)
+            wy, wl, ey, el, _ = between.recur(_np(x), _np(g), off)
+            _check(y, wy, ey, dtype)
+            _check(h, wl, el)
