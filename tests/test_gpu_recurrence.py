@@ -545,3 +545,29 @@ def test_shut_gates_of_any_type(gpu_lib, dtype):
             wy, wl, ey, el, _ = between.recur(_np(x), _np(g), off)
             _check(y, wy, ey, dtype)
             _check(h, wl, el)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gates_without_end_of_any_type(gpu_lib, dtype):
+    """Infinite gates keep the state or take the row exactly, also the largest finite ones; a gate
+    that is no number leaves none."""
+    n, d = 200, 6
+    torch.manual_seed(32)
+    x = torch.randn((n, d), device="cuda").to(dtype)
+    g = torch.zeros((n, d), device="cuda").to(dtype)
+    big = torch.finfo(dtype).max
+    g[:, 0], g[:, 1], g[:, 2], g[:, 3] = float("inf"), -float("inf"), big, -big
+    g[90, 4] = float("nan")
+    h0 = torch.randn((1, d), device="cuda")
+    y, last, _ = lst.lst_recur_forward(x, g, None, h0)
+    for c in (0, 2):
+        assert torch.equal(y[:, c], h0[0, c].to(dtype).expand(n)) and last[0, c] == h0[0, c]
+    for c in (1, 3):
+        assert torch.equal(y[:, c], x[:, c])
+    assert y[:90, 4].isfinite().all() and y[90:, 4].isnan().all() and last[0, 4].isnan()
+    assert y[:, 5].isfinite().all()
+    h = h0.repeat(n, 1)
+    lst.lst_recur_step(x, g, h)
+    assert torch.equal(h[:, 0], h0[0, 0].expand(n)) and torch.equal(h[:, 3], x[:, 3].float())
+    assert h[90, 4].isnan() and h[:90, 4].isfinite().all()
