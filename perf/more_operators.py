@@ -127,6 +127,10 @@ def prepare(case, seed):
             s["out"].append(torch.empty_like(t)[:, :cols] if c["above"] else t[:, :cols])
         total = sum(float(t.double().square().sum()) for t in s["grads"])
         s["max_norm"] = float(np.float32(math.sqrt(total) * (0.3 if c["above"] else 3.0)))
+        if own:  # the gradients' buffers stay from step to step, and so does their list
+            import paper_1412_7091_amd as lst
+
+            s["clip"] = lst.GradientClip(s["grads"], out=s["out"])
         return s
     dt = DTYPES[c["type"]]
     if c["op"] in ("norm", "coded"):
@@ -161,7 +165,7 @@ def prepare(case, seed):
         if c["op"] == "logtrain":
             s["grad_logp"] = _normal(g, m, K)
             s["grad_entropy"] = _normal(g, m, scale=0.1)
-    if own and c["op"] in ("norm", "coded"):
+    if own and c["op"] in ("norm", "coded"):  # a layer that the program keeps
         import paper_1412_7091_amd as lst
 
         s["layer"] = lst.RMSNorm(s["weight"], eps=EPS)
@@ -310,11 +314,11 @@ def _run_own(s, c):
         codes, scales, total = s["layer"].forward_coded(s["x"], s["residual"])
         return codes.view(torch.float8_e4m3fn), scales.view(torch.float8_e8m0fnu), total
     if c["op"] == "quantize4":
-        return lst.lst_quantize4(s["W"])
+        return lst.lst_quantize_four(s["W"])
     if c["op"] == "four":
-        return lst.lst_scores4(s["H"], s["codes"], s["scales"], dtype=DTYPES[c["out"]])
+        return lst.lst_scores_four(s["H"], s["codes"], s["scales"], dtype=DTYPES[c["out"]])
     if c["op"] == "clip":
-        return lst.lst_clip(s["grads"], s["max_norm"], out=s["out"]), s["out"]
+        return s["clip"].clip(s["max_norm"]), s["out"]
     logp, entropy, ids, best, saved = lst.lst_logprobs(
         s["logits"], s["tokens"], top=c["top"], temperature=s["temperature"],
         save=c["op"] == "logtrain")
