@@ -492,6 +492,40 @@ int lst_recur_step(int32_t dtype, int32_t rows, int32_t n_slots, int32_t d, cons
                    void* y, int64_t ldy, int32_t* status, void* hip_stream);
 
 /*
+ * lst_norm_forward -- root-mean-square norm of rows, with the residual's addition:
+ *   s = x + residual,  q = 1 / sqrt(mean(s^2) + eps),  y = q s weight.
+ *   rows, cols      0 <= rows <= 2^40, 1 <= cols <= 4096.
+ *   x, residual     rows x cols; residual may be NULL.
+ *   weight (device) cols floats.
+ *   eps             2^-100 .. 2^100.
+ *   sum             receives s, rounded to the type (the norm is of the rounded s); NULL when
+ *                   it is not wanted.  May be x or residual.
+ *   y               receives the rows; may be x or residual, not sum; NULL when codes are given.
+ *   codes, scales (device)  receive y (before it is rounded to the type) in 8 bits, as
+ *                   lst_quantize leaves a matrix: input for lst_scores_coded.  Both NULL when
+ *                   not wanted; codes 16-byte aligned.
+ *   rstd   (device) rows floats, receives q for lst_norm_backward; may be NULL.
+ * The squares are summed in 64 bits.
+ */
+int lst_norm_forward(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t ldx,
+                     const void* residual, int64_t ldr, const float* weight, double eps, void* sum,
+                     int64_t lds, void* y, int64_t ldy, uint8_t* codes, uint8_t* scales,
+                     float* rstd, void* hip_stream);
+
+/*
+ * lst_norm_backward -- gradients of lst_norm_forward.  sum: its s (x where there was no
+ * residual), rstd as it left it.  grad_y and grad_sum (or NULL) are dL/dy and what else of dL/ds
+ * there is; grad_x receives the gradient with respect to x, which is the residual's too, and may
+ * be sum, grad_y or grad_sum.  grad_weight (device, cols floats) receives the sums over all rows
+ * (zeros for none), added in an order that does not depend on timing.
+ */
+int lst_norm_backward(int32_t dtype, int64_t rows, int32_t cols, const void* sum, int64_t lds,
+                      const float* weight, const float* rstd, const void* grad_y, int64_t ldgy,
+                      const void* grad_sum, int64_t ldgs, void* grad_x, int64_t ldgx,
+                      float* grad_weight, void* workspace, void* hip_stream);
+int64_t lst_norm_workspace(int64_t rows, int32_t cols); /* bytes; -1 for a bad size */
+
+/*
  * lst_quantize -- a matrix (the weights of a trained layer: lst_materialize_W) into
  * 8 bits, with one scale for each block of 128 columns of a row.
  *   x       rows x cols, 1 <= cols <= 4096; rows x b below 2^28 - 15.
@@ -521,6 +555,47 @@ int lst_scores(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int32_t d
                int64_t ldh, const uint8_t* codes, const uint8_t* scales, void* O, int64_t ldo,
                void* workspace, void* hip_stream);
 int64_t lst_scores_workspace(int32_t m, int32_t d); /* bytes; -1 for a bad size */
+
+/*
+ * lst_scores_coded -- lst_scores for rows of H that are codes already: as lst_quantize or
+ * lst_norm_forward leaves them (h_codes 16-byte aligned).  The same outputs, bit for bit, as
+ * lst_scores gives for rows whose codes these are; workspace and limits are its own.
+ */
+int lst_scores_coded(int32_t out_dtype, int32_t m, int64_t D, int32_t d, const uint8_t* h_codes,
+                     const uint8_t* h_scales, const uint8_t* codes, const uint8_t* scales, void* O,
+                     int64_t ldo, void* workspace, void* hip_stream);
+
+/*
+ * lst_quantize_four -- a matrix into 4 bits, with one scale for each block of 32 columns of a
+ * row.
+ *   x       rows x cols, 1 <= cols <= 4096; rows x b below 2^30 - 63.
+ *   codes  (device)  rows x 16 b bytes, b = (cols + 31) / 32, 16-byte aligned: receives e2m1
+ *                    values (0, 1/2, 1, 3/2, 2, 3, 4, 6, and with the sign in the highest
+ *                    bit the same below zero), two a byte, the lower column in the lower
+ *                    half; zeros behind the last column.
+ *   scales (device)  rows x b bytes: receives biased exponents; a value of the block is its
+ *                    code's times 2^(scale - 127), the smallest power of two with no value of
+ *                    the block above 6 times it (at least 2^-127).
+ * Codes are rounded to nearest, ties to even.  A block with a value that is not finite gets the
+ * scale 255: all of it is no number.  A row takes 17 b bytes, 272 at 512 columns.
+ */
+int lst_quantize_four(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t ldx,
+                      uint8_t* codes, uint8_t* scales, void* hip_stream);
+
+/*
+ * lst_scores_four -- outputs of a layer held in 4 bits: O = H W^T.
+ *   H                m x d of type dtype, quantised by the call as lst_quantize_four does (each
+ *                    value to two binary digits).
+ *   codes, scales    W (D x d) as lst_quantize_four leaves it.
+ *   O                m x D of type out_dtype.
+ *   m <= 2^20, D <= 2^36; for m > 16, D <= 2^31 and m D <= 2^37.
+ * The quantised values are multiplied exactly and summed in float32 (those below 2^-126 may
+ * count as zero).
+ */
+int lst_scores_four(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int32_t d,
+                    const void* H, int64_t ldh, const uint8_t* codes, const uint8_t* scales,
+                    void* O, int64_t ldo, void* workspace, void* hip_stream);
+int64_t lst_scores_four_workspace(int32_t m, int32_t d); /* bytes; -1 for a bad size */
 
 /*
  * lst_sample -- a token from each row of outputs.

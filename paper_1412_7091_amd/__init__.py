@@ -152,6 +152,22 @@ _SIGS = {
     "lst_scores": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64,
                                   ctypes.c_int32, _P, ctypes.c_int64, _P, _P, _P, ctypes.c_int64,
                                   _P, _P]),
+    "lst_scores_coded": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int64,
+                                        ctypes.c_int32, _P, _P, _P, _P, _P, ctypes.c_int64, _P,
+                                        _P]),
+    "lst_norm_forward": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, _P,
+                                        ctypes.c_int64, _P, ctypes.c_int64, _P, ctypes.c_double,
+                                        _P, ctypes.c_int64, _P, ctypes.c_int64, _P, _P, _P, _P]),
+    "lst_norm_backward": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, _P,
+                                         ctypes.c_int64, _P, _P, _P, ctypes.c_int64, _P,
+                                         ctypes.c_int64, _P, ctypes.c_int64, _P, _P, _P]),
+    "lst_norm_workspace": (ctypes.c_int64, [ctypes.c_int64, ctypes.c_int32]),
+    "lst_quantize_four": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, _P,
+                                         ctypes.c_int64, _P, _P, _P]),
+    "lst_scores_four_workspace": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32]),
+    "lst_scores_four": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                       ctypes.c_int64, ctypes.c_int32, _P, ctypes.c_int64, _P, _P,
+                                       _P, ctypes.c_int64, _P, _P]),
     "lst_sample": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P,
                                   ctypes.c_int64, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
     "lst_sample_workspace": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32]),
@@ -609,6 +625,18 @@ def lst_scores_workspace(m: int, d: int) -> int:
     return int(load_library().lst_scores_workspace(m, d))
 
 
+def _scores_out(H, m, D, dtype, out):
+    """(out, its dtype code, address, row stride) for m rows of D outputs beside H."""
+    if out is None:
+        out = H.new_empty((m, D), dtype=dtype)
+    elif dtype is not None and out.dtype != dtype:
+        raise TypeError(f"out must be {dtype}, got {out.dtype}")
+    po, ldo = _matrix(out, "out", shape=(m, D))
+    if out.device != H.device:
+        raise TypeError(f"out must be on {H.device}")
+    return out, _dtype_code(out, "out"), po, ldo
+
+
 def lst_scores(H, codes, scales, *, dtype=None, out=None):
     """O = H W^T from the weights' codes and scales; dtype: that of O (H's when not given)."""
     import torch
@@ -620,19 +648,159 @@ def lst_scores(H, codes, scales, *, dtype=None, out=None):
     blocks = (d + 127) // 128
     if scales.dim() != 2 or scales.shape[1] != blocks or codes.shape != (D, 128 * blocks):
         raise ValueError(f"codes and scales must be those of a matrix with {d} columns")
-    if out is None:
-        out = H.new_empty((m, D), dtype=dtype or H.dtype)
-    elif dtype is not None and out.dtype != dtype:
-        raise TypeError(f"out must be {dtype}, got {out.dtype}")
-    po, ldo = _matrix(out, "out", shape=(m, D))
-    if out.device != dev:
-        raise TypeError(f"out must be on {dev}")
+    out, ocode, po, ldo = _scores_out(H, m, D, dtype or (H.dtype if out is None else None), out)
     work = _work(H, lst_scores_workspace(m, d))
-    _enqueue("lst_scores", dev, code, _dtype_code(out, "out"), m, D, d, ph, ldh,
+    _enqueue("lst_scores", dev, code, ocode, m, D, d, ph, ldh,
              _vector(codes, torch.uint8, "codes", dev),
              _vector(scales, torch.uint8, "scales", dev), po, ldo,
              None if work is None else work.data_ptr())
     return out
+
+
+def lst_scores_coded(h_codes, h_scales, codes, scales, *, d=None, dtype=None, out=None):
+    """lst_scores for rows of H that are codes and scales already; d: columns (whole blocks when
+    not given), dtype: that of O (float32 when not given)."""
+    import torch
+
+    dev = h_codes.device
+    if any(t.dim() != 2 for t in (h_codes, h_scales, codes, scales)):
+        raise ValueError("codes and scales must be matrices")
+    (m, blocks), D = h_scales.shape, scales.shape[0]
+    if d is None:
+        d = 128 * blocks
+    if not h_codes.is_cuda or (d + 127) // 128 != blocks or h_codes.shape != (m, 128 * blocks):
+        raise ValueError(f"h_codes and h_scales must be those of a device matrix with {d} columns")
+    if scales.shape[1] != blocks or codes.shape != (D, 128 * blocks):
+        raise ValueError(f"codes and scales must be those of a matrix with {d} columns")
+    u8 = torch.uint8
+    out, ocode, po, ldo = _scores_out(h_codes, m, D,
+                                      dtype or (torch.float32 if out is None else None), out)
+    work = _work(h_codes, lst_scores_workspace(m, d))
+    _enqueue("lst_scores_coded", dev, ocode, m, D, d, _vector(h_codes, u8, "h_codes", dev),
+             _vector(h_scales, u8, "h_scales", dev), _vector(codes, u8, "codes", dev),
+             _vector(scales, u8, "scales", dev), po, ldo,
+             None if work is None else work.data_ptr())
+    return out
+
+
+def lst_quantize_four(x, *, codes=None, scales=None):
+    """(codes, scales) of a matrix in 4 bits, one scale for each block of 32 columns."""
+    import torch
+
+    px, ldx = _matrix(x, "x")
+    code = _dtype_code(x, "x")
+    rows, cols = x.shape
+    blocks = (cols + 31) // 32
+    if codes is None:
+        codes = x.new_empty((rows, 16 * blocks), dtype=torch.uint8)
+    if scales is None:
+        scales = x.new_empty((rows, blocks), dtype=torch.uint8)
+    _enqueue("lst_quantize_four", x.device, code, rows, cols, px, ldx,
+             _vector(codes, torch.uint8, "codes", x.device, rows * 16 * blocks),
+             _vector(scales, torch.uint8, "scales", x.device, rows * blocks))
+    return codes, scales
+
+
+@functools.lru_cache(maxsize=256)
+def lst_scores_four_workspace(m: int, d: int) -> int:
+    return int(load_library().lst_scores_four_workspace(m, d))
+
+
+def lst_scores_four(H, codes, scales, *, dtype=None, out=None):
+    """O = H W^T from the weights' 4-bit codes and scales, H in 4 bits too; dtype: that of O."""
+    import torch
+
+    ph, ldh = _matrix(H, "H")
+    code = _dtype_code(H, "H")
+    (m, d), dev = H.shape, H.device
+    D = scales.shape[0]
+    blocks = (d + 31) // 32
+    if scales.dim() != 2 or scales.shape[1] != blocks or codes.shape != (D, 16 * blocks):
+        raise ValueError(f"codes and scales must be those of a matrix with {d} columns")
+    out, ocode, po, ldo = _scores_out(H, m, D, dtype or (H.dtype if out is None else None), out)
+    work = _work(H, lst_scores_four_workspace(m, d))
+    _enqueue("lst_scores_four", dev, code, ocode, m, D, d, ph, ldh,
+             _vector(codes, torch.uint8, "codes", dev),
+             _vector(scales, torch.uint8, "scales", dev), po, ldo,
+             None if work is None else work.data_ptr())
+    return out
+
+
+@functools.lru_cache(maxsize=256)
+def lst_norm_workspace(rows: int, cols: int) -> int:
+    return int(load_library().lst_norm_workspace(rows, cols))
+
+
+def _weight(weight, x):
+    import torch
+
+    return _vector(weight, torch.float32, "weight", x.device, x.shape[1])
+
+
+def lst_norm_forward(x, weight, residual=None, *, eps=1e-6, out=None, sum_out=None, rstd=None):
+    """(y, s) of the root-mean-square norm: s = x + residual (x itself without one) and
+    y = s weight / rms(s).  rstd: a vector that receives each row's factor."""
+    import torch
+
+    px, ldx = _matrix(x, "x")
+    code = _dtype_code(x, "x")
+    pr, ldr = _matrix(residual, "residual", x, x.shape)
+    if out is None:
+        out = x.new_empty(x.shape)
+    if sum_out is None:
+        sum_out = x.new_empty(x.shape) if residual is not None else x
+    ps, lds = _matrix(sum_out if sum_out is not x else None, "sum_out", x, x.shape)
+    _enqueue("lst_norm_forward", x.device, code, x.shape[0], x.shape[1], px, ldx, pr, ldr,
+             _weight(weight, x), float(eps), ps, lds, *_matrix(out, "out", x, x.shape), None, None,
+             _vector(rstd, torch.float32, "rstd", x.device, x.shape[0]))
+    return out, sum_out
+
+
+def lst_norm_coded(x, weight, residual=None, *, eps=1e-6, codes=None, scales=None, sum_out=None,
+                   rstd=None):
+    """(codes, scales, s): lst_norm_forward with y in 8 bits, for lst_scores_coded."""
+    import torch
+
+    px, ldx = _matrix(x, "x")
+    code = _dtype_code(x, "x")
+    pr, ldr = _matrix(residual, "residual", x, x.shape)
+    (rows, cols), dev = x.shape, x.device
+    blocks = (cols + 127) // 128
+    if codes is None:
+        codes = x.new_empty((rows, 128 * blocks), dtype=torch.uint8)
+    if scales is None:
+        scales = x.new_empty((rows, blocks), dtype=torch.uint8)
+    if sum_out is None:
+        sum_out = x.new_empty(x.shape) if residual is not None else x
+    ps, lds = _matrix(sum_out if sum_out is not x else None, "sum_out", x, x.shape)
+    _enqueue("lst_norm_forward", dev, code, rows, cols, px, ldx, pr, ldr, _weight(weight, x),
+             float(eps), ps, lds, None, 0,
+             _vector(codes, torch.uint8, "codes", dev, rows * 128 * blocks),
+             _vector(scales, torch.uint8, "scales", dev, rows * blocks),
+             _vector(rstd, torch.float32, "rstd", dev, rows))
+    return codes, scales, sum_out
+
+
+def lst_norm_backward(s, rstd, weight, grad_y, grad_sum=None, *, out=None, grad_weight=None):
+    """(grad_x, grad_weight) from the forward pass' s and rstd; grad_x is the residual's too."""
+    import torch
+
+    ps, lds = _matrix(s, "s")
+    code = _dtype_code(s, "s")
+    (rows, cols), dev = s.shape, s.device
+    py, ldy = _matrix(grad_y, "grad_y", s, s.shape)
+    pd, ldd = _matrix(grad_sum, "grad_sum", s, s.shape)
+    if out is None:
+        out = s.new_empty((rows, cols))
+    if grad_weight is None:
+        grad_weight = s.new_empty(cols, dtype=torch.float32)
+    work = _work(s, lst_norm_workspace(rows, cols))
+    _enqueue("lst_norm_backward", dev, code, rows, cols, ps, lds, _weight(weight, s),
+             _vector(rstd, torch.float32, "rstd", dev, rows), py, ldy, pd, ldd,
+             *_matrix(out, "grad_x", s, s.shape),
+             _vector(grad_weight, torch.float32, "grad_weight", dev, cols),
+             None if work is None else work.data_ptr())
+    return out, grad_weight
 
 
 @functools.lru_cache(maxsize=256)
@@ -912,6 +1080,41 @@ class GatedRecurrence:
         return code
 
 
+class RMSNorm:
+    """Root-mean-square norm of rows with the residual's addition: s = x + residual,
+    y = s weight / sqrt(mean(s^2) + eps).  weight is a vector of float32 on the device, which the
+    layer keeps and reads in each call.  The backward pass is called by name: torch's autograd does
+    not see either."""
+
+    def __init__(self, weight, eps: float = 1e-6):
+        import torch
+
+        load_library()
+        if weight.dim() != 1:
+            raise ValueError("weight must be a vector")
+        _vector(weight, torch.float32, "weight", weight.device)
+        self.weight, self.eps = weight, float(eps)
+
+    def forward(self, x, residual=None, *, out=None, sum_out=None, save=False):
+        """(y, s, rstd); s is x itself without a residual, rstd None unless save."""
+        import torch
+
+        rstd = x.new_empty(x.shape[0], dtype=torch.float32) if save else None
+        y, s = lst_norm_forward(x, self.weight, residual, eps=self.eps, out=out, sum_out=sum_out,
+                                rstd=rstd)
+        return y, s, rstd
+
+    def forward_coded(self, x, residual=None, *, codes=None, scales=None, sum_out=None):
+        """(codes, scales, s): y in 8 bits, for EightBitOutputLayer.scores."""
+        return lst_norm_coded(x, self.weight, residual, eps=self.eps, codes=codes, scales=scales,
+                              sum_out=sum_out)
+
+    def backward(self, s, rstd, grad_y, grad_sum=None, *, out=None, grad_weight=None):
+        """(grad_x, grad_weight); grad_x is the gradient of x and of the residual."""
+        return lst_norm_backward(s, rstd, self.weight, grad_y, grad_sum, out=out,
+                                 grad_weight=grad_weight)
+
+
 class EightBitOutputLayer:
     """The outputs O = H W^T of a trained layer, its weights held in 8 bits: W is any D x d matrix,
     or an output layer, whose materialize_W gives one.
@@ -919,10 +1122,13 @@ class EightBitOutputLayer:
     A row takes 129 bytes for each 128 columns begun: a quarter of float32's at d = 512, as many
     at d = 32.  H is rounded to 8 bits in the same way, in each call."""
 
+    _quantize = staticmethod(lst_quantize)
+    _scores = staticmethod(lst_scores)
+
     def __init__(self, W):
         W = self._weights(W)
         self.D, self.d = W.shape
-        self.codes, self.scales = lst_quantize(W)
+        self.codes, self.scales = self._quantize(W)
 
     @staticmethod
     def _weights(W):
@@ -943,13 +1149,32 @@ class EightBitOutputLayer:
         W = self._weights(W)
         if tuple(W.shape) != (self.D, self.d):
             raise ValueError(f"W must be ({self.D}, {self.d})")
-        lst_quantize(W, codes=self.codes, scales=self.scales)
+        self._quantize(W, codes=self.codes, scales=self.scales)
 
     def scores(self, H, *, dtype=None, out=None):
+        """O = H W^T; H may be the pair (codes, scales) that lst_quantize or RMSNorm.forward_coded
+        left (then O is float32 unless dtype says otherwise)."""
+        if isinstance(H, (tuple, list)):
+            return self._scores_coded(*H, dtype=dtype, out=out)
         if H.dim() != 2 or H.shape[1] != self.d:
             raise ValueError(f"H must have {self.d} columns")
-        return lst_scores(H, self.codes, self.scales, dtype=dtype, out=out)
+        return self._scores(H, self.codes, self.scales, dtype=dtype, out=out)
+
+    def _scores_coded(self, h_codes, h_scales, **kw):
+        return lst_scores_coded(h_codes, h_scales, self.codes, self.scales, d=self.d, **kw)
 
     def sample(self, H, u, **settings):
         """(tokens, prob) chosen from the outputs for H: lst_sample's settings."""
         return lst_sample(self.scores(H, dtype=settings.pop("dtype", None)), u, **settings)
+
+
+class FourBitOutputLayer(EightBitOutputLayer):
+    """The outputs O = H W^T of a trained layer, its weights held in 4 bits, with one scale for
+    each 32 columns: 17 bytes for each 32 columns begun.  H is rounded to 4 bits in the same way,
+    in each call."""
+
+    _quantize = staticmethod(lst_quantize_four)
+    _scores = staticmethod(lst_scores_four)
+
+    def _scores_coded(self, *_, **__):
+        raise TypeError("outputs from 4 bits take rows of values: they are rounded to 4 bits")

@@ -21,39 +21,18 @@
 #include <algorithm>
 
 #include "dtypes.h"
+#include "eight_bit.h"
 #include "gemm_tile.h"
 
 namespace lst {
 namespace {
 
-constexpr int kBlock = 128;
-
 constexpr int kFragment = 64 * 8;          // bfloat16 of a fragment: 16 rows, 32 columns
 constexpr int kTile = 4 * kFragment;       // of 16 rows of one block
 
-typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
-typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-// Biased exponent of the scale for the bits of a block's largest finite magnitude:
-// 448 = 1.75 2^8, so 1.f 2^E needs 2^(E - 8) when 1.f <= 1.75, else 2^(E - 7).
-__device__ inline int scale_of(uint32_t big) {
-  const int e = (int)(big >> 23) - ((big & 0x7FFFFF) <= 0x600000 ? 8 : 7);
-  return max(e, 0);
-}
-
-// Codes of values times 2^(127 - e), which is exact: e is at most 254 - 7.
-template <int N>
-__device__ inline void codes_of(const float (&v)[N], int e, uint32_t (&q)[N / 4]) {
-  const float s = __uint_as_float((uint32_t)(254 - e) << 23);
-#pragma unroll
-  for (int i = 0; i < N / 4; ++i) {
-    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i] * s, v[4 * i + 1] * s, 0, false);
-    q[i] = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2] * s, v[4 * i + 3] * s, lo, true);
-  }
-}
 
 __device__ inline float scale_value(int e) {
   return __uint_as_float(e ? (uint32_t)e << 23 : 0x400000u);  // 2^(e - 127)
@@ -77,32 +56,32 @@ __device__ inline void block_codes(const T* row, int col, int cols, uint32_t (&q
   T raw[8];
   load_part(row, col, cols, raw);
   float v[8];
-  uint32_t big = 0;  // largest magnitude, by its bits
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    v[i] = (float)raw[i];
-    big = max(big, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-  }
-  uint64_t bad = 0;  // bytes that are no number in e4m3
-  if (big >= 0x7F800000u) {
-    big = 0;
-    for (int i = 0; i < 8; ++i) {
-      const uint32_t b = __float_as_uint(v[i]) & 0x7FFFFFFFu;
-      if (b >= 0x7F800000u) {
-        bad |= (uint64_t)0x7F << (8 * i);
-        v[i] = 0.f;
-      } else {
-        big = max(big, b);
-      }
-    }
-  }
-#pragma unroll
-  for (int o = 8; o; o >>= 1) big = max(big, (uint32_t)__shfl_xor((int)big, o));
-  e = scale_of(big);
-  codes_of(v, e, q);
-  q[0] |= (uint32_t)bad;
-  q[1] |= (uint32_t)(bad >> 32);
+  for (int i = 0; i < 8; ++i) v[i] = (float)raw[i];
+  values_codes(v, q, e);
 }
+
+// Rows of H as the kernels take them: values that they quantise, or codes as lst_quantize and
+// lst_norm_forward leave them.
+template <class T>
+struct Values {
+  const T* x;
+  int64_t ld;
+  int cols;
+  __device__ void block(int64_t n, int b, int c, uint32_t (&q)[2], int& e) const {
+    block_codes(x + n * ld, b * kBlock + 8 * c, cols, q, e);
+  }
+};
+struct Coded {
+  const uint8_t *codes, *scales;
+  int blocks;
+  __device__ void block(int64_t n, int b, int c, uint32_t (&q)[2], int& e) const {
+    const int64_t at = n * blocks + b;
+    const uintx2 v = reinterpret_cast<const uintx2*>(codes)[at * 16 + c];
+    q[0] = v[0], q[1] = v[1];
+    e = scales[at];
+  }
+};
 
 // 16 lanes a block, eight columns a lane.  Bound by memory: 793 471 x 300 floats (1.26 GB
 // with the codes) take 222 us, 5.7 TB/s; 32 lanes a block, four columns a lane with an access
@@ -133,15 +112,15 @@ __device__ inline int fragment_at(int n16, int l) {
 
 // Rows of H into fragments, tiles of 16 rows of one block: tile (b, n / 16) of the workspace.
 // Rows behind the last one of the last tile are zeros.
-template <class T>
-__global__ __launch_bounds__(256) void fragments_kernel(const T* x, int64_t ldx, int m, int cols,
-                                                        int blocks, int tiles, __bf16* out) {
+template <class R>
+__global__ __launch_bounds__(256) void fragments_kernel(R rows, int m, int blocks, int tiles,
+                                                        __bf16* out) {
   const int at = blockIdx.x * 16 + threadIdx.x / 16;
   if (at >= tiles * 16 * blocks) return;
   const int n = at / blocks, b = at - n * blocks, l = threadIdx.x % 16;
   uint32_t q[2] = {0, 0};
   int e = 0;
-  if (n < m) block_codes(x + (int64_t)n * ldx, b * kBlock + 8 * l, cols, q, e);
+  if (n < m) rows.block(n, b, l, q, e);
   __bf16* p = out + ((int64_t)b * tiles + n / 16) * kTile + fragment_at(n % 16, l);
   *reinterpret_cast<bf16x8*>(p) = widen(uintx2{q[0], q[1]}, scale_value(e));
 }
@@ -186,18 +165,17 @@ __device__ inline void store_tile(T* O, int64_t ldo, int m, int64_t D, int n, in
 // waves go through tiles of 16 rows of W, four blocks' codes under way at a time.  Bound by
 // memory: one row by 200 000 x 512 codes (104 MB) takes 21 us, 5.0 TB/s; with the
 // quantisation in a launch of its own 27.
-template <class TH, class T>
-__global__ __launch_bounds__(512) void scores_few_kernel(const TH* H, int64_t ldh, int d,
-                                                         const uint8_t* W, const uint8_t* sw,
-                                                         int m, int64_t D, int blocks, T* O,
-                                                         int64_t ldo) {
+template <class R, class T>
+__global__ __launch_bounds__(512) void scores_few_kernel(R rows, const uint8_t* W,
+                                                         const uint8_t* sw, int m, int64_t D,
+                                                         int blocks, T* O, int64_t ldo) {
   extern __shared__ __attribute__((aligned(16))) __bf16 few_lds[];
   const int l = threadIdx.x % 64, i16 = l % 16, q4 = l / 16;
   for (int at = threadIdx.x / 16; at < 16 * blocks; at += 512 / 16) {
     const int n = at / blocks, b = at - n * blocks, c = threadIdx.x % 16;
     uint32_t q[2] = {0, 0};
     int e = 0;
-    if (n < m) block_codes(H + n * ldh, b * kBlock + 8 * c, d, q, e);
+    if (n < m) rows.block(n, b, c, q, e);
     *reinterpret_cast<bf16x8*>(few_lds + b * kTile + fragment_at(n, c)) =
         widen(uintx2{q[0], q[1]}, scale_value(e));
   }
@@ -313,6 +291,50 @@ constexpr int64_t kMostBlocks = (1 << 28) - 16;  // of a matrix: 2^32 threads
 
 int64_t blocks_of(int32_t cols) { return ((int64_t)cols + kBlock - 1) / kBlock; }
 
+template <class R>
+int scores(const R& rows, int32_t out_dtype, int32_t m, int64_t D, int32_t d,
+           const uint8_t* codes, const uint8_t* scales, void* O, int64_t ldo, void* workspace,
+           hipStream_t s) {
+  if (!known_dtype(out_dtype) || m < 0 || D < 1 || d < 1 || d > 4096) return LST_EINVAL;
+  if (m == 0) return LST_OK;
+  if (!codes || !scales || !O || !workspace || ldo < D) return LST_EINVAL;
+  if (((uintptr_t)codes & 15) || ((uintptr_t)workspace & 15)) return LST_EINVAL;
+  if (m > 1 << 20 || D > (int64_t)1 << 36) return LST_EINVAL;
+  const int blocks = (int)blocks_of(d), tiles = (m + 15) / 16;
+  if (m <= kFew && blocks <= kFewColumns / kBlock)
+    return with_dtype(out_dtype, [&](auto t) {
+      using T = decltype(t);
+      const int64_t groups = (D + 127) / 128;
+      const size_t lds = (size_t)blocks * kTile * sizeof(__bf16);
+      hipLaunchKernelGGL((scores_few_kernel<R, T>),
+                         dim3((unsigned)std::min<int64_t>(groups, kFewBlocks)), dim3(512), lds, s,
+                         rows, codes, scales, m, D, blocks, (T*)O, ldo);
+      return launched();
+    });
+  // 256 rows of W and up to 8 tiles of H a block; no more than there are: 32 rows of H by
+  // 200 000 x 512 codes take 37 us with 2 tiles and 47 with 8, 64 take 44 with 4 and 52 with 8
+  const int nt = tiles <= 2 ? 2 : tiles <= 4 ? 4 : 8;
+  const int64_t row_blocks = (D + 255) / 256;
+  const int64_t grid = (row_blocks + 7) / 8 * 8 * ((tiles + nt - 1) / nt);
+  if (grid > 0xFFFFFF) return LST_EINVAL;  // a launch has 2^32 threads at most
+  __bf16* fragments = (__bf16*)workspace;
+  hipLaunchKernelGGL(fragments_kernel<R>, dim3(tiles * blocks), dim3(256), 0, s, rows, m, blocks,
+                     tiles, fragments);
+  const int rc = launched();
+  if (rc != LST_OK) return rc;
+  return with_dtype(out_dtype, [&](auto t) {
+    using T = decltype(t);
+    auto run = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, s, codes, scales, fragments,
+                         m, D, blocks, (int)row_blocks, (T*)O, ldo);
+      return launched();
+    };
+    if (nt == 2) return run(scores_kernel<T, 4, 2, true>);
+    if (nt == 4) return run(scores_kernel<T, 4, 4, true>);
+    return tiles <= 8 ? run(scores_kernel<T, 4, 8, true>) : run(scores_kernel<T, 4, 8, false>);
+  });
+}
+
 }  // namespace
 }  // namespace lst
 
@@ -344,52 +366,21 @@ int64_t lst_scores_workspace(int32_t m, int32_t d) {
 int lst_scores(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int32_t d, const void* H,
                int64_t ldh, const uint8_t* codes, const uint8_t* scales, void* O, int64_t ldo,
                void* workspace, void* hip_stream) {
-  if (!known_dtype(dtype) || !known_dtype(out_dtype) || m < 0 || D < 1 || d < 1 || d > 4096)
-    return LST_EINVAL;
-  if (m == 0) return LST_OK;
-  if (!H || !codes || !scales || !O || !workspace || ldh < d || ldo < D) return LST_EINVAL;
-  if (((uintptr_t)codes & 15) || ((uintptr_t)workspace & 15)) return LST_EINVAL;
-  if (m > 1 << 20 || D > (int64_t)1 << 36) return LST_EINVAL;
-  hipStream_t s = (hipStream_t)hip_stream;
-  const int blocks = (int)blocks_of(d), tiles = (m + 15) / 16;
-  if (m <= kFew && blocks <= kFewColumns / kBlock)
-    return with_dtype(dtype, [&](auto th) {
-      return with_dtype(out_dtype, [&](auto t) {
-        using TH = decltype(th);
-        using T = decltype(t);
-        const int64_t groups = (D + 127) / 128;
-        const size_t lds = (size_t)blocks * kTile * sizeof(__bf16);
-        hipLaunchKernelGGL((scores_few_kernel<TH, T>),
-                           dim3((unsigned)std::min<int64_t>(groups, kFewBlocks)), dim3(512), lds,
-                           s, (const TH*)H, ldh, d, codes, scales, m, D, blocks, (T*)O, ldo);
-        return launched();
-      });
-    });
-  // 256 rows of W and up to 8 tiles of H a block; no more than there are: 32 rows of H by
-  // 200 000 x 512 codes take 37 us with 2 tiles and 47 with 8, 64 take 44 with 4 and 52 with 8
-  const int nt = tiles <= 2 ? 2 : tiles <= 4 ? 4 : 8;
-  const int64_t row_blocks = (D + 255) / 256;
-  const int64_t grid = (row_blocks + 7) / 8 * 8 * ((tiles + nt - 1) / nt);
-  if (grid > 0xFFFFFF) return LST_EINVAL;  // a launch has 2^32 threads at most
-  __bf16* fragments = (__bf16*)workspace;
-  int rc = with_dtype(dtype, [&](auto t) {
+  if (!known_dtype(dtype)) return LST_EINVAL;
+  if (m > 0 && (!H || ldh < d)) return LST_EINVAL;
+  return with_dtype(dtype, [&](auto t) {
     using T = decltype(t);
-    hipLaunchKernelGGL(fragments_kernel<T>, dim3(tiles * blocks), dim3(256), 0, s, (const T*)H,
-                       ldh, m, d, blocks, tiles, fragments);
-    return launched();
+    return scores(Values<T>{(const T*)H, ldh, d}, out_dtype, m, D, d, codes, scales, O, ldo,
+                  workspace, (hipStream_t)hip_stream);
   });
-  if (rc != LST_OK) return rc;
-  return with_dtype(out_dtype, [&](auto t) {
-    using T = decltype(t);
-    auto run = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, s, codes, scales, fragments,
-                         m, D, blocks, (int)row_blocks, (T*)O, ldo);
-      return launched();
-    };
-    if (nt == 2) return run(scores_kernel<T, 4, 2, true>);
-    if (nt == 4) return run(scores_kernel<T, 4, 4, true>);
-    return tiles <= 8 ? run(scores_kernel<T, 4, 8, true>) : run(scores_kernel<T, 4, 8, false>);
-  });
+}
+
+int lst_scores_coded(int32_t out_dtype, int32_t m, int64_t D, int32_t d, const uint8_t* h_codes,
+                     const uint8_t* h_scales, const uint8_t* codes, const uint8_t* scales, void* O,
+                     int64_t ldo, void* workspace, void* hip_stream) {
+  if (m > 0 && (!h_codes || !h_scales || ((uintptr_t)h_codes & 15))) return LST_EINVAL;
+  return scores(Coded{h_codes, h_scales, (int)blocks_of(d)}, out_dtype, m, D, d, codes, scales, O,
+                ldo, workspace, (hipStream_t)hip_stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,367 @@
+// Weights in 4 bits (lst_quantize_four) and a layer's outputs from them (lst_scores_four).
+//
+// A row is cut into blocks of 32 columns.  A block holds e2m1 codes q (0, 1/2, 1, 3/2, 2, 3, 4, 6
+// and a sign), two a byte with the lower column in the lower half, and one exponent e with 6 2^e
+// the smallest such bound on the block's values.  The rows of H are quantised in the same way in
+// each call:
+//
+//   O[i][r] = sum_b 2^(e_ib + e_rb) sum_{k in b} qh_ik qw_rk
+//
+// The scaled matrix instruction takes both sides as they are held: lane (n, q) of 16 x 4 gives
+// the 32 columns of one block, 16 bytes, and its exponent.  Its sums of 4-bit products are those
+// of float32 (measured: a product of 1/4 beside one of 36 2^40 or beside an accumulator of that
+// size is rounded as float32 rounds it, where sums of 8-bit products lose what is 2^-14 of the
+// largest), and it has four times the rate of the bfloat16 instruction.
+#include <algorithm>
+
+#include "eight_bit.h"
+#include "gemm_tile.h"
+
+namespace lst {
+namespace {
+
+constexpr int kSmall = 32;         // columns that share a scale
+constexpr int kStep = 128;         // columns of one matrix instruction
+constexpr int kPiece = 64 * 16;    // bytes of its operand: 16 rows
+constexpr int kGroup = 4;          // steps whose scales share a word, and a stage of LDS
+
+typedef int int32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Biased exponent of the scale for the bits of a block's largest magnitude: 6 = 1.5 2^2, so
+// 1.f 2^E needs 2^(E - 2) when 1.f <= 1.5, else 2^(E - 1).
+__device__ inline int small_scale_of(uint32_t big) {
+  const int e = (int)(big >> 23) - ((big & 0x7FFFFF) <= 0x400000 ? 2 : 1);
+  return max(e, 0);
+}
+
+// Codes of eight columns, a block being in four neighbouring lanes, and the block's biased
+// exponent.  The type has no code that is no number: a block with a value that is not finite
+// gets the exponent 255, which makes all of it no number, and codes of zero for such values.
+__device__ inline uint32_t small_codes(float (&v)[8], int& e) {
+  uint32_t bad, big = largest_finite(v, bad);
+  int worst = bad != 0;
+#pragma unroll
+  for (int o = 2; o; o >>= 1) {
+    big = max(big, (uint32_t)__shfl_xor((int)big, o));
+    worst |= __shfl_xor(worst, o);
+  }
+  e = small_scale_of(big);
+  const float s = __uint_as_float((uint32_t)(254 - e) << 23);  // exact: e is at most 253
+  uint32_t q = 0;
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[0] * s, v[1] * s, 1.f, 0);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[2] * s, v[3] * s, 1.f, 1);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[4] * s, v[5] * s, 1.f, 2);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, v[6] * s, v[7] * s, 1.f, 3);
+  if (worst) e = 255;
+  return q;
+}
+
+template <class T>
+__device__ inline uint32_t row_codes(const T* row, int col, int cols, int& e) {
+  T raw[8];
+  load_part(row, col, cols, raw);
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)raw[i];
+  return small_codes(v, e);
+}
+
+// Four lanes a block, eight columns a lane.
+template <class T>
+__global__ __launch_bounds__(256) void quantize_kernel(const T* x, int64_t ldx, int64_t rows,
+                                                       int cols, int blocks, uint32_t* codes,
+                                                       uint8_t* scales) {
+  const unsigned at = blockIdx.x * 64 + threadIdx.x / 4;  // the block
+  if (at >= (unsigned)(rows * blocks)) return;
+  const unsigned row = at / (unsigned)blocks;
+  const int l = threadIdx.x % 4, col = (int)(at - row * (unsigned)blocks) * kSmall + 8 * l;
+  int e;
+  const uint32_t q = row_codes(x + (int64_t)row * ldx, col, cols, e);
+  codes[(int64_t)at * 4 + l] = q;
+  if (l == 0) scales[at] = (uint8_t)e;
+}
+
+// Rows of H into operands: piece (step, tile of 16 rows), and behind the pieces the exponents of
+// four steps a word, for each lane of a tile.  Rows behind the last one of the last tile and
+// blocks behind a row's last are zeros.
+template <class T>
+__global__ __launch_bounds__(256) void operands_kernel(const T* x, int64_t ldx, int m, int cols,
+                                                       int blocks, int steps, int tiles,
+                                                       uint32_t* out, uint8_t* scales) {
+  const int at = blockIdx.x * 64 + threadIdx.x / 4;
+  if (at >= tiles * 16 * steps * 4) return;
+  const int n = at / (steps * 4), b = at - n * (steps * 4), l = threadIdx.x % 4;
+  const int step = b / 4, lane = b % 4 * 16 + n % 16, tile = n / 16;
+  uint32_t q = 0;
+  int e = 127;
+  if (n < m && b < blocks) q = row_codes(x + (int64_t)n * ldx, b * kSmall + 8 * l, cols, e);
+  out[((int64_t)step * tiles + tile) * (kPiece / 4) + lane * 4 + l] = q;
+  if (l == 0)
+    scales[(((int64_t)(step / kGroup) * tiles + tile) * 64 + lane) * kGroup + step % kGroup] =
+        (uint8_t)e;
+}
+
+__device__ inline int32x8 operand(uintx4 q) {
+  return int32x8{(int)q[0], (int)q[1], (int)q[2], (int)q[3], 0, 0, 0, 0};
+}
+
+template <int BYTE>  // of sb
+__device__ inline f32x4 multiply(uintx4 a, int sa, uintx4 b, int sb, f32x4 c) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(a), operand(b), c, 4, 4, 0, sa,
+                                                          BYTE, sb);
+}
+
+// What a lane gives to one step of a tile of W.  Blocks behind a row's last one are read as the
+// last one: the other side is zero there.
+struct Weights {
+  uintx4 q;
+  int e;
+  template <bool ONCE>
+  __device__ void load(const uint8_t* w, const uint8_t* scale, int block, int blocks) {
+    const int b = min(block, blocks - 1);
+    const uintx4* p = reinterpret_cast<const uintx4*>(w + b * 16);
+    q = ONCE ? __builtin_nontemporal_load(p) : *p;
+    e = scale[b];
+  }
+};
+
+template <class T, int N>
+__device__ inline void store_rows(T* O, int64_t ldo, int m, int64_t D, int n, int64_t r,
+                                  const float (&acc)[N]) {
+  if (n >= m || r >= D) return;
+  T* o = O + n * ldo + r;
+  T v[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = (T)acc[i];
+  if (r + N <= D) {
+    store_vec(o, v);
+  } else {
+    for (int i = 0; i < N; ++i)
+      if (r + i < D) o[i] = v[i];
+  }
+}
+
+// At most 16 rows of H: one launch.  Every block quantises them by itself, into LDS, and its
+// waves go through tiles of 16 rows of W, four steps' codes under way at a time.
+template <class TH, class T>
+__global__ __launch_bounds__(512) void few_kernel(const TH* H, int64_t ldh, int d,
+                                                  const uint8_t* W, const uint8_t* sw, int m,
+                                                  int64_t D, int blocks, int steps, T* O,
+                                                  int64_t ldo) {
+  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
+  int* exponents = (int*)(lds + steps * (kPiece / 4));
+  for (int at = threadIdx.x / 4; at < 16 * 4 * steps; at += 512 / 4) {
+    const int n = at / (4 * steps), b = at - n * (4 * steps), c = threadIdx.x % 4;
+    uint32_t q = 0;
+    int e = 127;
+    if (n < m && b < blocks) q = row_codes(H + n * ldh, b * kSmall + 8 * c, d, e);
+    const int lane = b / 4 * 64 + b % 4 * 16 + n;
+    lds[lane * 4 + c] = q;
+    if (c == 0) exponents[lane] = e;
+  }
+  __syncthreads();
+  const int l = threadIdx.x % 64, i16 = l % 16, q4 = l / 16;
+  const uintx4* operands = reinterpret_cast<const uintx4*>(lds);
+  const int64_t ld = (int64_t)blocks * 16, tiles = (D + 15) / 16;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  for (int64_t tile = (int64_t)blockIdx.x * 8 + w; tile < tiles; tile += (int64_t)gridDim.x * 8) {
+    const int64_t row = min(tile * 16 + i16, D - 1);
+    const uint8_t *p = W + row * ld, *ps = sw + row * blocks;
+    f32x4 acc = {};
+    for (int s0 = 0; s0 < steps; s0 += 4) {
+      Weights c[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c[j].load<false>(p, ps, (s0 + j) * 4 + q4, blocks);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (s0 + j < steps)
+          acc = multiply<0>(c[j].q, c[j].e, operands[(s0 + j) * 64 + l],
+                            exponents[(s0 + j) * 64 + l], acc);
+    }
+    const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
+    store_rows(O, ldo, m, D, i16, tile * 16 + 4 * q4, v);
+  }
+}
+
+// 16 MT rows of W a wave, four waves a block one after another, 16 NT rows of H a block.  Four
+// steps of H's operands go to LDS by DMA while the four before are multiplied; the codes of a
+// wave's own rows go to registers, two steps ahead.
+template <class T, int MT, int NT, bool ONCE>
+__global__ __launch_bounds__(256, 2) void scores_kernel(const uint8_t* W, const uint8_t* sw,
+                                                        const uint8_t* H, const int* sh, int m,
+                                                        int64_t D, int blocks, int steps,
+                                                        int row_blocks, T* O, int64_t ldo) {
+  __shared__ __attribute__((aligned(16))) uint8_t hb[2][kGroup * NT * kPiece];
+  const int l = threadIdx.x % 64, i16 = l % 16, q4 = l / 16;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  // the blocks of the same rows of W follow each other on one XCD, and share its L2
+  const int tiles = (m + 15) / 16, cols = (tiles + NT - 1) / NT;
+  const int xcd = blockIdx.x % 8, i = blockIdx.x / 8;
+  const int row_block = i / cols * 8 + xcd, t0 = i % cols * NT;
+  if (row_block >= row_blocks) return;
+  const int64_t r0 = ((int64_t)row_block * 4 + w) * 16 * MT, ld = (int64_t)blocks * 16;
+  // 16-bit outputs: rows of W are dealt to pairs of tiles in fours, so that a lane holds eight
+  // neighbouring outputs and four lanes 64 bytes of a row of O
+  constexpr bool kPairs = sizeof(T) == 2 && MT % 2 == 0;
+  const uint8_t *p[MT], *ps[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int at = kPairs ? t / 2 * 32 + i16 / 4 * 8 + t % 2 * 4 + i16 % 4 : 16 * t + i16;
+    const int64_t row = min(r0 + at, D - 1);
+    p[t] = W + row * ld;
+    ps[t] = sw + row * blocks;
+  }
+  auto fetch = [&](int g) {  // NT pieces for each step of the group, a quarter of them a wave
+#pragma unroll
+    for (int k = 0; k < NT; ++k) {
+      const int piece = w * NT + k, step = g * kGroup + piece / NT, t = t0 + piece % NT;
+      dma16((const float*)(H + ((int64_t)min(step, steps - 1) * tiles + min(t, tiles - 1)) * kPiece +
+                           l * 16),
+            lds_u32(&hb[g % 2][piece * kPiece]));
+    }
+  };
+  f32x4 acc[MT][NT] = {};
+  Weights c[kGroup][MT];
+  int e[NT];
+  auto load = [&](int slot, int step) {
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+      c[slot][t].template load<ONCE>(p[t], ps[t], min(step, steps - 1) * 4 + q4, blocks);
+  };
+  fetch(0);
+  load(0, 0);
+  load(1, 1);
+  const int groups = (steps + kGroup - 1) / kGroup;
+  for (int g = 0; g < groups; ++g) {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+      e[n] = sh[((int64_t)g * tiles + min(t0 + n, tiles - 1)) * 64 + l];
+    wait_vm_le(0);
+    lds_barrier();  // group g has landed; every wave is done with the one before
+    if (g + 1 < groups) fetch(g + 1);
+    const uintx4* h = reinterpret_cast<const uintx4*>(hb[g % 2]);
+    auto run = [&](auto byte) {
+      constexpr int s = byte;
+      if (g * kGroup + s >= steps) return;
+      load((s + 2) % kGroup, g * kGroup + s + 2);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const uintx4 b = h[(s * NT + n) * 64 + l];
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+          acc[t][n] = multiply<s>(c[s][t].q, c[s][t].e, b, e[n], acc[t][n]);
+      }
+    };
+    run(std::integral_constant<int, 0>{});
+    run(std::integral_constant<int, 1>{});
+    run(std::integral_constant<int, 2>{});
+    run(std::integral_constant<int, 3>{});
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int t = 0; t < MT; t += kPairs ? 2 : 1) {
+      const int row = (t0 + n) * 16 + i16;
+      if constexpr (kPairs) {
+        const f32x4 a = acc[t][n], b = acc[t + 1][n];
+        const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        store_rows(O, ldo, m, D, row, r0 + 16 * t + 8 * q4, v);
+      } else {
+        const f32x4 a = acc[t][n];
+        const float v[4] = {a[0], a[1], a[2], a[3]};
+        store_rows(O, ldo, m, D, row, r0 + 16 * t + 4 * q4, v);
+      }
+    }
+}
+
+constexpr int kFew = 16;         // rows of H that one launch takes
+constexpr int kFewBlocks = 512;  // blocks of that launch, two a compute unit
+constexpr int64_t kMostBlocks = (1 << 30) - 64;  // of a matrix: 2^32 threads
+
+int64_t blocks_of(int32_t cols) { return ((int64_t)cols + kSmall - 1) / kSmall; }
+int64_t steps_of(int32_t cols) { return ((int64_t)cols + kStep - 1) / kStep; }
+int64_t pieces_bytes(int32_t m, int32_t d) {
+  return ((int64_t)m + 15) / 16 * steps_of(d) * kPiece;
+}
+
+}  // namespace
+}  // namespace lst
+
+using namespace lst;
+
+extern "C" {
+
+int lst_quantize_four(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t ldx,
+                      uint8_t* codes, uint8_t* scales, void* hip_stream) {
+  if (!known_dtype(dtype) || rows < 0 || cols < 1 || cols > 4096) return LST_EINVAL;
+  if (rows == 0) return LST_OK;
+  if (!x || !codes || !scales || ldx < cols || ((uintptr_t)codes & 15)) return LST_EINVAL;
+  if (rows > kMostBlocks / blocks_of(cols)) return LST_EINVAL;
+  const int64_t n = (rows * blocks_of(cols) + 63) / 64;
+  return with_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    hipLaunchKernelGGL(quantize_kernel<T>, dim3((unsigned)n), dim3(256), 0,
+                       (hipStream_t)hip_stream, (const T*)x, ldx, rows, cols,
+                       (int)blocks_of(cols), (uint32_t*)codes, scales);
+    return launched();
+  });
+}
+
+int64_t lst_scores_four_workspace(int32_t m, int32_t d) {
+  if (m < 0 || d < 1 || d > 4096) return -1;
+  const int64_t groups = (steps_of(d) + kGroup - 1) / kGroup;
+  return pieces_bytes(m, d) + ((int64_t)m + 15) / 16 * groups * 64 * kGroup;
+}
+
+int lst_scores_four(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int32_t d,
+                    const void* H, int64_t ldh, const uint8_t* codes, const uint8_t* scales,
+                    void* O, int64_t ldo, void* workspace, void* hip_stream) {
+  if (!known_dtype(dtype) || !known_dtype(out_dtype) || m < 0 || D < 1 || d < 1 || d > 4096)
+    return LST_EINVAL;
+  if (m == 0) return LST_OK;
+  if (!H || !codes || !scales || !O || !workspace || ldh < d || ldo < D) return LST_EINVAL;
+  if (((uintptr_t)codes & 15) || ((uintptr_t)workspace & 15)) return LST_EINVAL;
+  if (m > 1 << 20 || D > (int64_t)1 << 36) return LST_EINVAL;
+  hipStream_t s = (hipStream_t)hip_stream;
+  const int blocks = (int)blocks_of(d), steps = (int)steps_of(d), tiles = (m + 15) / 16;
+  if (m <= kFew)
+    return with_dtype(dtype, [&](auto th) {
+      return with_dtype(out_dtype, [&](auto t) {
+        using TH = decltype(th);
+        using T = decltype(t);
+        const int64_t groups = (D + 127) / 128;
+        const size_t lds = (size_t)steps * (kPiece + 64 * sizeof(int));
+        hipLaunchKernelGGL((few_kernel<TH, T>),
+                           dim3((unsigned)std::min<int64_t>(groups, kFewBlocks)), dim3(512), lds,
+                           s, (const TH*)H, ldh, d, codes, scales, m, D, blocks, steps, (T*)O,
+                           ldo);
+        return launched();
+      });
+    });
+  const int nt = tiles <= 2 ? 2 : tiles <= 4 ? 4 : 8;
+  const int64_t row_blocks = (D + 255) / 256;
+  const int64_t grid = (row_blocks + 7) / 8 * 8 * ((tiles + nt - 1) / nt);
+  if (grid > 0xFFFFFF) return LST_EINVAL;  // a launch has 2^32 threads at most
+  uint8_t *pieces = (uint8_t*)workspace, *exponents = pieces + pieces_bytes(m, d);
+  const int rc = with_dtype(dtype, [&](auto t) {
+    using T = decltype(t);
+    hipLaunchKernelGGL(operands_kernel<T>, dim3(tiles * steps), dim3(256), 0, s, (const T*)H, ldh,
+                       m, d, blocks, steps, tiles, (uint32_t*)pieces, exponents);
+    return launched();
+  });
+  if (rc != LST_OK) return rc;
+  return with_dtype(out_dtype, [&](auto t) {
+    using T = decltype(t);
+    auto run = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), 0, s, codes, scales, pieces,
+                         (const int*)exponents, m, D, blocks, steps, (int)row_blocks, (T*)O, ldo);
+      return launched();
+    };
+    if (nt == 2) return run(scores_kernel<T, 4, 2, true>);
+    if (nt == 4) return run(scores_kernel<T, 4, 4, true>);
+    return tiles <= 8 ? run(scores_kernel<T, 4, 8, true>) : run(scores_kernel<T, 4, 8, false>);
+  });
+}
+
+}  // extern "C"
