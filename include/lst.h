@@ -627,6 +627,45 @@ int lst_sample(int32_t dtype, int32_t m, int32_t D, const void* logits, int64_t 
                void* hip_stream);
 int64_t lst_sample_workspace(int32_t m, int32_t D); /* bytes; -1 for a bad size */
 
+/*
+ * lst_logprobs -- log probabilities of given tokens, the entropy and the likeliest tokens of rows
+ * of outputs.  With p_j = exp((x_j - max) / temperature), divided by the sum of these over the
+ * row:
+ *   logits            m x D, 1 <= D <= 2^30.  Entries that are -inf or no number have no
+ *                     probability (log p = -inf); where some are +inf, those share all of it.
+ *   temperature (device) m values, or NULL for 1.  Above zero and finite.
+ *   tokens (device)   m x K ints, 0 <= K <= 1024: -1 is unused.  An index outside [-1, D) sets the
+ *                     status LST_EINDEX and counts as unused.
+ *   logp   (device)   m x K floats: log p of each token, 0 for an unused one.
+ *   entropy (device)  m floats, or NULL: - sum p log p.
+ *   top, top_ids, top_logp (device)  0 <= top <= 64; m x top ints and floats: the likeliest
+ *                     tokens, equal ones by index, and their log p; -1 and -inf where a row has
+ *                     no more.
+ *   saved  (device)   receives what lst_logprobs_backward needs, lst_logprobs_saved(m, K) floats;
+ *                     NULL when there will be no backward pass.
+ * A row without an entry that has a probability, or with a bad temperature, has log p = -inf for
+ * every used token, entropy 0, no likeliest tokens and a gradient of zeros.  All sums are float32.
+ */
+int lst_logprobs(int32_t dtype, int32_t m, int32_t D, int32_t K, int32_t top, const void* logits,
+                 int64_t ldx, const float* temperature, const int32_t* tokens, float* logp,
+                 float* entropy, int32_t* top_ids, float* top_logp, float* saved, void* workspace,
+                 int32_t* status, void* hip_stream);
+
+/*
+ * lst_logprobs_backward -- the gradient with respect to the logits of what lst_logprobs gave:
+ * grad_logp (m x K floats) and grad_entropy (m floats, or NULL) are dL/dlogp and dL/dentropy.
+ * logits, temperature and tokens as there, saved from that call.  grad_logits (m x D of the
+ * logits' type) may be the logits, with their row stride.  An unused token, and one whose log p is
+ * -inf, has no gradient; neither have the likeliest tokens' log p.  A token that a row names
+ * several times adds all of them, in order.
+ */
+int lst_logprobs_backward(int32_t dtype, int32_t m, int32_t D, int32_t K, const void* logits,
+                          int64_t ldx, const float* temperature, const int32_t* tokens,
+                          const float* saved, const float* grad_logp, const float* grad_entropy,
+                          void* grad_logits, int64_t ldg, void* hip_stream);
+int64_t lst_logprobs_saved(int32_t m, int32_t K); /* floats; -1 for a bad size */
+int64_t lst_logprobs_workspace(int32_t m, int32_t D, int32_t top); /* bytes; -1 for a bad size */
+
 /* lst_strerror -- static description of a status code. */
 const char* lst_strerror(int status);
 

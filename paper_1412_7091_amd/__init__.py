@@ -171,6 +171,12 @@ _SIGS = {
     "lst_sample": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _P,
                                   ctypes.c_int64, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
     "lst_sample_workspace": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32]),
+    "lst_logprobs": (ctypes.c_int, [ctypes.c_int32] * 5 + [
+        _P, ctypes.c_int64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "lst_logprobs_backward": (ctypes.c_int, [ctypes.c_int32] * 4 + [
+        _P, ctypes.c_int64, _P, _P, _P, _P, _P, _P, ctypes.c_int64, _P]),
+    "lst_logprobs_saved": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32]),
+    "lst_logprobs_workspace": (ctypes.c_int64, [ctypes.c_int32] * 3),
     "lst_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "lst_free": (None, [_P]),
 }
@@ -834,6 +840,76 @@ def lst_sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=Non
     return tokens, prob
 
 
+@functools.lru_cache(maxsize=256)
+def lst_logprobs_workspace(m: int, D: int, top: int) -> int:
+    return int(load_library().lst_logprobs_workspace(m, D, top))
+
+
+@functools.lru_cache(maxsize=256)
+def lst_logprobs_saved(m: int, K: int) -> int:
+    return int(load_library().lst_logprobs_saved(m, K))
+
+
+def _tokens(tokens, m, dev):
+    """(address, K) of m rows of tokens, or of a vector with one a row."""
+    import torch
+
+    if tokens is None:
+        return None, 0
+    if tokens.dim() not in (1, 2) or tokens.shape[0] != m:
+        raise ValueError("tokens must have a row, or an element, for each row of logits")
+    return _vector(tokens, torch.int32, "tokens", dev), 1 if tokens.dim() == 1 else tokens.shape[1]
+
+
+def lst_logprobs(logits, tokens=None, *, top=0, temperature=None, save=False, status=None):
+    """(logp, entropy, top_ids, top_logp, saved): log probabilities of the given tokens ((m, K) or
+    (m,); logp has their shape, None without tokens), the entropy of each row, its `top` likeliest
+    tokens and their log probabilities (None for top = 0), and what the backward pass needs (None
+    unless save)."""
+    import torch
+
+    px, ldx = _matrix(logits, "logits")
+    code = _dtype_code(logits, "logits")
+    (m, D), dev, f32, i32 = logits.shape, logits.device, torch.float32, torch.int32
+    pt, K = _tokens(tokens, m, dev)
+    top = int(top)
+    new = logits.new_empty
+    logp = None if tokens is None else new(tokens.shape, dtype=f32)
+    entropy = new(m, dtype=f32)
+    ids, best = (new((m, top), dtype=i32), new((m, top), dtype=f32)) if top > 0 else (None, None)
+    saved = new((m, K + 4), dtype=f32) if save else None
+    work = _work(logits, lst_logprobs_workspace(m, D, top))
+    _enqueue("lst_logprobs", dev, code, m, D, K, top, px, ldx,
+             _vector(temperature, f32, "temperature", dev, m), pt,
+             None if logp is None else logp.data_ptr(), entropy.data_ptr(),
+             None if ids is None else ids.data_ptr(), None if best is None else best.data_ptr(),
+             None if saved is None else saved.data_ptr(), None if work is None else work.data_ptr(),
+             _vector(status, i32, "status", dev, 1))
+    return logp, entropy, ids, best, saved
+
+
+def lst_logprobs_backward(logits, tokens, saved, grad_logp, grad_entropy=None, *, temperature=None,
+                          out=None):
+    """The gradient of the logits from those of logp and of the entropy; out may be the logits."""
+    import torch
+
+    px, ldx = _matrix(logits, "logits")
+    code = _dtype_code(logits, "logits")
+    (m, D), dev, f32 = logits.shape, logits.device, torch.float32
+    pt, K = _tokens(tokens, m, dev)
+    if out is None:
+        out = logits.new_empty((m, D))
+    if m and saved is None:
+        raise TypeError("saved must be what lst_logprobs left with save=True")
+    _enqueue("lst_logprobs_backward", dev, code, m, D, K, px, ldx,
+             _vector(temperature, f32, "temperature", dev, m), pt,
+             _vector(saved, f32, "saved", dev, m * (K + 4)),
+             _vector(grad_logp, f32, "grad_logp", dev, m * K),
+             _vector(grad_entropy, f32, "grad_entropy", dev, m),
+             *_matrix(out, "out", logits, logits.shape))
+    return out
+
+
 # ------------------------------------------------------------------- classes
 class _Layer:
     def __init__(self, handle, D: int, d: int, m_max: int, K_max: int, device):
@@ -1166,6 +1242,11 @@ class EightBitOutputLayer:
     def sample(self, H, u, **settings):
         """(tokens, prob) chosen from the outputs for H: lst_sample's settings."""
         return lst_sample(self.scores(H, dtype=settings.pop("dtype", None)), u, **settings)
+
+    def logprobs(self, H, tokens=None, **settings):
+        """Log probabilities of tokens, the entropy and the likeliest tokens of the outputs for H:
+        lst_logprobs' settings and results."""
+        return lst_logprobs(self.scores(H, dtype=settings.pop("dtype", None)), tokens, **settings)
 
 
 class FourBitOutputLayer(EightBitOutputLayer):
