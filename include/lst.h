@@ -666,6 +666,32 @@ int lst_logprobs_backward(int32_t dtype, int32_t m, int32_t D, int32_t K, const 
 int64_t lst_logprobs_saved(int32_t m, int32_t K); /* floats; -1 for a bad size */
 int64_t lst_logprobs_workspace(int32_t m, int32_t D, int32_t top); /* bytes; -1 for a bad size */
 
+/*
+ * lst_clip -- the norm over all gradients of a step, and the gradients scaled to a largest one:
+ * n = sqrt(the sum of the squares of all elements), every element times min(1, max_norm / n).
+ *   grads   (host)    n matrices, 0 <= n <= 65 536, of types of their own, 2^40 elements
+ *                     together at most; read before the call returns.
+ *   max_norm          at least 0; infinite: nothing is scaled.
+ *   norm   (device)   a float, receives n (of the gradients as they came).
+ * A matrix that is written shares memory with no other of the call, data or out: the call refuses
+ * a list in which one does, the same matrix twice among them (columns of one wider matrix are
+ * apart).  When n is not finite nothing is scaled, and the status is set to LST_ENONFINITE.
+ * The squares are summed in 64 bits, in an order that does not depend on timing.
+ */
+typedef struct lst_gradient {
+  const void* data;        /* rows x cols (device)                                          */
+  void* out;               /* receives the scaled matrix; NULL or data: in place, where a
+                              factor of 1 writes nothing                                     */
+  int64_t rows, cols;      /* either may be 0                                                */
+  int64_t ld, ldo;         /* row strides of data and out, in elements (in place: ldo is not
+                              read for NULL, and is ld for data)                             */
+  int32_t dtype;           /* of both                                                        */
+} lst_gradient;
+
+int lst_clip(int32_t n, const lst_gradient* grads, double max_norm, float* norm, void* workspace,
+             int32_t* status, void* hip_stream);
+int64_t lst_clip_workspace(int32_t n); /* bytes; -1 for a bad size */
+
 /* lst_strerror -- static description of a status code. */
 const char* lst_strerror(int status);
 

@@ -86,6 +86,18 @@ class lst_stab_report(ctypes.Structure):
     ]
 
 
+class lst_gradient(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("ld", ctypes.c_int64),
+        ("ldo", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+    ]
+
+
 class LstError(RuntimeError):
     def __init__(self, code: int, what: str = ""):
         self.code = code
@@ -177,6 +189,9 @@ _SIGS = {
         _P, ctypes.c_int64, _P, _P, _P, _P, _P, _P, ctypes.c_int64, _P]),
     "lst_logprobs_saved": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32]),
     "lst_logprobs_workspace": (ctypes.c_int64, [ctypes.c_int32] * 3),
+    "lst_clip": (ctypes.c_int, [ctypes.c_int32, ctypes.POINTER(lst_gradient), ctypes.c_double, _P,
+                                _P, _P, _P]),
+    "lst_clip_workspace": (ctypes.c_int64, [ctypes.c_int32]),
     "lst_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "lst_free": (None, [_P]),
 }
@@ -910,6 +925,60 @@ def lst_logprobs_backward(logits, tokens, saved, grad_logp, grad_entropy=None, *
     return out
 
 
+def _gradients(tensors, out):
+    """(device, table) of a list of device tensors: matrices with unit stride along their rows, or
+    contiguous tensors of any other number of dimensions."""
+    tensors = list(tensors)
+    out = list(out) if out is not None else [None] * len(tensors)
+    if not tensors or len(out) != len(tensors):
+        raise ValueError("there must be a tensor, and as many outputs as tensors")
+    table, dev = (lst_gradient * len(tensors))(), tensors[0].device
+    for t, o, g in zip(tensors, out, table):
+        if t.device != dev:
+            raise TypeError(f"all tensors must be on {dev}")
+        g.dtype = _dtype_code(t, "a gradient")
+        if o is not None and (o.dtype != t.dtype or o.device != dev or o.shape != t.shape):
+            raise TypeError("an output must be like its gradient")
+        for k, m in enumerate((t, o)):
+            if m is None:
+                continue
+            if m.dim() != 2:
+                if not m.is_cuda or not m.is_contiguous():
+                    raise TypeError("a gradient must be a matrix, or contiguous, on the device")
+                ptr, ld, shape = m.data_ptr(), m.numel(), (1, m.numel())
+            else:
+                (ptr, ld), shape = _matrix(m, "a gradient"), m.shape
+            if k == 0:
+                g.data, g.ld, (g.rows, g.cols) = ptr, ld, shape
+            else:
+                g.out, g.ldo = ptr, ld
+    return dev, table
+
+
+def _clip(dev, table, max_norm, norm, status):
+    import torch
+
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device=dev)
+    n = len(table)
+    work = torch.empty(lst_clip_workspace(n), dtype=torch.uint8, device=dev)
+    _enqueue("lst_clip", dev, n, table, float(max_norm),
+             _vector(norm, torch.float32, "norm", dev, 1), work.data_ptr(),
+             _vector(status, torch.int32, "status", dev, 1))
+    return norm
+
+
+@functools.lru_cache(maxsize=256)
+def lst_clip_workspace(n: int) -> int:
+    return int(load_library().lst_clip_workspace(n))
+
+
+def lst_clip(tensors, max_norm, *, out=None, norm=None, status=None):
+    """The norm over all tensors (a device tensor with one element), which are scaled to max_norm
+    where it is larger: in place, or into the tensors of out."""
+    return _clip(*_gradients(tensors, out), max_norm, norm, status)
+
+
 # ------------------------------------------------------------------- classes
 class _Layer:
     def __init__(self, handle, D: int, d: int, m_max: int, K_max: int, device):
@@ -1189,6 +1258,34 @@ class RMSNorm:
         """(grad_x, grad_weight); grad_x is the gradient of x and of the residual."""
         return lst_norm_backward(s, rstd, self.weight, grad_y, grad_sum, out=out,
                                  grad_weight=grad_weight)
+
+
+class GradientClip:
+    """The norm over the gradients of a step, and those scaled to a largest norm, for a program
+    whose gradients keep their memory from step to step: the list is checked once, and the object
+    keeps the tensors.  Scales in place, or into the tensors of out."""
+
+    def __init__(self, tensors, out=None):
+        import torch
+
+        load_library()
+        self._tensors = list(tensors), None if out is None else list(out)
+        self._device, self._table = _gradients(*self._tensors)
+        self._status = torch.zeros(1, dtype=torch.int32, device=self._device)
+
+    def clip(self, max_norm, *, norm=None):
+        """The norm before scaling, a device tensor with one element."""
+        return _clip(self._device, self._table, max_norm, norm, self._status)
+
+    def sync(self) -> int:
+        """Wait for the device; returns (and clears) the sticky status code."""
+        import torch
+
+        torch.cuda.synchronize(self._device)
+        code = int(self._status.item())
+        if code:
+            self._status.zero_()
+        return code
 
 
 class EightBitOutputLayer:

@@ -21,7 +21,7 @@ LIB = os.path.join(PKG, "liblst.so")
 SOURCES = ["gemm.hip", "step.hip", "small.hip", "stabilize.hip", "input_layer.hip", "online.hip",
            "lu.hip", "shifted.hip", "dropout.hip", "recur.hip",
            "eight_bit.hip", "sample.hip", "norm.hip", "four_bit.hip",
-           "logprobs.hip", "lst_api.hip"]
+           "logprobs.hip", "clip.hip", "lst_api.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

@@ -1,0 +1,324 @@
+// The norm over all gradients of a step, and the gradients scaled to a largest one (lst_clip).
+//
+//   n = sqrt(sum over all matrices of g^2),  g <- g min(1, max_norm / n)
+//
+// One pass for the squares, one that scales.  The squares are summed in float64: no value that a
+// type has overflows them, and millions of small ones are not lost beside a large one.  The
+// matrices' addresses and shapes travel as arguments of the launches, kTable of them at a time,
+// so nothing of the caller's host memory is read after the call.  Blocks take neighbouring tiles
+// of 8192 elements, through the matrices in the order of the list; each leaves its sum, and the
+// blocks of the second pass add these up by themselves, in the same order every time.
+#include <algorithm>
+#include <new>
+#include <vector>
+
+#include "dtypes.h"
+
+namespace lst {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kItems = 4;                        // groups of eight elements a thread and tile
+constexpr int64_t kGroups = kThreads * kItems;   // groups of a tile
+constexpr int kTable = 60;                       // matrices of a launch: 4 KB of arguments
+constexpr int kBlocks = 2048;                    // of a launch: eight a compute unit
+constexpr int kMost = 65536;
+
+struct Entry {
+  const void* data;
+  void* out;
+  int64_t rows, cols, ld, ldo, groups;  // groups: of a row
+  int32_t dtype;
+  uint32_t first;  // its first tile among those of the launch
+};
+
+struct Table {
+  Entry e[kTable];
+  int n;
+  uint32_t tiles, each;  // each: of a block
+};
+
+__device__ inline double block_sum(double v, double* lds) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
+  __syncthreads();
+  v = lds[0];
+#pragma unroll
+  for (int i = 1; i < kThreads / 64; ++i) v += lds[i];
+  return v;
+}
+
+// Where a group of a matrix is.
+struct Place {
+  int64_t row, col;
+  __device__ Place(const Entry& e, int64_t group) {
+    if (e.rows == 1) {
+      row = 0;
+      col = group * 8;
+    } else if (e.rows * e.groups <= 0x7FFFFFFF) {
+      const uint32_t r = (uint32_t)group / (uint32_t)e.groups;
+      row = r;
+      col = (int64_t)((uint32_t)group - r * (uint32_t)e.groups) * 8;
+    } else {
+      row = group / e.groups;
+      col = (group - row * e.groups) * 8;
+    }
+  }
+};
+
+// Eight elements, zeros behind the row's last.
+template <class T>
+__device__ inline void load_group(const Entry& e, int64_t group, T (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (T)0.f;
+  if (group >= e.rows * e.groups) return;
+  const Place at(e, group);
+  const T* p = (const T*)e.data + at.row * e.ld;
+  if (at.col + 8 <= e.cols) {
+    load_vec(p + at.col, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = p[min(at.col + i, e.cols - 1)];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = at.col + i < e.cols ? v[i] : (T)0.f;
+  }
+}
+
+template <class T>
+__device__ inline double tile_squares(const Entry& e, int64_t group) {
+  T v[kItems][8];
+#pragma unroll
+  for (int j = 0; j < kItems; ++j) load_group(e, group + j * kThreads, v[j]);
+  double sum = 0;
+#pragma unroll
+  for (int j = 0; j < kItems; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const double x = (float)v[j][i];
+      sum = fma(x, x, sum);
+    }
+  return sum;
+}
+
+template <class T>
+__device__ inline void scale_tile(const Entry& e, int64_t group, float factor) {
+  T v[kItems][8];
+#pragma unroll
+  for (int j = 0; j < kItems; ++j) load_group(e, group + j * kThreads, v[j]);
+#pragma unroll
+  for (int j = 0; j < kItems; ++j) {
+    const int64_t g = group + j * kThreads;
+    if (g >= e.rows * e.groups) return;
+    const Place at(e, g);
+    T* p = (T*)e.out + at.row * e.ldo + at.col;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[j][i] = (T)((float)v[j][i] * factor);
+    if (at.col + 8 <= e.cols) {
+      store_vec(p, v[j]);
+    } else {
+      for (int i = 0; i < 8; ++i)
+        if (at.col + i < e.cols) p[i] = v[j][i];
+    }
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void squares_kernel(Table t, double* partial) {
+  __shared__ double lds[kThreads / 64];
+  const uint32_t from = blockIdx.x * t.each, to = min(from + t.each, t.tiles);
+  double sum = 0;
+  int k = 0;
+  for (uint32_t tile = from; tile < to; ++tile) {
+    while (k + 1 < t.n && tile >= t.e[k + 1].first) ++k;
+    const Entry& e = t.e[k];
+    const int64_t group = (int64_t)(tile - e.first) * kGroups + threadIdx.x;
+    sum += e.dtype == LST_F32    ? tile_squares<float>(e, group)
+           : e.dtype == LST_BF16 ? tile_squares<__bf16>(e, group)
+                                 : tile_squares<_Float16>(e, group);
+  }
+  sum = block_sum(sum, lds);
+  if (threadIdx.x == 0) partial[blockIdx.x] = sum;
+}
+
+__device__ inline double total_of(const double* partial, int n, double* lds) {
+  double v = 0;
+  for (int i = threadIdx.x; i < n; i += kThreads) v += partial[i];
+  return block_sum(v, lds);
+}
+
+// Many launches' sums into one.
+__global__ __launch_bounds__(kThreads) void join_kernel(const double* partial, int n,
+                                                        double* total) {
+  __shared__ double lds[kThreads / 64];
+  const double v = total_of(partial, n, lds);
+  if (threadIdx.x == 0) *total = v;
+}
+
+// Tiles from the last to the first: what the pass before read last is the likeliest to be in the
+// caches still.
+__global__ __launch_bounds__(kThreads) void scale_kernel(Table t, const double* partial, int n,
+                                                         double max_norm, float* norm,
+                                                         int32_t* status, int first) {
+  __shared__ double lds[kThreads / 64];
+  const double all = sqrt(total_of(partial, n, lds));
+  const bool finite = all < (double)INFINITY;
+  const float factor = finite && all > max_norm ? (float)(max_norm / all) : 1.f;
+  if (first && blockIdx.x == 0 && threadIdx.x == 0) {
+    *norm = (float)all;
+    if (!finite && status) atomicCAS(status, 0, LST_ENONFINITE);
+  }
+  const uint32_t from = blockIdx.x * t.each, to = min(from + t.each, t.tiles);
+  int k = t.n - 1;
+  for (uint32_t tile = to; tile-- > from;) {
+    while (k > 0 && tile < t.e[k].first) --k;
+    const Entry& e = t.e[k];
+    if (factor == 1.f && e.out == e.data) continue;
+    const int64_t group = (int64_t)(tile - e.first) * kGroups + threadIdx.x;
+    if (e.dtype == LST_F32)
+      scale_tile<float>(e, group, factor);
+    else if (e.dtype == LST_BF16)
+      scale_tile<__bf16>(e, group, factor);
+    else
+      scale_tile<_Float16>(e, group, factor);
+  }
+}
+
+int64_t size_of(int dtype) { return dtype == LST_F32 ? 4 : 2; }
+
+// Memory that a matrix takes: `width` bytes of each `stride`.
+struct Region {
+  uintptr_t from, to;
+  int64_t stride, width;
+  int owner;
+  bool written;
+};
+
+bool overlap(const Region& a, const Region& b) {  // a.from <= b.from < a.to
+  if (a.stride != b.stride) return true;
+  // columns of the same matrix do not meet when neither is wrapped into the other
+  const int64_t off = (int64_t)((b.from - a.from) % (uintptr_t)a.stride);
+  return off < a.width || off + b.width > a.stride;
+}
+
+bool good(const lst_gradient& g) {
+  if (!known_dtype(g.dtype) || g.rows < 0 || g.cols < 0) return false;
+  if (g.rows == 0 || g.cols == 0) return true;
+  if (!g.data || g.rows > (int64_t)1 << 40 || g.cols > (int64_t)1 << 40) return false;
+  if (g.rows > ((int64_t)1 << 40) / g.cols || g.ld < g.cols) return false;
+  if (g.rows > 1 && g.ld > ((int64_t)1 << 50) / g.rows) return false;
+  const bool apart = g.out && g.out != g.data;
+  if (apart && (g.ldo < g.cols || (g.rows > 1 && g.ldo > ((int64_t)1 << 50) / g.rows)))
+    return false;
+  return apart || !g.out || g.rows <= 1 || g.ldo == g.ld;
+}
+
+// Whether every matrix that is written is memory of its own.
+bool apart(int n, const lst_gradient* grads) {
+  std::vector<Region> all;
+  all.reserve(2 * (size_t)n);
+  for (int i = 0; i < n; ++i) {
+    const lst_gradient& g = grads[i];
+    if (g.rows == 0 || g.cols == 0) continue;
+    const int64_t e = size_of(g.dtype), width = g.cols * e;
+    auto add = [&](const void* p, int64_t ld, bool written) {
+      const uintptr_t from = (uintptr_t)p;
+      const int64_t stride = g.rows == 1 ? width : ld * e;
+      all.push_back({from, from + (uintptr_t)((g.rows - 1) * stride + width), stride, width, i,
+                     written});
+    };
+    const bool own = !g.out || g.out == g.data;
+    add(g.data, g.ld, own);
+    if (!own) add(g.out, g.ldo, true);
+  }
+  std::sort(all.begin(), all.end(),
+            [](const Region& a, const Region& b) { return a.from < b.from; });
+  for (size_t i = 0; i < all.size(); ++i)
+    for (size_t j = i + 1; j < all.size() && all[j].from < all[i].to; ++j)
+      if ((all[i].written || all[j].written) && overlap(all[i], all[j])) return false;
+  return true;
+}
+
+// Fills a table with matrices from `at` on, and moves it behind the last one taken.
+Table fill(int n, const lst_gradient* grads, int& at) {
+  Table t{};
+  for (; at < n && t.n < kTable; ++at) {
+    const lst_gradient& g = grads[at];
+    if (g.rows == 0 || g.cols == 0) continue;
+    const bool own = !g.out || g.out == g.data;
+    Entry& e = t.e[t.n++];
+    e.data = g.data;
+    e.out = own ? const_cast<void*>(g.data) : g.out;
+    e.rows = g.rows;
+    e.cols = g.cols;
+    e.ld = g.ld;
+    e.ldo = own ? g.ld : g.ldo;
+    e.dtype = g.dtype;
+    if (e.rows > 1 && e.ld == e.cols && e.ldo == e.cols) {
+      e.cols *= e.rows;
+      e.rows = 1;
+    }
+    e.groups = (e.cols + 7) / 8;
+    e.first = t.tiles;
+    t.tiles += (uint32_t)((e.rows * e.groups + kGroups - 1) / kGroups);
+  }
+  t.each = std::max<uint32_t>(1, (t.tiles + kBlocks - 1) / kBlocks);
+  return t;
+}
+
+unsigned blocks_of(const Table& t) { return std::max<unsigned>(1, (t.tiles + t.each - 1) / t.each); }
+
+int tables_of(int n) { return std::max(1, (n + kTable - 1) / kTable); }
+
+}  // namespace
+}  // namespace lst
+
+using namespace lst;
+
+extern "C" {
+
+int64_t lst_clip_workspace(int32_t n) {
+  if (n < 0 || n > kMost) return -1;
+  return ((int64_t)tables_of(n) * kBlocks + 1) * (int64_t)sizeof(double);
+}
+
+int lst_clip(int32_t n, const lst_gradient* grads, double max_norm, float* norm, void* workspace,
+             int32_t* status, void* hip_stream) {
+  if (n < 0 || n > kMost || (n && !grads) || !(max_norm >= 0.0) || !norm || !workspace ||
+      ((uintptr_t)workspace & 15))
+    return LST_EINVAL;
+  int64_t most = 0;  // elements of the call: a launch's tiles are counted in 32 bits
+  for (int i = 0; i < n; ++i) {
+    if (!good(grads[i])) return LST_EINVAL;
+    most += grads[i].rows * grads[i].cols;
+    if (most > (int64_t)1 << 40) return LST_EINVAL;
+  }
+  try {
+    if (!apart(n, grads)) return LST_EINVAL;
+  } catch (const std::bad_alloc&) {
+    return LST_ENOMEM;
+  }
+  hipStream_t s = (hipStream_t)hip_stream;
+  double *total = (double*)workspace, *partial = total + 1;
+  int count = 0, launches = 0;
+  for (int at = 0; launches == 0 || at < n; ++launches) {
+    const Table t = fill(n, grads, at);
+    hipLaunchKernelGGL(squares_kernel, dim3(blocks_of(t)), dim3(kThreads), 0, s, t,
+                       partial + count);
+    count += (int)blocks_of(t);
+  }
+  if (launches > 1) {
+    hipLaunchKernelGGL(join_kernel, dim3(1), dim3(kThreads), 0, s, partial, count, total);
+    partial = total;
+    count = 1;
+  }
+  int rc = launched();
+  for (int at = 0, k = 0; rc == LST_OK && (k == 0 || at < n); ++k) {
+    const Table t = fill(n, grads, at);
+    hipLaunchKernelGGL(scale_kernel, dim3(blocks_of(t)), dim3(kThreads), 0, s, t, partial, count,
+                       max_norm, norm, status, k == 0);
+    rc = launched();
+  }
+  return rc;
+}
+
+}  // extern "C"

@@ -1,0 +1,215 @@
+"""lst_clip against oracle.norms: the norm, and every element within its roundings."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_1412_7091_amd as lst
+from oracle import norms
+
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+U = 2.0 ** -24
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _check(before, after, norm, max_norm):
+    """before, after: arrays in float64, after with its torch type."""
+    n, f, want = norms.clip(before, max_norm)
+    # sums in float64, whose own roundings are far below this one
+    assert abs(float(norm) - n) <= 1.01 * U * n
+    for w, a in zip(want, after):
+        if f == 1.0:
+            assert np.array_equal(_np(a), w)
+            continue
+        off = 2.01 * U * np.abs(w)  # the factor and the product
+        off = off + torch.finfo(a.dtype).eps / 2 * (np.abs(w) + off)
+        off += 2.0 ** -25 if a.dtype == torch.float16 else 2.0 ** -134
+        assert (np.abs(_np(a) - w) <= off).all()
+
+
+def _tensors(shapes, seed=0, kind=None):
+    g = torch.Generator("cuda").manual_seed(seed)
+    return [(torch.randn(s, device="cuda", generator=g) * 2.0 ** (i % 5 - 2)).to(
+        kind or TYPES[i % 3]) for i, s in enumerate(shapes)]
+
+
+SHAPES = [(1,), (7,), (3, 5), (1, 1), (8,), (500,), (500, 1000), (33, 129), (2, 3, 4), (), (0,),
+          (4, 0), (8192,), (8193,), (130, 64), (1, 20_000)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("apart", [False, True])
+@pytest.mark.parametrize("max_norm", [0.0, 1e-3, 500.0, 1e9, float("inf")])
+def test_of_many_shapes_and_types(gpu_lib, apart, max_norm):
+    tensors = _tensors(SHAPES)
+    before = [_np(t) for t in tensors]
+    out = [torch.full_like(t, 9.0) for t in tensors] if apart else None
+    norm = lst.lst_clip(tensors, max_norm, out=out)
+    assert norm.shape == (1,)
+    _check(before, out or tensors, norm, max_norm)
+    if apart:
+        assert all(np.array_equal(_np(t), b) for t, b in zip(tensors, before))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 59, 60, 61, 200])
+def test_numbers_of_tensors(gpu_lib, dtype, n):
+    tensors = _tensors([(i % 37 + 1, i % 11 + 1) for i in range(n)], n, dtype)
+    tensors.insert(n // 2, tensors[0].new_empty((0, 3)))
+    before = [_np(t) for t in tensors]
+    norm = lst.lst_clip(tensors, 2.0)
+    _check(before, tensors, norm, 2.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_columns_of_wider_matrices(gpu_lib, dtype):
+    """Gradients that are columns of one matrix, and what is beside them."""
+    whole = torch.randn((301, 80), device="cuda").to(dtype)
+    a, b, c = whole[:, :33], whole[:, 33:50], whole[::2, 60:]
+    was = whole.clone()
+    before = [_np(t) for t in (a, b, c)]
+    norm = lst.lst_clip([a, b], 3.0)
+    _check(before[:2], [a, b], norm, 3.0)
+    assert torch.equal(whole[:, 50:], was[:, 50:])
+    target = torch.zeros((301, 90), device="cuda", dtype=dtype)
+    norm = lst.lst_clip([c], 1.0, out=[target[:151, 3:23]])
+    _check(before[2:], [target[:151, 3:23]], norm, 1.0)
+    target[:151, 3:23] = 0
+    assert (target == 0).all() and torch.equal(whole[:, 50:], was[:, 50:])
+
+
+@pytest.mark.gpu
+def test_large(gpu_lib):
+    """More tiles than a launch has blocks, and a sum that float32 would not hold."""
+    t = torch.full((40_000_003,), 2.0 ** -10, device="cuda")
+    s = torch.ones((3000, 4001), device="cuda", dtype=torch.bfloat16)
+    half = s[:, :2001]
+    norm = lst.lst_clip([t, half], 100.0)
+    n = np.sqrt(40_000_003 * 2.0 ** -20 + 3000 * 2001)
+    assert abs(float(norm) - n) <= 1.01 * U * n
+    f = 100.0 / n
+    assert (torch.abs(t - f * 2.0 ** -10) <= 2.01 * U * f * 2.0 ** -10).all()
+    assert torch.equal(half, torch.full_like(half, f)) and (s[:, 2001:] == 1).all()
+
+
+@pytest.mark.gpu
+def test_extremes_and_what_is_not_finite(gpu_lib):
+    for big in (3e38, 2.0 ** -140):
+        t = [torch.full((1000,), big, device="cuda")]
+        norm = lst.lst_clip(t, big)
+        n = np.sqrt(1000.0) * float(np.float32(big))
+        f = float(np.float32(big)) / n
+        if big > 1:
+            assert torch.isinf(norm).all()  # no float, but the factor is what it is
+            assert (torch.abs(t[0].double() - f * big) <= 1e-6 * f * big).all()
+        else:
+            assert abs(float(norm) - n) <= 2.0 ** -149
+            assert (torch.abs(t[0].double() - f * big) <= 2.0 ** -149).all()
+    for bad in (float("inf"), float("nan")):
+        a, b = torch.randn(50, device="cuda"), torch.randn((9, 9), device="cuda")
+        a[7] = bad
+        was, out = b.clone(), [torch.zeros_like(a), torch.zeros_like(b)]
+        clip = lst.GradientClip([a, b])
+        norm = clip.clip(0.1)
+        assert clip.sync() == lst.LST_ENONFINITE and clip.sync() == lst.LST_OK
+        assert not torch.isfinite(norm).any() and torch.equal(b, was)
+        lst.lst_clip([a, b], 0.1, out=out)
+        assert torch.equal(out[1], b) and torch.equal(torch.nan_to_num(out[0]), torch.nan_to_num(a))
+
+
+@pytest.mark.gpu
+def test_repeats_captures_and_streams(gpu_lib):
+    tensors = _tensors([(500, 900), (700,), (33, 65)], 5)
+    out = [torch.empty_like(t) for t in tensors]
+    clip = lst.GradientClip(tensors, out=out)
+    first = float(clip.clip(1.0))
+    kept = [o.clone() for o in out]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = clip.clip(1.0)
+    side.synchronize()
+    assert float(again) == first and all(torch.equal(a, b) for a, b in zip(kept, out))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        norm = clip.clip(1.0)
+    for i in range(4):
+        for t in tensors:
+            t.copy_(torch.randn(t.shape, device="cuda") * (i + 1))
+        graph.replay()
+        torch.cuda.synchronize()
+        _check([_np(t) for t in tensors], out, norm, 1.0)
+    assert clip.sync() == lst.LST_OK
+
+
+def _list(*grads):
+    a = (lst.lst_gradient * max(1, len(grads)))()
+    for g, kw in zip(a, grads):
+        base = dict(data=4096, out=None, rows=2, cols=8, ld=8, ldo=8, dtype=0)
+        for k, v in {**base, **kw}.items():
+            setattr(g, k, v)
+    return a
+
+
+def test_refusals_on_the_host():
+    lib, bad = lst.load_library(), lst.LST_EINVAL
+    p = 1 << 20  # never read: every call is refused
+
+    def call(*grads, n=None, max_norm=1.0, norm=p, work=p):
+        return lib.lst_clip(len(grads) if n is None else n, _list(*grads), max_norm, norm, work,
+                            None, None)
+
+    for kw in (dict(dtype=3), dict(rows=-1), dict(cols=-1), dict(data=None), dict(ld=7),
+               dict(out=8192, ldo=7), dict(out=4096, ldo=9), dict(rows=1 << 41),
+               dict(cols=1 << 41, ld=1 << 41), dict(rows=1 << 21, cols=1 << 20, ld=1 << 20),
+               dict(rows=1 << 20, ld=1 << 40)):
+        assert call(kw) == bad, kw
+    assert call({}, n=-1) == bad and call({}, n=65_537) == bad
+    assert lib.lst_clip(1, None, 1.0, p, p, None, None) == bad
+    for kw in (dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(norm=None), dict(work=None),
+               dict(work=p + 8)):
+        assert call({}, **kw) == bad, kw
+    # memory that two of them share, one of which is written
+    for pair in (({}, {}), ({}, dict(data=4096 + 60)), ({}, dict(data=8192, out=4096 + 32)),
+                 (dict(out=8192), dict(data=8192, out=16384)), ({"out": 4096 + 32},),
+                 (dict(out=8192), dict(data=12288, out=8192 + 4)),
+                 (dict(ld=16), dict(data=4096 + 28, ld=16)),        # a column in both
+                 (dict(ld=16), dict(data=4096 + 40, ld=16)),        # wrapped into the next row
+                 (dict(ld=16), dict(data=4096 + 32, ld=17))):
+        assert call(*pair) == bad, pair
+    assert lst.lst_clip_workspace(1) == 8 * 2049 and lst.lst_clip_workspace(61) == 8 * 4097
+    assert lib.lst_clip_workspace(-1) == -1 and lib.lst_clip_workspace(65_537) == -1
+    assert ctypes.sizeof(lst.lst_gradient) == 56
+
+
+def test_tensors_on_the_host_are_refused():
+    with pytest.raises(TypeError):
+        lst.lst_clip([torch.zeros(3)], 1.0)
+    with pytest.raises(ValueError):
+        lst.lst_clip([], 1.0)
+
+
+@pytest.mark.gpu
+def test_refusals_of_tensors(gpu_lib):
+    x = torch.zeros((6, 8), device="cuda")
+    for bad in (lambda: lst.lst_clip([x, x], 1.0), lambda: lst.lst_clip([x, x[2:]], 1.0),
+                lambda: lst.lst_clip([x.double()], 1.0), lambda: lst.lst_clip([x.t()], 1.0),
+                lambda: lst.lst_clip([x.view(2, 3, 8)[:, :2]], 1.0),
+                lambda: lst.lst_clip([x], 1.0, out=[x.bfloat16()]),
+                lambda: lst.lst_clip([x], 1.0, out=[x[:5]]), lambda: lst.lst_clip([x], -1.0),
+                lambda: lst.lst_clip([x], 1.0, out=[]), lambda: lst.lst_clip([x, x.cpu()], 1.0),
+                lambda: lst.lst_clip([x[:, :5]], 1.0, out=[x[:, 3:]])):
+        with pytest.raises((TypeError, ValueError, lst.LstError)):
+            bad()
+    # both read, neither written
+    out = [torch.empty_like(x) for _ in range(2)]
+    lst.lst_clip([x + 1, x + 1], 1.0, out=out)
+    y = x + 1
+    norm = lst.lst_clip([y, y], 1.0, out=out)
+    assert abs(float(norm) - np.sqrt(96)) < 1e-5
