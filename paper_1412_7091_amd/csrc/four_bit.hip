@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const T* x, int64_t ldx, 
   if (l == 0) scales[at] = (uint8_t)e;
 }
 
-// Rows of H into operands: piece (step, tile of 16 rows), and behind the pieces the exponents of
+// Rows of H into operands: piece (tile of 16 rows, step), and behind the pieces the exponents of
 // four steps a word, for each lane of a tile.  Rows behind the last one of the last tile and
 // blocks behind a row's last are zeros.
 template <class T>
@@ -96,10 +96,10 @@ __global__ __launch_bounds__(256) void operands_kernel(const T* x, int64_t ldx, 
   uint32_t q = 0;
   int e = 127;
   if (n < m && b < blocks) q = row_codes(x + (int64_t)n * ldx, b * kSmall + 8 * l, cols, e);
-  out[((int64_t)step * tiles + tile) * (kPiece / 4) + lane * 4 + l] = q;
+  out[((int64_t)tile * steps + step) * (kPiece / 4) + lane * 4 + l] = q;
   if (l == 0)
-    scales[(((int64_t)(step / kGroup) * tiles + tile) * 64 + lane) * kGroup + step % kGroup] =
-        (uint8_t)e;
+    scales[(((int64_t)tile * ((steps + kGroup - 1) / kGroup) + step / kGroup) * 64 + lane) * kGroup +
+           step % kGroup] = (uint8_t)e;
 }
 
 __device__ inline int32x8 operand(uintx4 q) {
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(const uint8_t* W, const 
 #pragma unroll
     for (int k = 0; k < NT; ++k) {
       const int piece = w * NT + k, step = g * kGroup + piece / NT, t = t0 + piece % NT;
-      dma16((const float*)(H + ((int64_t)min(step, steps - 1) * tiles + min(t, tiles - 1)) * kPiece +
+      dma16((const float*)(H + ((int64_t)min(t, tiles - 1) * steps + min(step, steps - 1)) * kPiece +
                            l * 16),
             lds_u32(&hb[g % 2][piece * kPiece]));
     }
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(const uint8_t* W, const 
   for (int g = 0; g < groups; ++g) {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
-      e[n] = sh[((int64_t)g * tiles + min(t0 + n, tiles - 1)) * 64 + l];
+      e[n] = sh[((int64_t)min(t0 + n, tiles - 1) * groups + g) * 64 + l];
     wait_vm_le(0);
     lds_barrier();  // group g has landed; every wave is done with the one before
     if (g + 1 < groups) fetch(g + 1);
@@ -273,6 +273,123 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(const uint8_t* W, const 
         store_rows(O, ldo, m, D, row, r0 + 16 * t + 4 * q4, v);
       }
     }
+}
+
+constexpr int kHeldSteps = 8;    // of a wave's rows of W in registers: 1024 columns
+constexpr int kHeldBlocks = 256; // of that launch, one a compute unit
+constexpr int kHeldBytes = 144 * 1024;  // of LDS for H
+
+// All of H's rows that LDS holds, and waves that go through W by themselves: a wave has 16 MT rows
+// of W in registers, KS steps of them, the next ones' loads under way, multiplies them with one
+// tile of H's rows after another and stores what comes out.  No wave waits for another, so loads
+// of some stand beside the stores of others.  Where H takes several parts, blocks of one XCD take
+// them for the same rows of W, which come from its L2 to all but the first.
+template <class T, int MT, int KS>
+__global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const uint8_t* sw,
+                                                      const uint8_t* H, const int* sh, int m,
+                                                      int64_t D, int blocks, int steps, int part,
+                                                      int parts, int near, T* O, int64_t ldo) {
+  constexpr int G = (KS + kGroup - 1) / kGroup;  // words of exponents
+  __shared__ __attribute__((aligned(16))) uint8_t held[kHeldBytes];
+  const int l = threadIdx.x % 64, i16 = l % 16, q4 = l / 16;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int xcd = blockIdx.x % 8, i = blockIdx.x / 8;
+  const int t0 = i % parts * part, tiles = min(part, (m + 15) / 16 - t0);
+  const int groups = (steps + kGroup - 1) / kGroup;
+  int* exponents = (int*)(held + (int64_t)part * steps * kPiece);
+  for (int p = w; p < tiles * steps; p += 8)
+    dma16((const float*)(H + ((int64_t)t0 * steps + p) * kPiece + l * 16),
+          lds_u32(held + p * kPiece));
+  for (int p = threadIdx.x; p < tiles * groups * 64; p += 512)
+    exponents[p] = sh[(int64_t)t0 * groups * 64 + p];
+  constexpr bool kPairs = sizeof(T) == 2 && MT % 2 == 0;
+  const int64_t ld = (int64_t)blocks * 16, all = (D + 16 * MT - 1) / (16 * MT);
+  const int64_t each = (int64_t)(gridDim.x / 8 / parts) * 64;  // waves beside each other
+  uintx4 q[2][MT][KS];
+  int e[2][MT][KS];
+  auto load = [&](auto slot, int64_t tile) {
+    constexpr int S = slot;
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      const int at = kPairs ? t / 2 * 32 + i16 / 4 * 8 + t % 2 * 4 + i16 % 4 : 16 * t + i16;
+      const int64_t row = min(tile * 16 * MT + at, D - 1);
+      const uint8_t *p = W + row * ld, *ps = sw + row * blocks;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        // blocks behind a row's last one are read as the last: the other side is zero there
+        const int b = min(4 * s + q4, blocks - 1);
+        q[S][t][s] = *reinterpret_cast<const uintx4*>(p + b * 16);
+        if (blocks % 16) e[S][t][s] = ps[b];
+      }
+      if (blocks % 16 == 0) {  // the exponents of four steps, all of the row's, in one load
+        typedef unsigned words __attribute__((ext_vector_type(4), aligned(1)));
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const words u = *reinterpret_cast<const words*>(ps + min(16 * g, blocks - 16));
+#pragma unroll
+          for (int s = 0; s < kGroup && kGroup * g + s < KS; ++s)
+            e[S][t][kGroup * g + s] = u[s] >> (8 * q4);
+        }
+      }
+    }
+  };
+  auto run = [&](auto slot, int64_t tile) {
+    constexpr int S = slot;
+    for (int n = 0; n < tiles; ++n) {
+      f32x4 acc[MT] = {};
+      const uintx4* h = reinterpret_cast<const uintx4*>(held) + (int64_t)n * steps * 64 + l;
+      int eh[G];
+#pragma unroll
+      for (int g = 0; g < G; ++g) eh[g] = exponents[(n * groups + min(g, groups - 1)) * 64 + l];
+      auto step = [&](auto at) {
+        constexpr int s = at;
+        if constexpr (s < KS) {
+          if (s < steps) {
+            const uintx4 b = h[s * 64];
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+              acc[t] = multiply<s % kGroup>(q[S][t][s], e[S][t][s], b, eh[s / kGroup], acc[t]);
+          }
+        }
+      };
+      step(std::integral_constant<int, 0>{});
+      step(std::integral_constant<int, 1>{});
+      step(std::integral_constant<int, 2>{});
+      step(std::integral_constant<int, 3>{});
+      step(std::integral_constant<int, 4>{});
+      step(std::integral_constant<int, 5>{});
+      step(std::integral_constant<int, 6>{});
+      step(std::integral_constant<int, 7>{});
+      const int row = (t0 + n) * 16 + i16;
+#pragma unroll
+      for (int t = 0; t < MT; t += kPairs ? 2 : 1) {
+        const int64_t r = tile * 16 * MT + 16 * t;
+        if constexpr (kPairs) {
+          const f32x4 a = acc[t], b = acc[t + 1];
+          const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+          store_rows(O, ldo, m, D, row, r + 8 * q4, v);
+        } else {
+          const f32x4 a = acc[t];
+          const float v[4] = {a[0], a[1], a[2], a[3]};
+          store_rows(O, ldo, m, D, row, r + 4 * q4, v);
+        }
+      }
+    }
+  };
+  // neighbouring tiles in one block: what its waves store of a row of O is one piece
+  int64_t tile = (w / near * (each / 8) + (int64_t)(i / parts) * 8 + xcd) * near + w % near;
+  std::integral_constant<int, 0> even;
+  std::integral_constant<int, 1> odd;
+  if (tile < all) load(even, tile);
+  wait_vm_le(0);
+  __syncthreads();
+  for (; tile < all; tile += 2 * each) {
+    if (tile + each < all) load(odd, tile + each);
+    run(even, tile);
+    if (tile + each >= all) break;
+    if (tile + 2 * each < all) load(even, tile + 2 * each);
+    run(odd, tile + each);
+  }
 }
 
 constexpr int kFew = 16;         // rows of H that one launch takes
@@ -351,6 +468,35 @@ int lst_scores_four(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int3
     return launched();
   });
   if (rc != LST_OK) return rc;
+  if (steps <= kHeldSteps)
+    return with_dtype(out_dtype, [&](auto t) {
+      using T = decltype(t);
+      const int groups = (steps + kGroup - 1) / kGroup;
+      const int bytes = steps * kPiece + groups * 64 * (int)sizeof(int);  // of a tile of H
+      const int least = (tiles * bytes + kHeldBytes - 1) / kHeldBytes;
+      const int parts = (tiles + (tiles + least - 1) / least - 1) / ((tiles + least - 1) / least);
+      const int part = (tiles + parts - 1) / parts;
+      auto run = [&](auto kernel, int rows) {
+        // blocks of a part on an XCD: as many as leave the fewest of its 32 compute units idle
+        int strips = 1;
+        double best = 0;
+        for (int k = 1; k <= std::max(4, kHeldBlocks / 8 / parts); ++k) {
+          const int64_t n = (int64_t)k * parts, rounds = (n + 31) / 32;
+          const double share = n / (32.0 * rounds);
+          if (share > best) best = share, strips = k;
+        }
+        // few rows of W go to as many compute units as there are
+        const int near = (D + 16 * rows - 1) / (16 * rows) < strips * 64 ? 2 : 8;
+        hipLaunchKernelGGL(kernel, dim3(strips * parts * 8), dim3(512), 0, s, codes, scales,
+                           pieces, (const int*)exponents, m, D, blocks, steps, part, parts, near,
+                           (T*)O, ldo);
+        return launched();
+      };
+      if (steps <= 1) return run(held_kernel<T, 4, 1>, 4);
+      if (steps <= 2) return run(held_kernel<T, 4, 2>, 4);
+      if (steps <= 4) return run(held_kernel<T, 4, 4>, 4);
+      return run(held_kernel<T, 2, 8>, 2);
+    });
   return with_dtype(out_dtype, [&](auto t) {
     using T = decltype(t);
     auto run = [&](auto kernel) {
