@@ -112,6 +112,9 @@ __device__ inline f32x4 multiply(uintx4 a, int sa, uintx4 b, int sb, f32x4 c) {
                                                           BYTE, sb);
 }
 
+template <class T>
+using Sixteen = T __attribute__((ext_vector_type(16 / sizeof(T))));  // bytes
+
 // What a lane gives to one step of a tile of W.  Blocks behind a row's last one are read as the
 // last one: the other side is zero there.
 struct Weights {
@@ -137,6 +140,25 @@ __device__ inline void store_rows(T* O, int64_t ldo, int m, int64_t D, int n, in
   if (r + N <= D) {
     store_vec(o, v);
   } else {
+    for (int i = 0; i < N; ++i)
+      if (r + i < D) o[i] = v[i];
+  }
+}
+
+template <class T>
+__device__ inline void store_bytes(T* O, int64_t ldo, int m, int64_t D, int n, int64_t r,
+                                   uintx4 bytes) {
+  constexpr int N = 16 / (int)sizeof(T);
+  const auto u = __builtin_bit_cast(Sixteen<T>, bytes);
+  if (n >= m || r >= D) return;
+  T* o = O + n * ldo + r;
+  T v[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = u[i];
+  if (r + N <= D) {
+    store_vec(o, v);
+  } else {
+#pragma unroll
     for (int i = 0; i < N; ++i)
       if (r + i < D) o[i] = v[i];
   }
@@ -275,6 +297,20 @@ __global__ __launch_bounds__(256, 2) void scores_kernel(const uint8_t* W, const 
     }
 }
 
+// Trades places: register b of the lanes with bit BIT clear for register a of those with it set,
+// a neighbour's in the four.
+template <int BIT>
+__device__ inline void trade(uintx4& a, uintx4& b, bool set) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int give = (int)(set ? a[i] : b[i]);
+    const unsigned got = (unsigned)__builtin_amdgcn_update_dpp(0, give, BIT ? 0x4E : 0xB1, 0xF,
+                                                               0xF, true);
+    a[i] = set ? got : a[i];
+    b[i] = set ? b[i] : got;
+  }
+}
+
 constexpr int kHeldSteps = 8;    // of a wave's rows of W in registers: 1024 columns
 constexpr int kHeldBlocks = 256; // of that launch, one a compute unit
 constexpr int kHeldBytes = 144 * 1024;  // of LDS for H
@@ -302,7 +338,6 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
           lds_u32(held + p * kPiece));
   for (int p = threadIdx.x; p < tiles * groups * 64; p += 512)
     exponents[p] = sh[(int64_t)t0 * groups * 64 + p];
-  constexpr bool kPairs = sizeof(T) == 2 && MT % 2 == 0;
   const int64_t ld = (int64_t)blocks * 16, all = (D + 16 * MT - 1) / (16 * MT);
   const int64_t each = (int64_t)(gridDim.x / 8 / parts) * 64;  // waves beside each other
   uintx4 q[2][MT][KS];
@@ -311,7 +346,8 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
     constexpr int S = slot;
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-      const int at = kPairs ? t / 2 * 32 + i16 / 4 * 8 + t % 2 * 4 + i16 % 4 : 16 * t + i16;
+      // the four sums of a lane are neighbours, tile after tile
+      const int at = i16 / 4 * 4 * MT + 4 * t + i16 % 4;
       const int64_t row = min(tile * 16 * MT + at, D - 1);
       const uint8_t *p = W + row * ld, *ps = sw + row * blocks;
 #pragma unroll
@@ -360,20 +396,32 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
       step(std::integral_constant<int, 5>{});
       step(std::integral_constant<int, 6>{});
       step(std::integral_constant<int, 7>{});
-      const int row = (t0 + n) * 16 + i16;
+      // 16 bytes of a row of O a register set; neighbouring lanes trade them for those of the
+      // same row, so that a store has 256 bytes of a row (128 of 16 bits or with two tiles)
+      constexpr int kSets = MT * (int)sizeof(T) / 4, kEach = 16 / (int)sizeof(T);
+      uintx4 v[kSets];
 #pragma unroll
-      for (int t = 0; t < MT; t += kPairs ? 2 : 1) {
-        const int64_t r = tile * 16 * MT + 16 * t;
-        if constexpr (kPairs) {
-          const f32x4 a = acc[t], b = acc[t + 1];
-          const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-          store_rows(O, ldo, m, D, row, r + 8 * q4, v);
+      for (int t = 0; t < kSets; ++t) {
+        if constexpr (sizeof(T) == 4) {
+          v[t] = __builtin_bit_cast(uintx4, acc[t]);
         } else {
-          const f32x4 a = acc[t];
-          const float v[4] = {a[0], a[1], a[2], a[3]};
-          store_rows(O, ldo, m, D, row, r + 4 * q4, v);
+          T __attribute__((ext_vector_type(8))) u;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) u[i] = (T)acc[2 * t + i / 4][i % 4];
+          v[t] = __builtin_bit_cast(uintx4, u);
         }
       }
+      if constexpr (kSets >= 2)
+#pragma unroll
+        for (int t = 0; t < kSets; t += 2) trade<0>(v[t], v[t + 1], l & 1);
+      if constexpr (kSets == 4) {
+        trade<1>(v[0], v[2], l & 2);
+        trade<1>(v[1], v[3], l & 2);
+      }
+      const int64_t r = tile * 16 * MT + 4 * MT * q4 + kEach * (l % kSets);
+#pragma unroll
+      for (int j = 0; j < kSets; ++j)
+        store_bytes(O, ldo, m, D, (t0 + n) * 16 + i16 / kSets * kSets + j, r, v[j]);
     }
   };
   // neighbouring tiles in one block: what its waves store of a row of O is one piece
