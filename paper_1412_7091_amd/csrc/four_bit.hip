@@ -165,13 +165,42 @@ __device__ inline void store_bytes(T* O, int64_t ldo, int m, int64_t D, int n, i
 }
 
 // At most 16 rows of H: one launch.  Every block quantises them by itself, into LDS, and its
-// waves go through tiles of 16 rows of W, four steps' codes under way at a time.
+// waves go through tiles of 16 rows of W, four steps at a time, the next four's codes under way.
 template <class TH, class T>
 __global__ __launch_bounds__(512) void few_kernel(const TH* H, int64_t ldh, int d,
                                                   const uint8_t* W, const uint8_t* sw, int m,
                                                   int64_t D, int blocks, int steps, T* O,
                                                   int64_t ldo) {
   extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
+  const int l = threadIdx.x % 64, i16 = l % 16, q4 = l / 16;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int64_t ld = (int64_t)blocks * 16, tiles = (D + 15) / 16;
+  struct Four {
+    uintx4 q[kGroup];
+    int e[kGroup];
+  };
+  auto load = [&](int64_t tile, int s0) {
+    Four c;
+    const int64_t row = min(tile * 16 + i16, D - 1);
+    const uint8_t *p = W + row * ld, *ps = sw + row * blocks;
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j) {
+      // blocks behind a row's last one are read as the last: the other side is zero there
+      const int b = min((s0 + j) * 4 + q4, blocks - 1);
+      c.q[j] = *reinterpret_cast<const uintx4*>(p + b * 16);
+      if (blocks % 16) c.e[j] = ps[b];
+    }
+    if (blocks % 16 == 0) {  // the exponents of four steps, all of the row's, in one load
+      typedef unsigned words __attribute__((ext_vector_type(4), aligned(1)));
+      const words u = *reinterpret_cast<const words*>(ps + 4 * s0);
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) c.e[j] = u[j] >> (8 * q4);
+    }
+    return c;
+  };
+  int64_t tile = (int64_t)blockIdx.x * 8 + w;
+  Four next;
+  if (tile < tiles) next = load(tile, 0);
   int* exponents = (int*)(lds + steps * (kPiece / 4));
   for (int at = threadIdx.x / 4; at < 16 * 4 * steps; at += 512 / 4) {
     const int n = at / (4 * steps), b = at - n * (4 * steps), c = threadIdx.x % 4;
@@ -183,26 +212,26 @@ __global__ __launch_bounds__(512) void few_kernel(const TH* H, int64_t ldh, int 
     if (c == 0) exponents[lane] = e;
   }
   __syncthreads();
-  const int l = threadIdx.x % 64, i16 = l % 16, q4 = l / 16;
   const uintx4* operands = reinterpret_cast<const uintx4*>(lds);
-  const int64_t ld = (int64_t)blocks * 16, tiles = (D + 15) / 16;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  for (int64_t tile = (int64_t)blockIdx.x * 8 + w; tile < tiles; tile += (int64_t)gridDim.x * 8) {
-    const int64_t row = min(tile * 16 + i16, D - 1);
-    const uint8_t *p = W + row * ld, *ps = sw + row * blocks;
-    f32x4 acc = {};
-    for (int s0 = 0; s0 < steps; s0 += 4) {
-      Weights c[4];
+  f32x4 acc = {};
+  for (int s0 = 0; tile < tiles;) {
+    const Four c = next;
+    const int64_t at = tile;
+    const int s = s0;
+    s0 += kGroup;
+    const bool done = s0 >= steps;
+    if (done) s0 = 0, tile += (int64_t)gridDim.x * 8;
+    if (tile < tiles) next = load(tile, s0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) c[j].load<false>(p, ps, (s0 + j) * 4 + q4, blocks);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (s0 + j < steps)
-          acc = multiply<0>(c[j].q, c[j].e, operands[(s0 + j) * 64 + l],
-                            exponents[(s0 + j) * 64 + l], acc);
+    for (int j = 0; j < kGroup; ++j)
+      if (s + j < steps)
+        acc = multiply<0>(c.q[j], c.e[j], operands[(s + j) * 64 + l], exponents[(s + j) * 64 + l],
+                          acc);
+    if (done) {
+      const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
+      store_rows(O, ldo, m, D, i16, at * 16 + 4 * q4, v);
+      acc = f32x4{};
     }
-    const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
-    store_rows(O, ldo, m, D, i16, tile * 16 + 4 * q4, v);
   }
 }
 
@@ -317,14 +346,25 @@ constexpr int kHeldBytes = 144 * 1024;  // of LDS for H
 
 // All of H's rows that LDS holds, and waves that go through W by themselves: a wave has 16 MT rows
 // of W in registers, KS steps of them, the next ones' loads under way, multiplies them with one
-// tile of H's rows after another and stores what comes out.  No wave waits for another, so loads
-// of some stand beside the stores of others.  Where H takes several parts, blocks of one XCD take
-// them for the same rows of W, which come from its L2 to all but the first.
+// tile of H's rows after another and stores what comes out.  Where H takes several parts, blocks
+// of one XCD take them for the same rows of W, which come from its L2 to all but the first.
+//
+// The barriers in the loop stand for no data: they keep the waves, which have neighbouring tiles
+// of W, near each other, so that what two of them store of the same line of memory meets in L2
+// (512 rows of H in bfloat16 by 793 471 x 300: 321 us, with one for each tile of W 356, without
+// 415; by 500 000 x 1024 265, 260 and 251: no more than one a tile there).
+//
+// Measured: 128 rows by 200 000 x 500, float32 outputs, 36 us (157 MB, 4.4 TB/s); 512 rows by
+// 500 000 x 1024 in bfloat16 250 us (784 MB, 3.1 TB/s; 2.1 PFLOP/s).  Without the stores that
+// takes 165 us, without W's loads 150, without either 120; the matrix units alone take 75, at a
+// clock that they pull down from 2.4 to 1.8 GHz.  W through LDS by DMA and H in registers, which
+// halves what LDS gives, took 243 us, and twice as long for rows of O at odd addresses.
 template <class T, int MT, int KS>
 __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const uint8_t* sw,
                                                       const uint8_t* H, const int* sh, int m,
                                                       int64_t D, int blocks, int steps, int part,
                                                       int parts, int near, T* O, int64_t ldo) {
+  constexpr int kTogether = KS > 4 ? 0xFFFF : 3;  // tiles of H between two barriers, less one
   constexpr int G = (KS + kGroup - 1) / kGroup;  // words of exponents
   __shared__ __attribute__((aligned(16))) uint8_t held[kHeldBytes];
   const int l = threadIdx.x % 64, i16 = l % 16, q4 = l / 16;
@@ -372,6 +412,8 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
   auto run = [&](auto slot, int64_t tile) {
     constexpr int S = slot;
     for (int n = 0; n < tiles; ++n) {
+      if ((n & kTogether) == 0) __builtin_amdgcn_s_barrier();
+      if (tile >= all) continue;
       f32x4 acc[MT] = {};
       const uintx4* h = reinterpret_cast<const uintx4*>(held) + (int64_t)n * steps * 64 + l;
       int eh[G];
@@ -431,10 +473,10 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
   if (tile < all) load(even, tile);
   wait_vm_le(0);
   __syncthreads();
-  for (; tile < all; tile += 2 * each) {
+  const int64_t first = ((int64_t)(i / parts) * 8 + xcd) * near;  // of the block's waves
+  for (int64_t u = first; u < all; u += 2 * each, tile += 2 * each) {
     if (tile + each < all) load(odd, tile + each);
     run(even, tile);
-    if (tile + each >= all) break;
     if (tile + 2 * each < all) load(even, tile + 2 * each);
     run(odd, tile + each);
   }

@@ -204,44 +204,76 @@ __device__ inline float value_of(uint64_t key) {
   return __uint_as_float(b >> 31 ? b ^ 0x80000000u : ~b);
 }
 
-__device__ inline uint64_t exchange(uint64_t k, int o) {
-  return (uint64_t)__shfl_xor((unsigned long long)k, o);
+// The key of the lane whose number differs in bit O: without LDS, whose shuffles take four times
+// as long.
+template <int O>
+__device__ inline unsigned exchange(unsigned v) {
+  if constexpr (O == 1) return __builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true);
+  if constexpr (O == 2) return __builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true);
+  if constexpr (O == 4) {  // the eight mirrored, then the four
+    const int m = __builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true);
+    return __builtin_amdgcn_update_dpp(0, m, 0x1B, 0xF, 0xF, true);
+  }
+  if constexpr (O == 8) return __builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, true);
+  if constexpr (O == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
+  }
+  const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return threadIdx.x & 32 ? r[0] : r[1];
+}
+template <int O>
+__device__ inline uint64_t exchange(uint64_t k) {
+  return (uint64_t)exchange<O>((unsigned)(k >> 32)) << 32 | exchange<O>((unsigned)k);
 }
 
-// The keys of a wave, largest first: a lane each.
-__device__ inline uint64_t merge_down(uint64_t k, int lane, int width) {
-  for (int o = width / 2; o; o >>= 1) {
-    const uint64_t other = exchange(k, o);
-    k = ((lane & o) == 0) == (k > other) ? k : other;
+// One step of a bitonic sort: of two lanes the one that `first` names takes the larger key.
+template <int O>
+__device__ inline void order(uint64_t& k, bool first) {
+  const uint64_t other = exchange<O>(k);
+  k = first == (k > other) ? k : other;
+}
+
+// Keys that rise and then fall (or fall and rise): largest first, a lane each.
+template <int WIDTH>
+__device__ inline void merge(uint64_t& k, int lane, bool down) {
+  if constexpr (WIDTH > 1) {
+    order<WIDTH / 2>(k, ((lane & WIDTH / 2) == 0) == down);
+    merge<WIDTH / 2>(k, lane, down);
   }
+}
+// The keys of a wave, smallest first.
+__device__ inline uint64_t sort_up(uint64_t k, int lane) {
+  merge<2>(k, lane, (lane & 2) == 0);
+  merge<4>(k, lane, (lane & 4) == 0);
+  merge<8>(k, lane, (lane & 8) == 0);
+  merge<16>(k, lane, (lane & 16) == 0);
+  merge<32>(k, lane, (lane & 32) == 0);
+  merge<64>(k, lane, false);
   return k;
 }
-__device__ inline uint64_t sort_down(uint64_t k, int lane) {
-  for (int width = 2; width < 64; width <<= 1)
-    for (int o = width / 2; o; o >>= 1) {
-      const uint64_t other = exchange(k, o);
-      const bool first = ((lane & o) == 0) == ((lane & width) == 0);  // keeps the larger
-      k = first == (k > other) ? k : other;
-    }
-  return merge_down(k, lane, 64);
+// The 64 largest of two sets, one largest first, the other smallest first.
+__device__ inline uint64_t join(uint64_t a, uint64_t up, int lane) {
+  uint64_t k = max(a, up);
+  merge<64>(k, lane, true);
+  return k;
 }
-// The 64 largest of two sorted sets.
-__device__ inline uint64_t join(uint64_t a, uint64_t b, int lane) {
-  const uint64_t r = (uint64_t)__shfl((unsigned long long)b, 63 - lane);
-  return merge_down(max(a, r), lane, 64);
+
+__device__ inline uint64_t key_at(uint64_t k, int lane) {  // the same lane for the whole wave
+  return (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 |
+         (unsigned)__builtin_amdgcn_readlane((int)k, lane);
 }
 
 // Takes a key a lane (0: none) into the sorted list of a wave, of which the first n count.
 __device__ inline void take(uint64_t& list, uint64_t k, int n, int lane) {
-  const uint64_t border = (uint64_t)__shfl((unsigned long long)list, n - 1);
-  uint64_t in = __ballot(k > border);
+  uint64_t in = __ballot(k > key_at(list, n - 1));
   if (!in) return;
-  if (__popcll(in) > 6) {
-    list = join(list, sort_down(k, lane), lane);
+  if (__popcll(in) > 4) {
+    list = join(list, sort_up(k, lane), lane);
     return;
   }
   for (; in; in &= in - 1) {
-    const uint64_t one = (uint64_t)__shfl((unsigned long long)k, __ffsll((unsigned long long)in) - 1);
+    const uint64_t one = key_at(k, __builtin_ctzll(in));
     const int at = __popcll(__ballot(list > one));
     const uint64_t before = (uint64_t)__shfl_up((unsigned long long)list, 1);
     list = lane < at ? list : lane == at ? one : before;
@@ -258,7 +290,7 @@ __device__ inline uint64_t join_waves(uint64_t list, uint64_t (&lds)[WAVES][64])
 #pragma unroll
   for (int w = WAVES / 2; w; w >>= 1) {
     if (wave < w) {
-      list = join(list, lds[wave + w][lane], lane);
+      list = join(list, lds[wave + w][63 - lane], lane);
       lds[wave][lane] = list;
     }
     __syncthreads();
@@ -268,9 +300,24 @@ __device__ inline uint64_t join_waves(uint64_t list, uint64_t (&lds)[WAVES][64])
 
 // ------------------------------------------------------------------------------- a row
 // What is left for one block when a row's sums and segments are known.
+// The first token of a thread, read before the row's sums are known.
+struct Token {
+  int token;
+  float value;
+};
+template <class T>
+__device__ inline Token token_of(const Args& a, int row, const T* x, int k) {
+  Token t{-1, 0.f};
+  if (k < a.K) {
+    t.token = a.tokens[(int64_t)row * a.K + k];
+    if (t.token >= 0 && t.token < a.D) t.value = (float)x[t.token];
+  }
+  return t;
+}
+
 template <class T, int THREADS>
 __device__ inline void finish_row(const Args& a, int row, const T* x, Sums sums, float t,
-                                  const float* largest) {
+                                  const float* largest, Token first) {
   constexpr int kWaves = THREADS / 64;
   __shared__ uint64_t lists[kWaves][64];
   const bool some = sums.m > -INFINITY && t > 0.f;
@@ -293,10 +340,11 @@ __device__ inline void finish_row(const Args& a, int row, const T* x, Sums sums,
   }
   for (int k = threadIdx.x; k < a.K; k += THREADS) {
     const int64_t at = (int64_t)row * a.K + k;
-    const int token = a.tokens[at];
+    const Token one = k < THREADS ? first : token_of(a, row, x, k);
+    const int token = one.token;
     float v = __builtin_nanf(""), l = 0.f;
     if (token >= 0 && token < a.D) {
-      v = (float)x[token];
+      v = one.value;
       l = log_of(v);
       if (l == -INFINITY) v = __builtin_nanf("");  // no gradient
     } else if (token != -1 && a.status) {
@@ -308,26 +356,40 @@ __device__ inline void finish_row(const Args& a, int row, const T* x, Sums sums,
   if (!a.top) return;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, n = a.top;
   uint64_t list = 0;
-  if (some)
-    for (int s0 = wave * 64; s0 < a.segments; s0 += THREADS) {
-      const int s = s0 + lane;
-      take(list, s < a.segments ? key_of(largest[s], s) : 0, n, lane);
+  if (some) {
+    float next = wave * 64 + lane < a.segments ? largest[wave * 64 + lane] : -INFINITY;
+    for (int s = wave * 64 + lane; s - lane < a.segments; s += THREADS) {
+      const float v = next;
+      next = s + THREADS < a.segments ? largest[s + THREADS] : -INFINITY;
+      take(list, key_of(v, s), n, lane);
     }
+  }
   join_waves<kWaves>(list, lists);
   const uint64_t border = lists[0][n - 1] >> 32 << 32;  // the n-th entry is no smaller
   list = 0;
-  if (some)
-    for (int i = wave; i < n; i += kWaves) {
-      const uint64_t k = lists[0][i];
-      if (!k) break;
-      const int64_t first = (int64_t)(uint32_t)~k * kSegment;
+  if (some) {
+    constexpr int kEach = kMostTop / kWaves;  // segments of a wave: all of their loads first
+    float v[kEach][kSegment / 64];
 #pragma unroll
-      for (int j = 0; j < kSegment; j += 64) {
-        const int64_t at = first + j + lane;
-        const uint64_t e = at < a.D ? key_of((float)x[at], (uint32_t)at) : 0;
+    for (int i = 0; i < kEach; ++i) {
+      const uint64_t k = i * kWaves + wave < n ? lists[0][i * kWaves + wave] : 0;
+#pragma unroll
+      for (int j = 0; j < kSegment / 64; ++j) {
+        const int64_t at = (int64_t)(uint32_t)~k * kSegment + j * 64 + lane;
+        v[i][j] = k && at < a.D ? (float)x[at] : -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (i * kWaves + wave >= n) break;
+      const uint64_t k = lists[0][i * kWaves + wave];
+#pragma unroll
+      for (int j = 0; j < kSegment / 64; ++j) {
+        const uint64_t e = key_of(v[i][j], (uint32_t)~k * kSegment + j * 64 + lane);
         take(list, e >= border ? e : 0, n, lane);
       }
     }
+  }
   list = join_waves<kWaves>(list, lists);
   if (threadIdx.x < n) {
     const int64_t at = (int64_t)row * n + threadIdx.x;
@@ -342,6 +404,7 @@ template <class T>
 __global__ __launch_bounds__(512) void join_kernel(Args a, const T* logits) {
   const int row = a.row0 + blockIdx.x;
   const float t = temperature_of(a.temperature, row), c = rate_of(t);
+  const Token first = token_of(a, row, logits + row * a.ldx, threadIdx.x);
   Sums sums{-INFINITY, 0.f, 0.f};
   for (int i = threadIdx.x; i < a.chunks; i += 512) {
     const float4 p = a.partial[(int64_t)blockIdx.x * a.chunks + i];
@@ -354,7 +417,7 @@ __global__ __launch_bounds__(512) void join_kernel(Args a, const T* logits) {
   }
   sums = block_sums<512>(sums, c);
   finish_row<T, 512>(a, row, logits + row * a.ldx, sums, t,
-                     a.top ? a.largest + (int64_t)blockIdx.x * a.segments : nullptr);
+                     a.top ? a.largest + (int64_t)blockIdx.x * a.segments : nullptr, first);
 }
 
 template <class T>
@@ -363,11 +426,12 @@ __global__ __launch_bounds__(512) void short_kernel(Args a, const T* logits) {
   const int row = a.row0 + blockIdx.x;
   const float t = temperature_of(a.temperature, row), c = rate_of(t);
   const T* x = logits + row * a.ldx;
+  const Token first = token_of(a, row, x, threadIdx.x);
   Sums sums{-INFINITY, 0.f, 0.f};
-  for (int first = 0; first < a.D; first += 8 * 512)
-    read_entries<T, 512, 1>(sums, x, first, a.D, c, a.top ? largest : nullptr);
+  for (int at = 0; at < a.D; at += 8 * 512)
+    read_entries<T, 512, 1>(sums, x, at, a.D, c, a.top ? largest : nullptr);
   sums = block_sums<512>(sums, c);  // and its barrier is behind the last of `largest`
-  finish_row<T, 512>(a, row, x, sums, t, largest);
+  finish_row<T, 512>(a, row, x, sums, t, largest, first);
 }
 
 // -------------------------------------------------------------------------- the gradient
