@@ -73,15 +73,44 @@ __device__ inline void move_to(Sums& a, float m, float c) {
   a.m = m;
 }
 
+// What the lane holds whose number differs in bit O: without LDS, whose shuffles take several
+// times as long.
+template <int O>
+__device__ inline unsigned exchange(unsigned v) {
+  if constexpr (O == 1) return __builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true);
+  if constexpr (O == 2) return __builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true);
+  if constexpr (O == 4) {  // the eight mirrored, then the four
+    const int m = __builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true);
+    return __builtin_amdgcn_update_dpp(0, m, 0x1B, 0xF, 0xF, true);
+  }
+  if constexpr (O == 8) return __builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, true);
+  if constexpr (O == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return threadIdx.x & 16 ? r[0] : r[1];
+  }
+  const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return threadIdx.x & 32 ? r[0] : r[1];
+}
+template <int O>
+__device__ inline float exchange(float v) {
+  return __uint_as_float(exchange<O>(__float_as_uint(v)));
+}
+
 __device__ inline float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
+  v = fmaxf(v, exchange<1>(v));
+  v = fmaxf(v, exchange<2>(v));
+  v = fmaxf(v, exchange<4>(v));
+  v = fmaxf(v, exchange<8>(v));
+  v = fmaxf(v, exchange<16>(v));
+  return fmaxf(v, exchange<32>(v));
 }
 __device__ inline float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+  v += exchange<1>(v);
+  v += exchange<2>(v);
+  v += exchange<4>(v);
+  v += exchange<8>(v);
+  v += exchange<16>(v);
+  return v + exchange<32>(v);
 }
 
 // The block's sums, in every thread.
@@ -110,16 +139,11 @@ __device__ inline Sums block_sums(Sums a, float c) {
 }
 
 // Largest value of 16 neighbouring lanes, in each of them.
-template <int CTRL>
-__device__ inline float dpp(float v) {
-  return __int_as_float(
-      __builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
-}
 __device__ inline float row_max(float v) {
-  v = fmaxf(v, dpp<0xB1>(v));    // lanes 1 0 3 2
-  v = fmaxf(v, dpp<0x4E>(v));    // lanes 2 3 0 1
-  v = fmaxf(v, dpp<0x141>(v));   // the eight mirrored
-  return fmaxf(v, dpp<0x140>(v));  // the sixteen mirrored
+  v = fmaxf(v, exchange<1>(v));
+  v = fmaxf(v, exchange<2>(v));
+  v = fmaxf(v, exchange<4>(v));
+  return fmaxf(v, exchange<8>(v));
 }
 
 struct Args {
@@ -204,24 +228,6 @@ __device__ inline float value_of(uint64_t key) {
   return __uint_as_float(b >> 31 ? b ^ 0x80000000u : ~b);
 }
 
-// The key of the lane whose number differs in bit O: without LDS, whose shuffles take four times
-// as long.
-template <int O>
-__device__ inline unsigned exchange(unsigned v) {
-  if constexpr (O == 1) return __builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, true);
-  if constexpr (O == 2) return __builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, true);
-  if constexpr (O == 4) {  // the eight mirrored, then the four
-    const int m = __builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, true);
-    return __builtin_amdgcn_update_dpp(0, m, 0x1B, 0xF, 0xF, true);
-  }
-  if constexpr (O == 8) return __builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, true);
-  if constexpr (O == 16) {
-    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-    return threadIdx.x & 16 ? r[0] : r[1];
-  }
-  const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return threadIdx.x & 32 ? r[0] : r[1];
-}
 template <int O>
 __device__ inline uint64_t exchange(uint64_t k) {
   return (uint64_t)exchange<O>((unsigned)(k >> 32)) << 32 | exchange<O>((unsigned)k);
@@ -280,6 +286,33 @@ __device__ inline void take(uint64_t& list, uint64_t k, int n, int lane) {
   }
 }
 
+// The n-th largest of the lanes' values: of many more values, n are no smaller.
+__device__ inline float border_of(float v, int n, int lane) {
+  const uint64_t up = sort_up(key_of(v, 0), lane);
+  const uint64_t k = key_at(up, 64 - n);
+  return k ? value_of(k) : -INFINITY;
+}
+
+// Takes N values a lane, whose indices `index` gives, into a wave's list: those that are no
+// smaller than `least`, nor than the n-th of the lanes' largest.  They wait in the wave's `own`
+// part of LDS: a loop over registers would have its body N times.
+template <int N, class F>
+__device__ inline void take_all(uint64_t& list, const float (&v)[N], float least, int n, int lane,
+                                float (*own)[64], F index) {
+  float m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    own[i][lane] = v[i];
+    m = fmaxf(m, v[i]);
+  }
+  least = fmaxf(least, border_of(m, n, lane));
+#pragma unroll 1
+  for (int i = 0; i < N; ++i) {
+    const float x = own[i][lane];
+    if (__ballot(x >= least)) take(list, x >= least ? key_of(x, index(i)) : 0, n, lane);
+  }
+}
+
 // The waves' lists joined: in the first wave's registers, and in lds[0 .. 63] of every thread.
 template <int WAVES>
 __device__ inline uint64_t join_waves(uint64_t list, uint64_t (&lds)[WAVES][64]) {
@@ -296,6 +329,119 @@ __device__ inline uint64_t join_waves(uint64_t list, uint64_t (&lds)[WAVES][64])
     __syncthreads();
   }
   return list;
+}
+
+// The n likeliest of a row, largest first: put(rank, key).  A bound that n entries reach comes
+// from the lanes' largest segments: the n-th of any wave, or the (n / waves)-th of every wave.
+// Segments that reach it, then their entries that do, are gathered without an order, and each
+// entry's rank is counted.  False, and nothing is put, where too many reach it (rows of few
+// values) or the row has more segments than the lanes take.
+template <class T, int THREADS, class F>
+__device__ inline bool few_candidates(int segments, int D, int n, const T* x,
+                                      const float* largest, F put) {
+  constexpr int kWaves = THREADS / 64, kEach = 16, kSegments = 128, kKeys = 1024;
+  __shared__ float bounds[2][kWaves];
+  __shared__ int counts[2];
+  __shared__ uint32_t found[kSegments];
+  __shared__ __attribute__((aligned(16))) uint64_t keys[kKeys];
+  if (segments > kEach * THREADS) return false;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  if (threadIdx.x < 2) counts[threadIdx.x] = 0;
+  float v[kEach], m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int s = i * THREADS + threadIdx.x;
+    v[i] = s < segments ? largest[s] : -INFINITY;
+    m = fmaxf(m, v[i]);
+  }
+  const uint64_t up = sort_up(key_of(m, 0), lane);
+  if (lane == 64 - n) bounds[0][wave] = up ? value_of(up) : -INFINITY;
+  if (lane == 64 - (n + kWaves - 1) / kWaves) bounds[1][wave] = up ? value_of(up) : -INFINITY;
+  __syncthreads();
+  float any = bounds[0][0], every = bounds[1][0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) {
+    any = fmaxf(any, bounds[0][w]);
+    every = fminf(every, bounds[1][w]);
+  }
+  const float bound = fmaxf(fmaxf(any, every), kLowest);  // -inf is none
+#pragma unroll
+  for (int i = 0; i < kEach; ++i)
+    if (v[i] >= bound) {
+      const int at = atomicAdd(&counts[0], 1);
+      if (at < kSegments) found[at] = i * THREADS + threadIdx.x;
+    }
+  __syncthreads();
+  const int segs = counts[0];
+  if (segs > kSegments) return false;
+  for (int s0 = wave; s0 < segs; s0 += kEach / 2 * kWaves) {
+    uint32_t first[kEach / 2];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int s = s0 + i / 2 * kWaves;
+      if (i % 2 == 0) first[i / 2] = s < segs ? found[s] * kSegment + lane : 0xFFFFFFFFu;
+      const uint32_t at = first[i / 2] + i % 2 * 64;
+      v[i] = s < segs && at < (uint32_t)D ? (float)x[at] : -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (v[i] >= bound) {
+        const int at = atomicAdd(&counts[1], 1);
+        if (at < kKeys) keys[at] = key_of(v[i], first[i / 2] + i % 2 * 64);
+      }
+  }
+  __syncthreads();
+  const int all = counts[1];
+  if (all > kKeys) return false;
+  for (int k = threadIdx.x; k < all; k += THREADS) {
+    const uint64_t key = keys[k];
+    int rank = 0;
+    for (int j = 0; j < all; ++j) rank += keys[j] > key;
+    if (rank < n) put(rank, key);
+  }
+  if ((int)threadIdx.x >= all && threadIdx.x < n) put(threadIdx.x, 0);
+  return true;
+}
+
+// The same for any row: the waves' sorted lists of segments, and then of entries, joined.
+template <class T, int THREADS, class F>
+__device__ inline void many_candidates(int segments, int D, int n, const T* x,
+                                       const float* largest, F put) {
+  constexpr int kWaves = THREADS / 64;
+  constexpr int kEach = 2 * kMostTop / kWaves;  // values of a lane at a time
+  __shared__ uint64_t lists[kWaves][64];
+  __shared__ float values[kWaves][kEach][64];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  uint64_t list = 0;
+  for (int s0 = 0; s0 < segments; s0 += kEach * THREADS) {
+    float v[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int64_t s = s0 + (int64_t)i * THREADS + threadIdx.x;
+      v[i] = s < segments ? largest[s] : -INFINITY;
+    }
+    take_all(list, v, -INFINITY, n, lane, values[wave],
+             [&](int i) { return s0 + i * THREADS + threadIdx.x; });
+  }
+  join_waves<kWaves>(list, lists);
+  const float least = lists[0][n - 1] ? value_of(lists[0][n - 1]) : -INFINITY;
+  auto segment = [&](int i) {  // where part i of the wave's segments begins; -1 for none
+    const int at = i / 2 * kWaves + wave;
+    const uint64_t k = at < n ? lists[0][at] : 0;
+    return k ? (int64_t)(uint32_t)~k * kSegment + i % 2 * 64 : -1;
+  };
+  static_assert(kSegment == 128, "two parts of 64");
+  float v[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int64_t first = segment(i);
+    v[i] = first >= 0 && first + lane < D ? (float)x[first + lane] : -INFINITY;
+  }
+  list = 0;
+  take_all(list, v, least, n, lane, values[wave],
+           [&](int i) { return (uint32_t)segment(i) + lane; });
+  list = join_waves<kWaves>(list, lists);
+  if (threadIdx.x < n) put(threadIdx.x, list);
 }
 
 // ------------------------------------------------------------------------------- a row
@@ -318,8 +464,6 @@ __device__ inline Token token_of(const Args& a, int row, const T* x, int k) {
 template <class T, int THREADS>
 __device__ inline void finish_row(const Args& a, int row, const T* x, Sums sums, float t,
                                   const float* largest, Token first) {
-  constexpr int kWaves = THREADS / 64;
-  __shared__ uint64_t lists[kWaves][64];
   const bool some = sums.m > -INFINITY && t > 0.f;
   const float log_s = some ? logf(sums.s) : 0.f;
   const float entropy = some ? log_s - kLn2 * sums.t / sums.s : 0.f;
@@ -354,49 +498,18 @@ __device__ inline void finish_row(const Args& a, int row, const T* x, Sums sums,
     if (saved) saved[4 + k] = v;
   }
   if (!a.top) return;
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, n = a.top;
-  uint64_t list = 0;
-  if (some) {
-    float next = wave * 64 + lane < a.segments ? largest[wave * 64 + lane] : -INFINITY;
-    for (int s = wave * 64 + lane; s - lane < a.segments; s += THREADS) {
-      const float v = next;
-      next = s + THREADS < a.segments ? largest[s + THREADS] : -INFINITY;
-      take(list, key_of(v, s), n, lane);
-    }
-  }
-  join_waves<kWaves>(list, lists);
-  const uint64_t border = lists[0][n - 1] >> 32 << 32;  // the n-th entry is no smaller
-  list = 0;
-  if (some) {
-    constexpr int kEach = kMostTop / kWaves;  // segments of a wave: all of their loads first
-    float v[kEach][kSegment / 64];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const uint64_t k = i * kWaves + wave < n ? lists[0][i * kWaves + wave] : 0;
-#pragma unroll
-      for (int j = 0; j < kSegment / 64; ++j) {
-        const int64_t at = (int64_t)(uint32_t)~k * kSegment + j * 64 + lane;
-        v[i][j] = k && at < a.D ? (float)x[at] : -INFINITY;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      if (i * kWaves + wave >= n) break;
-      const uint64_t k = lists[0][i * kWaves + wave];
-#pragma unroll
-      for (int j = 0; j < kSegment / 64; ++j) {
-        const uint64_t e = key_of(v[i][j], (uint32_t)~k * kSegment + j * 64 + lane);
-        take(list, e >= border ? e : 0, n, lane);
-      }
-    }
-  }
-  list = join_waves<kWaves>(list, lists);
-  if (threadIdx.x < n) {
-    const int64_t at = (int64_t)row * n + threadIdx.x;
+  const int n = a.top;
+  auto put = [&](int rank, uint64_t key) {
+    const int64_t at = (int64_t)row * n + rank;
     // beside an infinite entry the others have no probability
-    const bool one = list && (sums.m < INFINITY || value_of(list) == INFINITY);
-    a.ids[at] = one ? (int32_t)~(uint32_t)list : -1;
-    a.best[at] = one ? log_of(value_of(list)) : -INFINITY;
+    const bool one = key && (sums.m < INFINITY || value_of(key) == INFINITY);
+    a.ids[at] = one ? (int32_t)~(uint32_t)key : -1;
+    a.best[at] = one ? log_of(value_of(key)) : -INFINITY;
+  };
+  if (!some) {
+    if (threadIdx.x < n) put(threadIdx.x, 0);
+  } else if (!few_candidates<T, THREADS>(a.segments, a.D, n, x, largest, put)) {
+    many_candidates<T, THREADS>(a.segments, a.D, n, x, largest, put);
   }
 }
 
