@@ -182,27 +182,57 @@ __device__ inline void load_entries(const T* x, int64_t col, int D, float (&v)[8
   }
 }
 
+// Eight entries' weights, relative to 2^from, a whole number: the exponent is one rounding of
+// x c - from, without the difference x - m, whose rounding c would scale.
+__device__ inline void add_near(float& s, float& t, const float (&x)[8], float from, float c) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float d = fmaxf(fmaf(x[i], c, -from), -1e4f), e = __builtin_amdgcn_exp2f(d);
+    s += e;
+    t = fmaf(e, d, t);
+  }
+}
+
 // N passes of a block over a row from entry `first`.
 template <class T, int THREADS, int N>
 __device__ inline void read_entries(Sums& sums, const T* x, int64_t first, int D, float c,
                                     float* largest) {
-  float v[N][8];
+  float v[N][8], of[N], m = -INFINITY;
 #pragma unroll
   for (int j = 0; j < N; ++j)
     load_entries(x, first + (int64_t)(j * THREADS + threadIdx.x) * 8, D, v[j]);
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    float m = v[j][0];
+    of[j] = v[j][0];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) m = fmaxf(m, v[j][i]);
-    m = fmaxf(m, -INFINITY);  // where all are no numbers
+    for (int i = 1; i < 8; ++i) of[j] = fmaxf(of[j], v[j][i]);
+    of[j] = fmaxf(of[j], -INFINITY);  // where all are no numbers
+    m = fmaxf(m, of[j]);
     if (largest) {
-      const float of = row_max(m);
+      const float best = row_max(of[j]);
       const int64_t at = first + (int64_t)(j * THREADS + threadIdx.x) * 8;
-      if (threadIdx.x % 16 == 0 && at < D) largest[at / kSegment] = of;
+      if (threadIdx.x % 16 == 0 && at < D) largest[at / kSegment] = best;
     }
-    add_entries(sums, v[j], m, c);
   }
+  Sums a{-INFINITY, 0.f, 0.f};
+  const float top = m * c;
+  if (fabsf(top) < 4194304.f) {
+    const float from = rintf(top), d = fmaf(m, c, -from);
+#pragma unroll
+    for (int j = 0; j < N; ++j) add_near(a.s, a.t, v[j], from, c);
+    const float f = __builtin_amdgcn_exp2f(-d);  // relative to m
+    a.t = f * (a.t - d * a.s);
+    a.s *= f;
+    a.m = m;
+  } else {  // large entries or small temperatures, infinite ones, or none
+#pragma unroll
+    for (int j = 0; j < N; ++j) add_entries(a, v[j], of[j], c);
+  }
+  m = fmaxf(sums.m, m);
+  move_to(sums, m, c);
+  move_to(a, m, c);
+  sums.s += a.s;
+  sums.t += a.t;
 }
 
 template <class T, int N>
