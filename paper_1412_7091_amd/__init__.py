@@ -959,7 +959,7 @@ def _clip(dev, table, max_norm, norm, status):
     import torch
 
     if norm is None:
-        norm = torch.empty(1, dtype=torch.float32, device=dev)
+        norm = torch.empty((), dtype=torch.float32, device=dev)
     n = len(table)
     work = torch.empty(lst_clip_workspace(n), dtype=torch.uint8, device=dev)
     _enqueue("lst_clip", dev, n, table, float(max_norm),
@@ -974,7 +974,7 @@ def lst_clip_workspace(n: int) -> int:
 
 
 def lst_clip(tensors, max_norm, *, out=None, norm=None, status=None):
-    """The norm over all tensors (a device tensor with one element), which are scaled to max_norm
+    """The norm over all tensors (a device tensor without dimensions), which are scaled to max_norm
     where it is larger: in place, or into the tensors of out."""
     return _clip(*_gradients(tensors, out), max_norm, norm, status)
 
@@ -1274,7 +1274,7 @@ class GradientClip:
         self._status = torch.zeros(1, dtype=torch.int32, device=self._device)
 
     def clip(self, max_norm, *, norm=None):
-        """The norm before scaling, a device tensor with one element."""
+        """The norm before scaling, a device tensor without dimensions."""
         return _clip(self._device, self._table, max_norm, norm, self._status)
 
     def sync(self) -> int:
