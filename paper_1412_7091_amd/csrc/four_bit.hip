@@ -563,8 +563,7 @@ int lst_scores_four(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int3
       using T = decltype(t);
       const int groups = (steps + kGroup - 1) / kGroup;
       const int bytes = steps * kPiece + groups * 64 * (int)sizeof(int);  // of a tile of H
-      const int least = (tiles * bytes + kHeldBytes - 1) / kHeldBytes;
-      const int parts = (tiles + (tiles + least - 1) / least - 1) / ((tiles + least - 1) / least);
+      const int most = kHeldBytes / bytes, parts = (tiles + most - 1) / most;
       const int part = (tiles + parts - 1) / parts;
       auto run = [&](auto kernel, int rows) {
         // blocks of a part on an XCD: as many as leave the fewest of its 32 compute units idle

@@ -78,7 +78,10 @@ def _check_scores(H, layer, got):
     (1, 1, 1), (1, 15, 32), (2, 16, 33), (5, 63, 500), (16, 64, 37), (17, 65, 300),
     (33, 1000, 500), (64, 127, 512), (65, 128, 1024), (100, 129, 130), (128, 2001, 500),
     (129, 257, 256), (300, 700, 385), (513, 4097, 128), (3, 300, 4096), (40, 270, 4096),
-    (130, 300, 1153), (16, 8200, 700), (20, 60, 16)])
+    (130, 300, 1153), (16, 8200, 700), (20, 60, 16),
+    # parts of H's rows that LDS just holds, and one tile more
+    (256, 200, 1000), (272, 200, 1000), (513, 300, 1000), (528, 70, 1024), (1100, 90, 600),
+    (1850, 50, 120), (1841, 33, 100)])
 def test_scores(gpu_lib, m, D, d):
     g = torch.Generator("cuda").manual_seed(m + D + d)
     W = torch.randn((D, d), device="cuda", generator=g) / d ** 0.5
