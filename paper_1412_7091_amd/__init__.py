@@ -758,6 +758,16 @@ def _weight(weight, x):
     return _vector(weight, torch.float32, "weight", x.device, x.shape[1])
 
 
+def _sum(x, residual, out):
+    """(s, address, row stride) of the sum's rows: x itself, not written, where there is nothing
+    to add and no rows to put it in."""
+    if out is None:
+        if residual is None:
+            return x, None, 0
+        out = x.new_empty(x.shape)
+    return (out, *_matrix(out, "sum_out", x, x.shape))
+
+
 def lst_norm_forward(x, weight, residual=None, *, eps=1e-6, out=None, sum_out=None, rstd=None):
     """(y, s) of the root-mean-square norm: s = x + residual (x itself without one) and
     y = s weight / rms(s).  rstd: a vector that receives each row's factor."""
@@ -768,13 +778,11 @@ def lst_norm_forward(x, weight, residual=None, *, eps=1e-6, out=None, sum_out=No
     pr, ldr = _matrix(residual, "residual", x, x.shape)
     if out is None:
         out = x.new_empty(x.shape)
-    if sum_out is None:
-        sum_out = x.new_empty(x.shape) if residual is not None else x
-    ps, lds = _matrix(sum_out if sum_out is not x else None, "sum_out", x, x.shape)
+    s, ps, lds = _sum(x, residual, sum_out)
     _enqueue("lst_norm_forward", x.device, code, x.shape[0], x.shape[1], px, ldx, pr, ldr,
              _weight(weight, x), float(eps), ps, lds, *_matrix(out, "out", x, x.shape), None, None,
              _vector(rstd, torch.float32, "rstd", x.device, x.shape[0]))
-    return out, sum_out
+    return out, s
 
 
 def lst_norm_coded(x, weight, residual=None, *, eps=1e-6, codes=None, scales=None, sum_out=None,
@@ -791,15 +799,13 @@ def lst_norm_coded(x, weight, residual=None, *, eps=1e-6, codes=None, scales=Non
         codes = x.new_empty((rows, 128 * blocks), dtype=torch.uint8)
     if scales is None:
         scales = x.new_empty((rows, blocks), dtype=torch.uint8)
-    if sum_out is None:
-        sum_out = x.new_empty(x.shape) if residual is not None else x
-    ps, lds = _matrix(sum_out if sum_out is not x else None, "sum_out", x, x.shape)
+    s, ps, lds = _sum(x, residual, sum_out)
     _enqueue("lst_norm_forward", dev, code, rows, cols, px, ldx, pr, ldr, _weight(weight, x),
              float(eps), ps, lds, None, 0,
              _vector(codes, torch.uint8, "codes", dev, rows * 128 * blocks),
              _vector(scales, torch.uint8, "scales", dev, rows * blocks),
              _vector(rstd, torch.float32, "rstd", dev, rows))
-    return codes, scales, sum_out
+    return codes, scales, s
 
 
 def lst_norm_backward(s, rstd, weight, grad_y, grad_sum=None, *, out=None, grad_weight=None):

@@ -291,6 +291,11 @@ int partials_of(int64_t rows, int cols) {
 
 constexpr int64_t kMostRows = (int64_t)1 << 40;
 
+// Whether a matrix may be written while another is read: it is another one, or the same rows.
+bool may_be(const void* out, int64_t ldo, const void* in, int64_t ld, int64_t rows) {
+  return out != in || ldo == ld || rows <= 1;
+}
+
 }  // namespace
 }  // namespace lst
 
@@ -310,6 +315,12 @@ int lst_norm_forward(int32_t dtype, int64_t rows, int32_t cols, const void* x, i
     return LST_EINVAL;
   if ((!y && !codes) || (y && (ldy < cols || y == sum)) || !codes != !scales) return LST_EINVAL;
   if ((uintptr_t)codes & 15) return LST_EINVAL;
+  for (int i = 0; i < 2; ++i) {
+    const void *out = i ? y : sum, *in[2] = {x, residual};
+    const int64_t ldo = i ? ldy : lds, ld[2] = {ldx, ldr};
+    for (int j = 0; j < 2; ++j)
+      if (out && !may_be(out, ldo, in[j], ld[j], rows)) return LST_EINVAL;
+  }
   ForwardArgs a{rows, ldx, ldr, lds, ldy, cols, (cols + kBlock - 1) / kBlock, eps, weight,
                 rstd, codes, scales};
   const int per = 256 / lanes_of(cols);
@@ -347,6 +358,10 @@ int lst_norm_backward(int32_t dtype, int64_t rows, int32_t cols, const void* sum
                    ldgy < cols || ldgx < cols || (grad_sum && ldgs < cols)))
     return LST_EINVAL;
   if ((uintptr_t)workspace & 15) return LST_EINVAL;
+  if (rows > 0 && (!may_be(grad_x, ldgx, sum, lds, rows) ||
+                   !may_be(grad_x, ldgx, grad_y, ldgy, rows) ||
+                   !may_be(grad_x, ldgx, grad_sum, ldgs, rows)))
+    return LST_EINVAL;
   hipStream_t stream = (hipStream_t)hip_stream;
   const int n = partials_of(rows, cols);
   float* partial = n == 1 ? grad_weight : (float*)workspace;

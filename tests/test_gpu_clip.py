@@ -99,6 +99,17 @@ def test_large(gpu_lib):
 
 
 @pytest.mark.gpu
+def test_no_matrices(gpu_lib):
+    """None at all, by the C entry, and none with an element."""
+    norm = torch.ones((), device="cuda")
+    work = torch.empty(lst.lst_clip_workspace(0), dtype=torch.uint8, device="cuda")
+    assert lst.load_library().lst_clip(0, None, 1.0, norm.data_ptr(), work.data_ptr(), None,
+                                       torch.cuda.current_stream().cuda_stream) == lst.LST_OK
+    assert float(norm) == 0
+    assert float(lst.lst_clip([torch.zeros((3, 0), device="cuda")], 0.0)) == 0
+
+
+@pytest.mark.gpu
 def test_extremes_and_what_is_not_finite(gpu_lib):
     for big in (3e38, 2.0 ** -140):
         t = [torch.full((1000,), big, device="cuda")]

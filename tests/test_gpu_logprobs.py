@@ -125,7 +125,7 @@ def _run(m, D, K, top, dtype, temperature, spread=3.0):
     (1, 1, 1, 1), (3, 7, 2, 5), (2, 8, 1, 8), (4, 127, 3, 3), (5, 128, 1, 1), (2, 129, 1, 64),
     (7, 1000, 10, 20), (3, 4096, 5, 0), (2, 4097, 1, 33), (6, 16384, 4, 7), (2, 16385, 3, 64),
     (1, 16386, 1, 2), (3, 50_000, 16, 20), (40, 20_001, 1, 5), (1, 1_000_003, 2, 32),
-    (300, 60_000, 1, 1)])
+    (300, 60_000, 1, 1), (2, 5, 1, 9), (1, 1_100_001, 2, 64), (1, 1_048_576, 1, 20)])
 def test_float32(gpu_lib, m, D, K, top):
     _run(m, D, K, top, torch.float32, False)
 
@@ -253,6 +253,33 @@ def test_many_tokens_of_one_place(gpu_lib, D):
         _check_grad(_np(x)[i], i, tokens[i], 1.0, g[i], 0.0, grad, torch.float32)
     again = lst.lst_logprobs_backward(x, td, got[4], _dev(g))
     assert torch.equal(grad, again)
+
+
+@pytest.mark.gpu
+def test_more_rows_than_a_batch_of_launches(gpu_lib):
+    """66 000 rows of 16 400: the second batch of both directions, and the rows around its begin."""
+    m, D = 66_000, 16_400
+    batch = 0xFFFFFF // 9
+    assert batch > m and (1 << 30) // D < m  # the second is what bounds a batch
+    first = (1 << 30) // D
+    x = torch.zeros((m, D), device="cuda", dtype=torch.bfloat16)
+    rows = [0, first - 1, first, first + 1, m - 1]
+    part = torch.randn((5, D), device="cuda", generator=torch.Generator("cuda").manual_seed(3))
+    x[rows] = part.bfloat16()
+    td = torch.full((m, 1), 7, dtype=torch.int32, device="cuda")
+    got = lst.lst_logprobs(x, td, top=2, save=True)
+    g, ge = torch.ones((m, 1), device="cuda"), torch.full((m,), 0.5, device="cuda")
+    want = lst.lst_logprobs(x[rows].contiguous(), td[:5].contiguous(), top=2, save=True)
+    for a, b in zip(got, want):
+        assert torch.equal(a[rows], b)
+    flat = torch.ones(m, dtype=torch.bool, device="cuda")
+    flat[rows] = False
+    assert (torch.abs(got[0][flat] + np.log(D)) < 1e-5).all()
+    assert (got[2][flat] == torch.tensor([0, 1], device="cuda", dtype=torch.int32)).all()
+    small = lst.lst_logprobs_backward(x[rows].contiguous(), td[:5].contiguous(), want[4], g[:5],
+                                      ge[:5])
+    grad = lst.lst_logprobs_backward(x, td, got[4], g, ge, out=x)
+    assert torch.equal(grad[rows], small)
 
 
 @pytest.mark.gpu

@@ -163,6 +163,18 @@ def test_strides_in_place_and_what_is_beside(gpu_lib, dtype, cols):
     got = layer.forward(x, r, out=x, sum_out=r)
     assert got[0].data_ptr() == x.data_ptr() and got[1].data_ptr() == r.data_ptr()
     assert torch.equal(x, y) and torch.equal(r, s) and torch.equal(whole[:, beside], was)
+    # the sum where x was, and a copy of x where there is nothing to add
+    whole, (x, r), beside, was = held(a, b)
+    got = layer.forward(x, r, sum_out=x)
+    assert torch.equal(got[0], y) and got[1] is x and torch.equal(x, s) and torch.equal(r, b)
+    got = layer.forward(a, sum_out=r)
+    assert got[1] is r and torch.equal(r, a)
+    codes, scales, _ = layer.forward_coded(a, b)
+    x.copy_(a)
+    r.copy_(b)
+    got = layer.forward_coded(x, r, sum_out=r)
+    assert torch.equal(r, s) and torch.equal(got[0], codes) and torch.equal(got[1], scales)
+    assert torch.equal(whole[:, beside], was)
     for which in range(3):
         whole, views, beside, was = held(s, c, e)
         g, gw = layer.backward(views[0], rstd, views[1], views[2], out=views[which])
@@ -268,6 +280,7 @@ def test_refusals_on_the_host():
     for kw in (dict(dtype=3), dict(rows=-1), dict(rows=(1 << 40) + 1), dict(cols=0),
                dict(cols=4097), dict(x=None), dict(ldx=7), dict(r=p, ldr=7), dict(w=None),
                dict(eps=0.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(s=p + 4, lds=7),
+               dict(ldy=9), dict(s=p, lds=9, y=p + 4), dict(r=p + 4, ldr=9, y=p + 4),
                dict(y=None), dict(ldy=7), dict(s=p, y=p), dict(codes=p), dict(scales=p),
                dict(codes=p + 8, scales=p)):
         assert forward(**kw) == bad, kw
@@ -279,6 +292,7 @@ def test_refusals_on_the_host():
 
     for kw in (dict(dtype=-1), dict(rows=-1), dict(cols=0), dict(cols=4097), dict(s=None),
                dict(lds=7), dict(w=None), dict(q=None), dict(gy=None), dict(ldgy=7),
+               dict(ldgx=9), dict(gy=p + 4, ldgy=9, gx=p + 4), dict(gs=p + 4, ldgs=9, gx=p + 4),
                dict(gs=p, ldgs=7), dict(gx=None), dict(ldgx=7), dict(gw=None), dict(work=None),
                dict(work=p + 4)):
         assert backward(**kw) == bad, kw
