@@ -9,8 +9,8 @@
 // overflows it, and the factor is the same whichever lanes hold the row.
 //
 // Bound by memory: 65 536 x 1024 bfloat16 with a residual (537 MB each way) take 89 us forwards
-// and 108 backwards, 6.0 and 5.0 TB/s (backwards without the next row's loads under way 188);
-// 8191 x 500 float32 (66 MB) 15 us each way.
+// and 104 backwards, 6.0 and 5.2 TB/s (backwards without the next row's loads under way 188);
+// 65 536 x 500 (262 MB) 44 and 52; 8191 x 500 float32 (66 MB) 15 us each way.
 #include <algorithm>
 
 #include "dtypes.h"
@@ -43,33 +43,50 @@ __device__ inline S sum_lanes(S v, S* lds, int& turn) {
 template <class T>
 using Eight = T __attribute__((ext_vector_type(8)));
 
-// WHOLE: the row's columns are a multiple of eight.
-template <bool WHOLE, class T>
-__device__ inline Eight<T> load_eight(const T* row, int col, int cols) {
+template <class T, int N>
+using At = T __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+
+// How a row's columns fall on eights: all of them do (kWhole); the last lane takes the row's last
+// eight, of which it shares the first `skip` with the lane before (kShared: they count once in the
+// sums, and both write the same); or the row has fewer than eight (kTiny).  A lane that reads one
+// to seven columns by themselves waits for them before it can read on: 65 536 rows of 500 in
+// bfloat16 took 56 and 75 us so, and now take 44 and 52.
+enum { kWhole, kShared, kTiny };
+
+struct Columns {
+  int at, skip;  // skip = 8: none
+};
+template <int MODE>
+__device__ inline Columns columns_of(int col, int cols) {
+  if (MODE == kShared && col < cols && col + 8 > cols) return {cols - 8, col - (cols - 8)};
+  return {col, col < cols ? 0 : 8};
+}
+
+template <int MODE, class T>
+__device__ inline Eight<T> load_eight(const T* row, Columns c, int cols) {
   Eight<T> v;
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = (T)0.f;
-  if (col + 8 <= cols) {
-    typedef T vec __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-    v = *reinterpret_cast<const vec*>(row + col);
-  } else if (!WHOLE && col < cols) {
-    T part[8];
-    load_part(row, col, cols, part);
+  if (c.skip == 8) return v;
+  if constexpr (MODE == kTiny) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = part[i];
+    for (int i = 0; i < 8; ++i)
+      if (i < cols) v[i] = row[i];
+  } else {
+    v = *reinterpret_cast<const At<T, 8>*>(row + c.at);
   }
   return v;
 }
 
-template <bool WHOLE, class T>
-__device__ inline void store_eight(T* row, int col, int cols, Eight<T> v) {
-  if (col + 8 <= cols) {
-    typedef T vec __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-    *reinterpret_cast<vec*>(row + col) = v;
-  } else if (!WHOLE) {
+template <int MODE, class T>
+__device__ inline void store_eight(T* row, Columns c, int cols, Eight<T> v) {
+  if (c.skip == 8) return;
+  if constexpr (MODE == kTiny) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (col + i < cols) row[col + i] = v[i];
+      if (i < cols) row[i] = v[i];
+  } else {
+    *reinterpret_cast<At<T, 8>*>(row + c.at) = v;
   }
 }
 
@@ -83,23 +100,24 @@ struct ForwardArgs {
 };
 
 // LANES lanes a row, GROUPS groups of eight columns a lane.
-template <class T, int LANES, int GROUPS, bool WHOLE, bool CODED>
+template <class T, int LANES, int GROUPS, int MODE, bool CODED>
 __global__ __launch_bounds__(256) void forward_kernel(ForwardArgs a, const T* x, const T* r, T* s,
                                                       T* y) {
   constexpr int kRows = 256 / LANES;  // of a block
   __shared__ double sums[8];
   int turn = 0;
   const int l = threadIdx.x % LANES;
+  Columns c[GROUPS];
+#pragma unroll
+  for (int g = 0; g < GROUPS; ++g) c[g] = columns_of<MODE>((g * LANES + l) * 8, a.cols);
   for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES; row < a.rows;
        row += (int64_t)gridDim.x * kRows) {
     Eight<T> v[GROUPS], res[GROUPS];
 #pragma unroll
-    for (int g = 0; g < GROUPS; ++g)
-      v[g] = load_eight<WHOLE>(x + row * a.ldx, (g * LANES + l) * 8, a.cols);
+    for (int g = 0; g < GROUPS; ++g) v[g] = load_eight<MODE>(x + row * a.ldx, c[g], a.cols);
     if (r) {
 #pragma unroll
-      for (int g = 0; g < GROUPS; ++g)
-        res[g] = load_eight<WHOLE>(r + row * a.ldr, (g * LANES + l) * 8, a.cols);
+      for (int g = 0; g < GROUPS; ++g) res[g] = load_eight<MODE>(r + row * a.ldr, c[g], a.cols);
 #pragma unroll
       for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
@@ -111,7 +129,7 @@ __global__ __launch_bounds__(256) void forward_kernel(ForwardArgs a, const T* x,
     for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const double f = (float)v[g][i];
+        const double f = MODE == kShared && i < c[g].skip ? 0.f : (float)v[g][i];
         sum = fma(f, f, sum);
       }
     sum = sum_lanes<LANES>(sum, sums, turn);
@@ -119,16 +137,25 @@ __global__ __launch_bounds__(256) void forward_kernel(ForwardArgs a, const T* x,
     if (l == 0 && a.rstd) a.rstd[row] = (float)q;
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
-      const int col = (g * LANES + l) * 8;
-      const Eight<float> w = load_eight<WHOLE>(a.weight, col, a.cols);
-      if (s) store_eight<WHOLE>(s + row * a.lds, col, a.cols, v[g]);
+      const Eight<float> w = load_eight<MODE>(a.weight, c[g], a.cols);
+      if (s) store_eight<MODE>(s + row * a.lds, c[g], a.cols, v[g]);
       if constexpr (CODED) {
         // in float64: a value that float32's roundings move over a border of the codes would
         // be off by a sixteenth
+        const int col = (g * LANES + l) * 8, move = MODE == kShared ? c[g].skip : 0;
         float f[8];
 #pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = (float)((double)(float)v[g][i] * q * (double)w[i]);
+        if constexpr (MODE == kShared) {  // the lane's own columns to the front
+#pragma unroll
+          for (int o = 4; o; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (move & o) f[i] = i + o < 8 ? f[i + o] : 0.f;
+        }
+#pragma unroll
         for (int i = 0; i < 8; ++i)  // zeros behind the last column, also where q is no number
-          f[i] = col + i < a.cols ? (float)((double)(float)v[g][i] * q * (double)w[i]) : 0.f;
+          f[i] = col + i < a.cols ? f[i] : 0.f;
         uint32_t code[2];
         int e;
         values_codes(f, code, e);
@@ -143,7 +170,7 @@ __global__ __launch_bounds__(256) void forward_kernel(ForwardArgs a, const T* x,
         Eight<T> out;
 #pragma unroll
         for (int i = 0; i < 8; ++i) out[i] = (T)((float)v[g][i] * (float)q * w[i]);
-        store_eight<WHOLE>(y + row * a.ldy, col, a.cols, out);
+        store_eight<MODE>(y + row * a.ldy, c[g], a.cols, out);
       }
     }
   }
@@ -162,7 +189,7 @@ constexpr int threads_of(int lanes) { return lanes > 64 ? lanes : 512; }
 // A wave goes through rows by itself, the next one's loads under way, and keeps its sums for dw
 // in registers; the waves' sums are added in order in LDS, the blocks' by sum_kernel: no order
 // depends on timing.
-template <class T, int LANES, int GROUPS, bool WHOLE>
+template <class T, int LANES, int GROUPS, int MODE>
 __global__ __launch_bounds__(threads_of(LANES)) void backward_kernel(BackwardArgs a, const T* s,
                                                                      const T* gy, const T* gs,
                                                                      T* gx) {
@@ -172,10 +199,13 @@ __global__ __launch_bounds__(threads_of(LANES)) void backward_kernel(BackwardArg
   const int l = threadIdx.x % LANES;
   const int64_t step = (int64_t)gridDim.x * kRows;
   int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
+  Columns c[GROUPS];
   Eight<float> w[GROUPS], dw[GROUPS] = {};
 #pragma unroll
-  for (int g = 0; g < GROUPS; ++g)
-    w[g] = load_eight<WHOLE>(a.weight, (g * LANES + l) * 8, a.cols);
+  for (int g = 0; g < GROUPS; ++g) {
+    c[g] = columns_of<MODE>((g * LANES + l) * 8, a.cols);
+    w[g] = load_eight<MODE>(a.weight, c[g], a.cols);
+  }
   struct Row {
     Eight<T> s[GROUPS], y[GROUPS], d[GROUPS];
     float q;
@@ -184,10 +214,9 @@ __global__ __launch_bounds__(threads_of(LANES)) void backward_kernel(BackwardArg
     Row r;
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
-      const int col = (g * LANES + l) * 8;
-      r.s[g] = load_eight<WHOLE>(s + row * a.lds, col, a.cols);
-      r.y[g] = load_eight<WHOLE>(gy + row * a.ldgy, col, a.cols);
-      if (gs) r.d[g] = load_eight<WHOLE>(gs + row * a.ldgs, col, a.cols);
+      r.s[g] = load_eight<MODE>(s + row * a.lds, c[g], a.cols);
+      r.y[g] = load_eight<MODE>(gy + row * a.ldgy, c[g], a.cols);
+      if (gs) r.d[g] = load_eight<MODE>(gs + row * a.ldgs, c[g], a.cols);
     }
     r.q = a.rstd[row];
     return r;
@@ -201,21 +230,25 @@ __global__ __launch_bounds__(threads_of(LANES)) void backward_kernel(BackwardArg
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        inner = fmaf((float)r.y[g][i] * w[g][i], (float)r.s[g][i] * r.q, inner);
+      for (int i = 0; i < 8; ++i) {
+        const float hat = (float)r.s[g][i] * r.q;
+        // columns that the lane before has count there
+        const float dy = MODE == kShared && i < c[g].skip ? 0.f : (float)r.y[g][i];
+        inner = fmaf(dy * w[g][i], hat, inner);
+        dw[g][i] = fmaf(dy, hat, dw[g][i]);
+      }
     inner = sum_lanes<LANES>(inner, sums, turn) / a.cols;
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
       Eight<T> out;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float hat = (float)r.s[g][i] * r.q, dy = (float)r.y[g][i];
-        float v = r.q * (dy * w[g][i] - hat * inner);
+        const float hat = (float)r.s[g][i] * r.q;
+        float v = r.q * ((float)r.y[g][i] * w[g][i] - hat * inner);
         if (gs) v += (float)r.d[g][i];
         out[i] = (T)v;
-        dw[g][i] = fmaf(dy, hat, dw[g][i]);
       }
-      store_eight<WHOLE>(gx + row * a.ldgx, (g * LANES + l) * 8, a.cols, out);
+      store_eight<MODE>(gx + row * a.ldgx, c[g], a.cols, out);
     }
   }
 #pragma unroll
@@ -231,7 +264,8 @@ __global__ __launch_bounds__(threads_of(LANES)) void backward_kernel(BackwardArg
       for (int g = 0; g < GROUPS; ++g)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          float* p = lds + (g * LANES + l) * 8 + i;
+          if (c[g].skip == 8 || (MODE == kShared && i < c[g].skip)) continue;
+          float* p = lds + c[g].at + i;
           *p = k && LANES <= 64 ? *p + dw[g][i] : dw[g][i];
         }
     }
@@ -268,18 +302,25 @@ __global__ __launch_bounds__(1024) void sum_kernel(const float* partial, int n, 
   }
 }
 
-// Calls f with the lanes that share a row, and the groups of eight columns of each.
+// Calls f with the lanes that share a row, the groups of eight columns of each, and how the
+// columns fall on them.
 template <class F>
 int with_shape(int cols, F f) {
   using std::integral_constant;
   integral_constant<int, 1> one;
   integral_constant<int, 2> two;
-  if (cols <= 128) return f(integral_constant<int, 16>{}, one);
-  if (cols <= 256) return f(integral_constant<int, 32>{}, one);
-  if (cols <= 512) return f(integral_constant<int, 64>{}, one);
-  if (cols <= 1024) return f(integral_constant<int, 64>{}, two);
-  if (cols <= 2048) return f(integral_constant<int, 256>{}, one);
-  return f(integral_constant<int, 256>{}, two);
+  integral_constant<int, 16> few;
+  if (cols < 8) return f(few, one, integral_constant<int, kTiny>{});
+  auto whole = [&](auto mode) {
+    if (cols <= 128) return f(few, one, mode);
+    if (cols <= 256) return f(integral_constant<int, 32>{}, one, mode);
+    if (cols <= 512) return f(integral_constant<int, 64>{}, one, mode);
+    if (cols <= 1024) return f(integral_constant<int, 64>{}, two, mode);
+    if (cols <= 2048) return f(integral_constant<int, 256>{}, one, mode);
+    return f(integral_constant<int, 256>{}, two, mode);
+  };
+  return cols % 8 ? whole(integral_constant<int, kShared>{})
+                  : whole(integral_constant<int, kWhole>{});
 }
 
 int lanes_of(int cols) { return cols <= 128 ? 16 : cols <= 256 ? 32 : cols <= 1024 ? 64 : 256; }
@@ -326,18 +367,15 @@ int lst_norm_forward(int32_t dtype, int64_t rows, int32_t cols, const void* x, i
   const int per = 256 / lanes_of(cols);
   const unsigned grid = (unsigned)std::min<int64_t>((rows + per - 1) / per, 1 << 20);
   return with_dtype(dtype, [&](auto t) {
-    return with_shape(cols, [&](auto lanes, auto groups) {
+    return with_shape(cols, [&](auto lanes, auto groups, auto mode) {
       using T = decltype(t);
       auto run = [&](auto kernel) {
         hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, (hipStream_t)hip_stream, a,
                            (const T*)x, (const T*)residual, (T*)sum, (T*)y);
         return launched();
       };
-      if (cols % 8 == 0)
-        return codes ? run(forward_kernel<T, lanes, groups, true, true>)
-                     : run(forward_kernel<T, lanes, groups, true, false>);
-      return codes ? run(forward_kernel<T, lanes, groups, false, true>)
-                   : run(forward_kernel<T, lanes, groups, false, false>);
+      return codes ? run(forward_kernel<T, lanes, groups, mode, true>)
+                   : run(forward_kernel<T, lanes, groups, mode, false>);
     });
   });
 }
@@ -368,15 +406,14 @@ int lst_norm_backward(int32_t dtype, int64_t rows, int32_t cols, const void* sum
   if (n > 0) {
     BackwardArgs a{rows, lds, ldgy, ldgs, ldgx, cols, weight, rstd, partial};
     const int rc = with_dtype(dtype, [&](auto t) {
-      return with_shape(cols, [&](auto lanes, auto groups) {
+      return with_shape(cols, [&](auto lanes, auto groups, auto mode) {
         using T = decltype(t);
         auto run = [&](auto kernel) {
           hipLaunchKernelGGL(kernel, dim3(n), dim3(threads_of(lanes)), 0, stream, a,
                              (const T*)sum, (const T*)grad_y, (const T*)grad_sum, (T*)grad_x);
           return launched();
         };
-        return cols % 8 == 0 ? run(backward_kernel<T, lanes, groups, true>)
-                             : run(backward_kernel<T, lanes, groups, false>);
+        return run(backward_kernel<T, lanes, groups, mode>);
       });
     });
     if (rc != LST_OK || n == 1) return rc;
