@@ -106,10 +106,10 @@ __device__ inline int32x8 operand(uintx4 q) {
   return int32x8{(int)q[0], (int)q[1], (int)q[2], (int)q[3], 0, 0, 0, 0};
 }
 
-template <int BYTE>  // of sb
+template <int BYTE, int BYTE_A = 0>  // of sb and of sa
 __device__ inline f32x4 multiply(uintx4 a, int sa, uintx4 b, int sb, f32x4 c) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(a), operand(b), c, 4, 4, 0, sa,
-                                                          BYTE, sb);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(a), operand(b), c, 4, 4, BYTE_A,
+                                                          sa, BYTE, sb);
 }
 
 template <class T>
@@ -362,8 +362,8 @@ constexpr int kHeldBytes = 144 * 1024;  // of LDS for H
 template <class T, int MT, int KS>
 __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const uint8_t* sw,
                                                       const uint8_t* H, const int* sh, int m,
-                                                      int64_t D, int blocks, int steps, int part,
-                                                      int parts, int near, T* O, int64_t ldo) {
+                                                      int64_t D, int blocks, int part, int parts,
+                                                      int near, T* O, int64_t ldo) {
   constexpr int kTogether = KS > 4 ? 0xFFFF : 3;  // tiles of H between two barriers, less one
   constexpr int G = (KS + kGroup - 1) / kGroup;  // words of exponents
   __shared__ __attribute__((aligned(16))) uint8_t held[kHeldBytes];
@@ -371,17 +371,17 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int xcd = blockIdx.x % 8, i = blockIdx.x / 8;
   const int t0 = i % parts * part, tiles = min(part, (m + 15) / 16 - t0);
-  const int groups = (steps + kGroup - 1) / kGroup;
-  int* exponents = (int*)(held + (int64_t)part * steps * kPiece);
-  for (int p = w; p < tiles * steps; p += 8)
-    dma16((const float*)(H + ((int64_t)t0 * steps + p) * kPiece + l * 16),
+  int* exponents = (int*)(held + (int64_t)part * KS * kPiece);
+  for (int p = w; p < tiles * KS; p += 8)
+    dma16((const float*)(H + ((int64_t)t0 * KS + p) * kPiece + l * 16),
           lds_u32(held + p * kPiece));
-  for (int p = threadIdx.x; p < tiles * groups * 64; p += 512)
-    exponents[p] = sh[(int64_t)t0 * groups * 64 + p];
+  for (int p = threadIdx.x; p < tiles * G * 64; p += 512)
+    exponents[p] = sh[(int64_t)t0 * G * 64 + p];
   const int64_t ld = (int64_t)blocks * 16, all = (D + 16 * MT - 1) / (16 * MT);
   const int64_t each = (int64_t)(gridDim.x / 8 / parts) * 64;  // waves beside each other
   uintx4 q[2][MT][KS];
-  int e[2][MT][KS];
+  int e[2][MT][G];  // four steps a word
+  const unsigned pick = 0x0400u + 0x0101u * q4;  // byte q4 of one word, and of another
   auto load = [&](auto slot, int64_t tile) {
     constexpr int S = slot;
 #pragma unroll
@@ -391,20 +391,21 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
       const int64_t row = min(tile * 16 * MT + at, D - 1);
       const uint8_t *p = W + row * ld, *ps = sw + row * blocks;
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        // blocks behind a row's last one are read as the last: the other side is zero there
-        const int b = min(4 * s + q4, blocks - 1);
-        q[S][t][s] = *reinterpret_cast<const uintx4*>(p + b * 16);
-        if (blocks % 16) e[S][t][s] = ps[b];
-      }
-      if (blocks % 16 == 0) {  // the exponents of four steps, all of the row's, in one load
-        typedef unsigned words __attribute__((ext_vector_type(4), aligned(1)));
+      for (int s = 0; s < KS; ++s)  // blocks behind a row's last one are read as the last: the
+                                    // other side is zero there
+        q[S][t][s] = *reinterpret_cast<const uintx4*>(p + min(4 * s + q4, blocks - 1) * 16);
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-          const words u = *reinterpret_cast<const words*>(ps + min(16 * g, blocks - 16));
+      for (int g = 0; g < G; ++g) {
+        if (blocks % 16 == 0) {  // all of the row's, in one load
+          typedef unsigned words __attribute__((ext_vector_type(4), aligned(1)));
+          const words u = *reinterpret_cast<const words*>(ps + 16 * g);
+          e[S][t][g] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], pick),
+                                             __builtin_amdgcn_perm(u[1], u[0], pick), 0x05040100);
+        } else {
+          e[S][t][g] = 0;
 #pragma unroll
           for (int s = 0; s < kGroup && kGroup * g + s < KS; ++s)
-            e[S][t][kGroup * g + s] = u[s] >> (8 * q4);
+            e[S][t][g] |= ps[min(16 * g + 4 * s + q4, blocks - 1)] << (8 * s);
         }
       }
     }
@@ -415,20 +416,20 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
       if ((n & kTogether) == 0) __builtin_amdgcn_s_barrier();
       if (tile >= all) continue;
       f32x4 acc[MT] = {};
-      const uintx4* h = reinterpret_cast<const uintx4*>(held) + (int64_t)n * steps * 64 + l;
+      const uintx4* h = reinterpret_cast<const uintx4*>(held) + (int64_t)n * KS * 64 + l;
+      uintx4 b[KS];
       int eh[G];
 #pragma unroll
-      for (int g = 0; g < G; ++g) eh[g] = exponents[(n * groups + min(g, groups - 1)) * 64 + l];
+      for (int s = 0; s < KS; ++s) b[s] = h[s * 64];
+#pragma unroll
+      for (int g = 0; g < G; ++g) eh[g] = exponents[(n * G + g) * 64 + l];
       auto step = [&](auto at) {
         constexpr int s = at;
-        if constexpr (s < KS) {
-          if (s < steps) {
-            const uintx4 b = h[s * 64];
+        if constexpr (s < KS)
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
-              acc[t] = multiply<s % kGroup>(q[S][t][s], e[S][t][s], b, eh[s / kGroup], acc[t]);
-          }
-        }
+          for (int t = 0; t < MT; ++t)
+            acc[t] = multiply<s % kGroup, s % kGroup>(q[S][t][s], e[S][t][s / kGroup], b[s],
+                                                      eh[s / kGroup], acc[t]);
       };
       step(std::integral_constant<int, 0>{});
       step(std::integral_constant<int, 1>{});
@@ -577,14 +578,20 @@ int lst_scores_four(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int3
         // few rows of W go to as many compute units as there are
         const int near = (D + 16 * rows - 1) / (16 * rows) < strips * 64 ? 2 : 8;
         hipLaunchKernelGGL(kernel, dim3(strips * parts * 8), dim3(512), 0, s, codes, scales,
-                           pieces, (const int*)exponents, m, D, blocks, steps, part, parts, near,
-                           (T*)O, ldo);
+                           pieces, (const int*)exponents, m, D, blocks, part, parts, near, (T*)O,
+                           ldo);
         return launched();
       };
-      if (steps <= 1) return run(held_kernel<T, 4, 1>, 4);
-      if (steps <= 2) return run(held_kernel<T, 4, 2>, 4);
-      if (steps <= 4) return run(held_kernel<T, 4, 4>, 4);
-      return run(held_kernel<T, 2, 8>, 2);
+      switch (steps) {
+        case 1: return run(held_kernel<T, 4, 1>, 4);
+        case 2: return run(held_kernel<T, 4, 2>, 4);
+        case 3: return run(held_kernel<T, 4, 3>, 4);
+        case 4: return run(held_kernel<T, 4, 4>, 4);
+        case 5: return run(held_kernel<T, 2, 5>, 2);
+        case 6: return run(held_kernel<T, 2, 6>, 2);
+        case 7: return run(held_kernel<T, 2, 7>, 2);
+        default: return run(held_kernel<T, 2, 8>, 2);
+      }
     });
   return with_dtype(out_dtype, [&](auto t) {
     using T = decltype(t);
