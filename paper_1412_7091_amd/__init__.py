@@ -646,10 +646,12 @@ def lst_scores_workspace(m: int, d: int) -> int:
     return int(load_library().lst_scores_workspace(m, d))
 
 
-def _scores_out(H, m, D, dtype, out):
-    """(out, its dtype code, address, row stride) for m rows of D outputs beside H."""
+def _scores_out(H, m, D, dtype, out, lines=False):
+    """(out, its dtype code, address, row stride) for m rows of D outputs beside H; lines: rows of
+    a new matrix begin at multiples of 128 bytes."""
     if out is None:
-        out = H.new_empty((m, D), dtype=dtype)
+        part = 128 // dtype.itemsize if lines else 1
+        out = H.new_empty_strided((m, D), (-(-D // part) * part, 1), dtype=dtype)
     elif dtype is not None and out.dtype != dtype:
         raise TypeError(f"out must be {dtype}, got {out.dtype}")
     po, ldo = _matrix(out, "out", shape=(m, D))
@@ -728,7 +730,11 @@ def lst_scores_four_workspace(m: int, d: int) -> int:
 
 
 def lst_scores_four(H, codes, scales, *, dtype=None, out=None):
-    """O = H W^T from the weights' 4-bit codes and scales, H in 4 bits too; dtype: that of O."""
+    """O = H W^T from the weights' 4-bit codes and scales, H in 4 bits too; dtype: that of O.
+
+    Where out is not given, the rows of O begin at multiples of 128 bytes, so that O is contiguous
+    only if D is such a multiple: 512 rows of 793 471 in bfloat16 take 220 us so, and 321 without
+    space between them."""
     import torch
 
     ph, ldh = _matrix(H, "H")
@@ -738,7 +744,8 @@ def lst_scores_four(H, codes, scales, *, dtype=None, out=None):
     blocks = (d + 31) // 32
     if scales.dim() != 2 or scales.shape[1] != blocks or codes.shape != (D, 16 * blocks):
         raise ValueError(f"codes and scales must be those of a matrix with {d} columns")
-    out, ocode, po, ldo = _scores_out(H, m, D, dtype or (H.dtype if out is None else None), out)
+    out, ocode, po, ldo = _scores_out(H, m, D, dtype or (H.dtype if out is None else None), out,
+                                      lines=m > 1)
     work = _work(H, lst_scores_four_workspace(m, d))
     _enqueue("lst_scores_four", dev, code, ocode, m, D, d, ph, ldh,
              _vector(codes, torch.uint8, "codes", dev),

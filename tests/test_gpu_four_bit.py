@@ -126,6 +126,21 @@ def test_scores_strides_and_what_is_beside(gpu_lib, out, m):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("out", TYPES)
+def test_rows_of_new_outputs_begin_at_lines(gpu_lib, out):
+    g = torch.Generator("cuda").manual_seed(2)
+    layer = lst.FourBitOutputLayer(torch.randn((203, 40), device="cuda", generator=g))
+    H = torch.randn((33, 40), device="cuda", generator=g)
+    got = layer.scores(H, dtype=out)
+    assert got.shape == (33, 203) and got.stride(1) == 1
+    assert got.stride(0) * got.element_size() == -(-203 * got.element_size() // 128) * 128
+    tight = torch.empty((33, 203), device="cuda", dtype=out)
+    assert torch.equal(layer.scores(H, out=tight), got)
+    assert layer.scores(H[:1]).is_contiguous()
+    assert lst.FourBitOutputLayer(torch.ones((256, 40), device="cuda")).scores(H).is_contiguous()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("m", [3, 35])
 def test_sums_of_sizes_far_apart(gpu_lib, m):
     """Blocks 2^20 apart that one instruction adds up: what float32 keeps of the smaller stays."""
