@@ -384,7 +384,8 @@ __device__ inline bool few_candidates(int segments, int D, int n, const T* x,
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   if (threadIdx.x < 2) counts[threadIdx.x] = 0;
   float v[kEach];
-  const int own = lane * kWaves + wave;  // few segments go to all waves
+  // few segments go to all waves (many: neighbouring lanes read neighbours, 8 us for 11)
+  const int own = segments < THREADS ? lane * kWaves + wave : threadIdx.x;
   auto bound_of = [&](int turn) {
     float m = v[0];
 #pragma unroll
