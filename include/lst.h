@@ -388,8 +388,10 @@ void lst_input_free(lst_input* s);
  *
  * The sparse input layer and the output layer leave the rows between them (m x d
  * activations and their gradients) to the caller.  The calls below work on such
- * rows: dropout, a gated linear recurrence over packed sequences, outputs of a
- * layer whose weights are held in 8 bits, and the choice of a token from them.
+ * rows: dropout, a gated linear recurrence over packed sequences, a norm with the
+ * residual's addition, outputs of a layer whose weights are held in 8 or 4 bits, the
+ * choice of a token from them, log probabilities with their gradient, and the clipping
+ * of a step's gradients.
  *
  * They hold no state.  Shared by all of them:
  *   - Matrices are row-major with unit stride along a row and any row stride ld

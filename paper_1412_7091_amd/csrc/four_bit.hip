@@ -67,7 +67,8 @@ __device__ inline uint32_t row_codes(const T* row, int col, int cols, int& e) {
   return small_codes(v, e);
 }
 
-// Four lanes a block, eight columns a lane.
+// Four lanes a block, eight columns a lane.  Bound by memory: 793 471 x 300 floats (1.09 GB with
+// the codes) take 202 us, 5.4 TB/s.
 template <class T>
 __global__ __launch_bounds__(256) void quantize_kernel(const T* x, int64_t ldx, int64_t rows,
                                                        int cols, int blocks, uint32_t* codes,
@@ -166,6 +167,8 @@ __device__ inline void store_bytes(T* O, int64_t ldo, int m, int64_t D, int n, i
 
 // At most 16 rows of H: one launch.  Every block quantises them by itself, into LDS, and its
 // waves go through tiles of 16 rows of W, four steps at a time, the next four's codes under way.
+// Bound by memory: one row by 200 000 x 500 (55 MB) takes 13.0 us, 4.2 TB/s (13.9 without the next
+// codes under way).
 template <class TH, class T>
 __global__ __launch_bounds__(512) void few_kernel(const TH* H, int64_t ldh, int d,
                                                   const uint8_t* W, const uint8_t* sw, int m,
@@ -235,6 +238,8 @@ __global__ __launch_bounds__(512) void few_kernel(const TH* H, int64_t ldh, int 
   }
 }
 
+// Rows of more than 1024 columns, which do not fit a wave's registers.
+//
 // 16 MT rows of W a wave, four waves a block one after another, 16 NT rows of H a block.  Four
 // steps of H's operands go to LDS by DMA while the four before are multiplied; the codes of a
 // wave's own rows go to registers, two steps ahead.
@@ -340,7 +345,7 @@ __device__ inline void trade(uintx4& a, uintx4& b, bool set) {
   }
 }
 
-constexpr int kHeldSteps = 8;    // of a wave's rows of W in registers: 1024 columns
+constexpr int kHeldSteps = 8;    // of a wave's rows of W in registers: 1024 columns, two sets
 constexpr int kHeldBlocks = 256; // of that launch, one a compute unit
 constexpr int kHeldBytes = 144 * 1024;  // of LDS for H
 
@@ -354,11 +359,15 @@ constexpr int kHeldBytes = 144 * 1024;  // of LDS for H
 // (512 rows of H in bfloat16 by 793 471 x 300: 321 us, with one for each tile of W 356, without
 // 415; by 500 000 x 1024 265, 260 and 251: no more than one a tile there).
 //
+// A wave reads all of a tile's operands before it multiplies them: with a branch for each step,
+// which the number of steps as an argument asks for, each read was waited for by itself, and 512
+// rows by 500 000 x 1024 took 251 us.
+//
 // Measured: 128 rows by 200 000 x 500, float32 outputs, 36 us (157 MB, 4.4 TB/s); 512 rows by
-// 500 000 x 1024 in bfloat16 250 us (784 MB, 3.1 TB/s; 2.1 PFLOP/s).  Without the stores that
-// takes 165 us, without W's loads 150, without either 120; the matrix units alone take 75, at a
-// clock that they pull down from 2.4 to 1.8 GHz.  W through LDS by DMA and H in registers, which
-// halves what LDS gives, took 243 us, and twice as long for rows of O at odd addresses.
+// 500 000 x 1024 in bfloat16 226 us (784 MB, 3.5 TB/s; 2.3 PFLOP/s).  W through LDS by DMA with H
+// in registers, which halves what LDS gives, took 243 us where this took 251, and twice as long
+// for rows of O at odd addresses; two tiles of H at a time, and the next tile's operands under
+// way, nothing to gain (231, 235: the registers).
 template <class T, int MT, int KS>
 __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const uint8_t* sw,
                                                       const uint8_t* H, const int* sh, int m,
@@ -483,7 +492,8 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
   }
 }
 
-constexpr int kFew = 16;         // rows of H that one launch takes
+constexpr int kFew = 16;         // rows of H that one launch takes: 17.8 us (16 by 200 000 x
+                                 // 500 codes), with operands first 20.4; one row 15.9 and 19.8
 constexpr int kFewBlocks = 512;  // blocks of that launch, two a compute unit
 constexpr int64_t kMostBlocks = (1 << 30) - 64;  // of a matrix: 2^32 threads
 
@@ -547,6 +557,8 @@ int lst_scores_four(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int3
         return launched();
       });
     });
+  // 256 rows of W and up to 8 tiles of H a block; no more than there are: 17 rows of H by 200 000
+  // x 2048 codes take 92 us with 2 tiles and 97 with 8, 64 take 105 with 4 and 107 with 8
   const int nt = tiles <= 2 ? 2 : tiles <= 4 ? 4 : 8;
   const int64_t row_blocks = (D + 255) / 256;
   const int64_t grid = (row_blocks + 7) / 8 * 8 * ((tiles + nt - 1) / nt);
