@@ -180,7 +180,7 @@ __global__ __launch_bounds__(512) void few_kernel(const TH* H, int64_t ldh, int 
   const int64_t ld = (int64_t)blocks * 16, tiles = (D + 15) / 16;
   struct Four {
     uintx4 q[kGroup];
-    int e[kGroup];
+    unsigned e[kGroup];
   };
   auto load = [&](int64_t tile, int s0) {
     Four c;
@@ -197,10 +197,12 @@ __global__ __launch_bounds__(512) void few_kernel(const TH* H, int64_t ldh, int 
       typedef unsigned words __attribute__((ext_vector_type(4), aligned(1)));
       const words u = *reinterpret_cast<const words*>(ps + 4 * s0);
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j) c.e[j] = u[j] >> (8 * q4);
+      for (int j = 0; j < kGroup; ++j) c.e[j] = u[j];
     }
     return c;
   };
+  // of the lane's own blocks: taken where they are used, or the load would be waited for at once
+  const int shift = blocks % 16 == 0 ? 8 * q4 : 0;
   int64_t tile = (int64_t)blockIdx.x * 8 + w;
   Four next;
   if (tile < tiles) next = load(tile, 0);
@@ -228,8 +230,8 @@ __global__ __launch_bounds__(512) void few_kernel(const TH* H, int64_t ldh, int 
 #pragma unroll
     for (int j = 0; j < kGroup; ++j)
       if (s + j < steps)
-        acc = multiply<0>(c.q[j], c.e[j], operands[(s + j) * 64 + l], exponents[(s + j) * 64 + l],
-                          acc);
+        acc = multiply<0>(c.q[j], c.e[j] >> shift, operands[(s + j) * 64 + l],
+                          exponents[(s + j) * 64 + l], acc);
     if (done) {
       const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
       store_rows(O, ldo, m, D, i16, at * 16 + 4 * q4, v);
@@ -389,7 +391,7 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
   const int64_t ld = (int64_t)blocks * 16, all = (D + 16 * MT - 1) / (16 * MT);
   const int64_t each = (int64_t)(gridDim.x / 8 / parts) * 64;  // waves beside each other
   uintx4 q[2][MT][KS];
-  int e[2][MT][G];  // four steps a word
+  unsigned raw[2][MT][G * kGroup];  // exponents as they were read
   const unsigned pick = 0x0400u + 0x0101u * q4;  // byte q4 of one word, and of another
   auto load = [&](auto slot, int64_t tile) {
     constexpr int S = slot;
@@ -408,19 +410,30 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
         if (blocks % 16 == 0) {  // all of the row's, in one load
           typedef unsigned words __attribute__((ext_vector_type(4), aligned(1)));
           const words u = *reinterpret_cast<const words*>(ps + 16 * g);
-          e[S][t][g] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], pick),
-                                             __builtin_amdgcn_perm(u[1], u[0], pick), 0x05040100);
-        } else {
-          e[S][t][g] = 0;
 #pragma unroll
-          for (int s = 0; s < kGroup && kGroup * g + s < KS; ++s)
-            e[S][t][g] |= ps[min(16 * g + 4 * s + q4, blocks - 1)] << (8 * s);
+          for (int s = 0; s < kGroup; ++s) raw[S][t][kGroup * g + s] = u[s];
+        } else {
+#pragma unroll
+          for (int s = 0; s < kGroup; ++s)
+            raw[S][t][kGroup * g + s] = ps[min(16 * g + 4 * s + q4, blocks - 1)];
         }
       }
     }
   };
   auto run = [&](auto slot, int64_t tile) {
     constexpr int S = slot;
+    // four steps of the lane's own blocks a word: put together here, or the loads would be waited
+    // for where they are issued (512 rows by 500 000 x 1024: 226 us so)
+    int e[MT][G];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        const unsigned* u = raw[S][t] + kGroup * g;
+        const unsigned how = blocks % 16 == 0 ? pick : 0x0400u;
+        e[t][g] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], how),
+                                        __builtin_amdgcn_perm(u[1], u[0], how), 0x05040100);
+      }
     for (int n = 0; n < tiles; ++n) {
       if ((n & kTogether) == 0) __builtin_amdgcn_s_barrier();
       if (tile >= all) continue;
@@ -437,7 +450,7 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
         if constexpr (s < KS)
 #pragma unroll
           for (int t = 0; t < MT; ++t)
-            acc[t] = multiply<s % kGroup, s % kGroup>(q[S][t][s], e[S][t][s / kGroup], b[s],
+            acc[t] = multiply<s % kGroup, s % kGroup>(q[S][t][s], e[t][s / kGroup], b[s],
                                                       eh[s / kGroup], acc[t]);
       };
       step(std::integral_constant<int, 0>{});
