@@ -167,9 +167,10 @@ __device__ inline void store_bytes(T* O, int64_t ldo, int m, int64_t D, int n, i
 
 // At most 16 rows of H: one launch.  Every block quantises them by itself, into LDS, and its
 // waves go through tiles of 16 rows of W, four steps at a time, the next four's codes under way.
-// Bound by memory: one row by 200 000 x 500 (55 MB) takes 13.0 us, 4.2 TB/s (13.9 without the next
-// codes under way).
-template <class TH, class T>
+// Bound by memory: one row by 200 000 x 500 (55 MB) takes 12.1 us, 4.6 TB/s (13.9 without the next
+// codes under way).  WIDE: a row has a multiple of 16
+// blocks, so that its exponents are loaded by words.
+template <class TH, class T, bool WIDE>
 __global__ __launch_bounds__(512) void few_kernel(const TH* H, int64_t ldh, int d,
                                                   const uint8_t* W, const uint8_t* sw, int m,
                                                   int64_t D, int blocks, int steps, T* O,
@@ -191,9 +192,9 @@ __global__ __launch_bounds__(512) void few_kernel(const TH* H, int64_t ldh, int 
       // blocks behind a row's last one are read as the last: the other side is zero there
       const int b = min((s0 + j) * 4 + q4, blocks - 1);
       c.q[j] = *reinterpret_cast<const uintx4*>(p + b * 16);
-      if (blocks % 16) c.e[j] = ps[b];
+      if constexpr (!WIDE) c.e[j] = ps[b];
     }
-    if (blocks % 16 == 0) {  // the exponents of four steps, all of the row's, in one load
+    if constexpr (WIDE) {  // the exponents of four steps, all of the row's, in one load
       typedef unsigned words __attribute__((ext_vector_type(4), aligned(1)));
       const words u = *reinterpret_cast<const words*>(ps + 4 * s0);
 #pragma unroll
@@ -202,10 +203,9 @@ __global__ __launch_bounds__(512) void few_kernel(const TH* H, int64_t ldh, int 
     return c;
   };
   // of the lane's own blocks: taken where they are used, or the load would be waited for at once
-  const int shift = blocks % 16 == 0 ? 8 * q4 : 0;
+  const int shift = WIDE ? 8 * q4 : 0;
   int64_t tile = (int64_t)blockIdx.x * 8 + w;
-  Four next;
-  if (tile < tiles) next = load(tile, 0);
+  Four next = load(tile, 0);
   int* exponents = (int*)(lds + steps * (kPiece / 4));
   for (int at = threadIdx.x / 4; at < 16 * 4 * steps; at += 512 / 4) {
     const int n = at / (4 * steps), b = at - n * (4 * steps), c = threadIdx.x % 4;
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(512) void few_kernel(const TH* H, int64_t ldh, int 
     s0 += kGroup;
     const bool done = s0 >= steps;
     if (done) s0 = 0, tile += (int64_t)gridDim.x * 8;
-    if (tile < tiles) next = load(tile, s0);
+    next = load(tile, s0);  // behind the last tile, where W's last row is read, too
 #pragma unroll
     for (int j = 0; j < kGroup; ++j)
       if (s + j < steps)
@@ -366,11 +366,12 @@ constexpr int kHeldBytes = 144 * 1024;  // of LDS for H
 // rows by 500 000 x 1024 took 251 us.
 //
 // Measured: 128 rows by 200 000 x 500, float32 outputs, 36 us (157 MB, 4.4 TB/s); 512 rows by
-// 500 000 x 1024 in bfloat16 226 us (784 MB, 3.5 TB/s; 2.3 PFLOP/s).  W through LDS by DMA with H
+// 500 000 x 1024 in bfloat16 214 us (784 MB, 3.7 TB/s; 2.5 PFLOP/s).  W through LDS by DMA with H
 // in registers, which halves what LDS gives, took 243 us where this took 251, and twice as long
 // for rows of O at odd addresses; two tiles of H at a time, and the next tile's operands under
-// way, nothing to gain (231, 235: the registers).
-template <class T, int MT, int KS>
+// way, nothing to gain (231, 235, where this took 226: the registers).  WIDE as for few rows: with
+// the choice made by each load, all loads under way were waited for, 226 us where this takes 214.
+template <class T, int MT, int KS, bool WIDE>
 __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const uint8_t* sw,
                                                       const uint8_t* H, const int* sh, int m,
                                                       int64_t D, int blocks, int part, int parts,
@@ -407,7 +408,7 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
         q[S][t][s] = *reinterpret_cast<const uintx4*>(p + min(4 * s + q4, blocks - 1) * 16);
 #pragma unroll
       for (int g = 0; g < G; ++g) {
-        if (blocks % 16 == 0) {  // all of the row's, in one load
+        if constexpr (WIDE) {  // all of the row's, in one load
           typedef unsigned words __attribute__((ext_vector_type(4), aligned(1)));
           const words u = *reinterpret_cast<const words*>(ps + 16 * g);
 #pragma unroll
@@ -423,14 +424,14 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
   auto run = [&](auto slot, int64_t tile) {
     constexpr int S = slot;
     // four steps of the lane's own blocks a word: put together here, or the loads would be waited
-    // for where they are issued (512 rows by 500 000 x 1024: 226 us so)
+    // for where they are issued
     int e[MT][G];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         const unsigned* u = raw[S][t] + kGroup * g;
-        const unsigned how = blocks % 16 == 0 ? pick : 0x0400u;
+        const unsigned how = WIDE ? pick : 0x0400u;
         e[t][g] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], how),
                                         __builtin_amdgcn_perm(u[1], u[0], how), 0x05040100);
       }
@@ -493,14 +494,16 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
   int64_t tile = (w / near * (each / 8) + (int64_t)(i / parts) * 8 + xcd) * near + w % near;
   std::integral_constant<int, 0> even;
   std::integral_constant<int, 1> odd;
-  if (tile < all) load(even, tile);
+  load(even, tile);
   wait_vm_le(0);
   __syncthreads();
   const int64_t first = ((int64_t)(i / parts) * 8 + xcd) * near;  // of the block's waves
   for (int64_t u = first; u < all; u += 2 * each, tile += 2 * each) {
-    if (tile + each < all) load(odd, tile + each);
+    // also behind the last tile, where all lanes read W's last row: a load that a branch may leave
+    // out cannot be told from those before it, and would be waited for with them
+    load(odd, tile + each);
     run(even, tile);
-    if (tile + 2 * each < all) load(even, tile + 2 * each);
+    load(even, tile + 2 * each);
     run(odd, tile + each);
   }
 }
@@ -563,11 +566,13 @@ int lst_scores_four(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int3
         using T = decltype(t);
         const int64_t groups = (D + 127) / 128;
         const size_t lds = (size_t)steps * (kPiece + 64 * sizeof(int));
-        hipLaunchKernelGGL((few_kernel<TH, T>),
-                           dim3((unsigned)std::min<int64_t>(groups, kFewBlocks)), dim3(512), lds,
-                           s, (const TH*)H, ldh, d, codes, scales, m, D, blocks, steps, (T*)O,
-                           ldo);
-        return launched();
+        auto run = [&](auto kernel) {
+          hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(groups, kFewBlocks)),
+                             dim3(512), lds, s, (const TH*)H, ldh, d, codes, scales, m, D, blocks,
+                             steps, (T*)O, ldo);
+          return launched();
+        };
+        return blocks % 16 == 0 ? run(few_kernel<TH, T, true>) : run(few_kernel<TH, T, false>);
       });
     });
   // 256 rows of W and up to 8 tiles of H a block; no more than there are: 17 rows of H by 200 000
@@ -607,15 +612,18 @@ int lst_scores_four(int32_t dtype, int32_t out_dtype, int32_t m, int64_t D, int3
                            ldo);
         return launched();
       };
+      const bool wide = blocks % 16 == 0;  // whole words of exponents
       switch (steps) {
-        case 1: return run(held_kernel<T, 4, 1>, 4);
-        case 2: return run(held_kernel<T, 4, 2>, 4);
-        case 3: return run(held_kernel<T, 4, 3>, 4);
-        case 4: return run(held_kernel<T, 4, 4>, 4);
-        case 5: return run(held_kernel<T, 2, 5>, 2);
-        case 6: return run(held_kernel<T, 2, 6>, 2);
-        case 7: return run(held_kernel<T, 2, 7>, 2);
-        default: return run(held_kernel<T, 2, 8>, 2);
+        case 1: return run(held_kernel<T, 4, 1, false>, 4);
+        case 2: return run(held_kernel<T, 4, 2, false>, 4);
+        case 3: return run(held_kernel<T, 4, 3, false>, 4);
+        case 4: return wide ? run(held_kernel<T, 4, 4, true>, 4)
+                            : run(held_kernel<T, 4, 4, false>, 4);
+        case 5: return run(held_kernel<T, 2, 5, false>, 2);
+        case 6: return run(held_kernel<T, 2, 6, false>, 2);
+        case 7: return run(held_kernel<T, 2, 7, false>, 2);
+        default: return wide ? run(held_kernel<T, 2, 8, true>, 2)
+                             : run(held_kernel<T, 2, 8, false>, 2);
       }
     });
   return with_dtype(out_dtype, [&](auto t) {
