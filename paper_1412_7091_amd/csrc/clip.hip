@@ -195,17 +195,18 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(Table t, const double* 
 
 int64_t size_of(int dtype) { return dtype == LST_F32 ? 4 : 2; }
 
-// Memory that a matrix takes: `width` bytes of each `stride`.
+// Memory that a matrix takes: `width` bytes of each `stride`, or once for a single row.
 struct Region {
   uintptr_t from, to;
   int64_t stride, width;
-  int owner;
-  bool written;
+  bool single, written;
 };
 
 bool overlap(const Region& a, const Region& b) {  // a.from <= b.from < a.to
-  if (a.stride != b.stride) return true;
-  // columns of the same matrix do not meet when neither is wrapped into the other
+  // rows of different strides are not followed through each other
+  if (!a.single && !b.single && a.stride != b.stride) return true;
+  // b begins in a row of a, or behind one in front of another: columns of the same matrix do not
+  // meet when neither is wrapped into the other
   const int64_t off = (int64_t)((b.from - a.from) % (uintptr_t)a.stride);
   return off < a.width || off + b.width > a.stride;
 }
@@ -233,8 +234,8 @@ bool apart(int n, const lst_gradient* grads) {
     auto add = [&](const void* p, int64_t ld, bool written) {
       const uintptr_t from = (uintptr_t)p;
       const int64_t stride = g.rows == 1 ? width : ld * e;
-      all.push_back({from, from + (uintptr_t)((g.rows - 1) * stride + width), stride, width, i,
-                     written});
+      all.push_back({from, from + (uintptr_t)((g.rows - 1) * stride + width), stride, width,
+                     g.rows == 1, written});
     };
     const bool own = !g.out || g.out == g.data;
     add(g.data, g.ld, own);

@@ -85,6 +85,26 @@ def test_columns_of_wider_matrices(gpu_lib, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_single_rows_beside_columns(gpu_lib, dtype):
+    """A row, and a vector, whose memory lies between the rows of another matrix: taken where they
+    share no element, on either side of it, and refused where they share one."""
+    whole = torch.randn((100, 64), device="cuda").to(dtype)
+    flat = whole.view(-1)
+    for others in ((whole[:, :32], whole[3:4, 32:]), (whole[3:4, 32:], whole[:, :32]),
+                   (whole[:, :32], whole[99, 32:], whole[0, 32:]),
+                   (whole[1:, 8:40], flat[:72], flat[104:136], whole[99, 40:]),
+                   (whole[5:6, 1:2], whole[5:, 2:], whole[:, :1])):
+        before = [_np(t) for t in others]
+        _check(before, others, lst.lst_clip(others, 1.5), 1.5)
+    for others in ((whole[:, :33], whole[3:4, 32:]), (whole[3, 32:], whole[:, :33]),
+                   (whole[1:, 8:40], flat[:73]), (whole[1:, 8:40], flat[103:136]),
+                   (whole[:, 8:40], flat[104:137]), (whole[:, 8:40], flat[40:136])):
+        with pytest.raises(lst.LstError):
+            lst.lst_clip(others, 1.5)
+
+
+@pytest.mark.gpu
 def test_large(gpu_lib):
     """More tiles than a launch has blocks, and a sum that float32 would not hold."""
     t = torch.full((40_000_003,), 2.0 ** -10, device="cuda")
