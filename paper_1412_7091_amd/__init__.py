@@ -1275,8 +1275,9 @@ class RMSNorm:
 
 class GradientClip:
     """The norm over the gradients of a step, and those scaled to a largest norm, for a program
-    whose gradients keep their memory from step to step: the list is checked once, and the object
-    keeps the tensors.  Scales in place, or into the tensors of out."""
+    whose gradients keep their memory from step to step: the tensors' types, shapes and addresses
+    are taken once, and the object keeps the tensors; whether their memory is apart is looked at in
+    each call, as in lst_clip.  Scales in place, or into the tensors of out."""
 
     def __init__(self, tensors, out=None):
         import torch

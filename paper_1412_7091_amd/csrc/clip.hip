@@ -202,13 +202,116 @@ struct Region {
   bool single, written;
 };
 
-bool overlap(const Region& a, const Region& b) {  // a.from <= b.from < a.to
-  // rows of different strides are not followed through each other
-  if (!a.single && !b.single && a.stride != b.stride) return true;
-  // b begins in a row of a, or behind one in front of another: columns of the same matrix do not
-  // meet when neither is wrapped into the other
-  const int64_t off = (int64_t)((b.from - a.from) % (uintptr_t)a.stride);
-  return off < a.width || off + b.width > a.stride;
+// Elements of a region as rows and columns of a matrix whose row stride is the region's, or any
+// for a single row.
+struct Box {
+  int64_t row0, row1, col0, col1;
+  bool written;
+};
+
+void add_boxes(const Region& r, uintptr_t base, int64_t stride, std::vector<Box>& boxes) {
+  const int64_t from = (int64_t)(r.from - base), row = from / stride, col = from % stride;
+  const int64_t rows = r.single ? 1 : (int64_t)(r.to - r.from - r.width) / stride + 1;
+  const int64_t head = std::min(r.width, stride - col), rest = r.width - head;
+  const int64_t full = rest / stride, tail = rest % stride;  // full: of a single row alone
+  boxes.push_back({row, row + rows, col, col + head, r.written});
+  if (full) boxes.push_back({row + 1, row + 1 + full, 0, stride, r.written});
+  if (tail) boxes.push_back({row + 1 + full, row + 1 + full + rows, 0, tail, r.written});
+}
+
+// How many of the numbers that are in it are below another one.
+struct Count {
+  std::vector<int32_t> n;
+  explicit Count(size_t size) : n(size + 1) {}
+  void add(size_t at, int32_t v) {
+    for (++at; at < n.size(); at += at & -at) n[at] += v;
+  }
+  int32_t below(size_t at) const {
+    int32_t sum = 0;
+    for (; at; at -= at & -at) sum += n[at];
+    return sum;
+  }
+};
+
+// Whether two boxes meet, one of which is written: the columns are gone through, and of the boxes
+// that have a column the rows are counted, so that n boxes take n log n steps (65 536 matrices of
+// neighbouring columns 15 ms on the host; compared by pairs 7.7 s).
+bool meet(const std::vector<Box>& boxes) {
+  struct Event {
+    int64_t col;
+    int begins;  // ends come first
+    size_t box;
+  };
+  std::vector<int64_t> rows;
+  std::vector<Event> events;
+  for (size_t i = 0; i < boxes.size(); ++i) {
+    rows.push_back(boxes[i].row0);
+    rows.push_back(boxes[i].row1);
+    events.push_back({boxes[i].col0, 1, i});
+    events.push_back({boxes[i].col1, 0, i});
+  }
+  std::sort(rows.begin(), rows.end());
+  rows.erase(std::unique(rows.begin(), rows.end()), rows.end());
+  std::sort(events.begin(), events.end(), [](const Event& a, const Event& b) {
+    return a.col != b.col ? a.col < b.col : a.begins < b.begins;
+  });
+  auto at = [&](int64_t row) {
+    return (size_t)(std::lower_bound(rows.begin(), rows.end(), row) - rows.begin());
+  };
+  // where rows of the open boxes begin and end, of those that are only read and of the written
+  Count first[2] = {Count(rows.size()), Count(rows.size())}, last[2] = {first[0], first[0]};
+  for (const Event& e : events) {
+    const Box& b = boxes[e.box];
+    const size_t lo = at(b.row0), hi = at(b.row1);
+    if (e.begins)
+      for (int w = !b.written; w < 2; ++w)
+        if (first[w].below(hi) > last[w].below(lo + 1)) return true;
+    first[b.written].add(lo, e.begins ? 1 : -1);
+    last[b.written].add(hi, e.begins ? 1 : -1);
+  }
+  return false;
+}
+
+// The furthest end of the regions so far, and that of those with another stride.
+struct Reach {
+  uintptr_t to[2] = {0, 0};
+  int64_t stride[2] = {0, 0};
+  void add(const Region& r) {
+    if (r.stride == stride[0]) {
+      to[0] = std::max(to[0], r.to);
+    } else if (r.to > to[0]) {
+      to[1] = to[0], stride[1] = stride[0];
+      to[0] = r.to, stride[0] = r.stride;
+    } else if (r.to > to[1]) {
+      to[1] = r.to, stride[1] = r.stride;
+    }
+  }
+  bool other(const Region& r) const { return to[stride[0] == r.stride] > r.from; }
+};
+
+// Whether regions that reach into each other, in order, share no element that is written.
+bool apart(const Region* r, size_t n) {
+  // several rows of different strides are not followed through each other
+  Reach all, written;
+  std::vector<int64_t> strides;
+  for (size_t i = 0; i < n; ++i) {
+    if (r[i].single) continue;
+    if ((r[i].written ? all : written).other(r[i])) return false;
+    all.add(r[i]);
+    if (r[i].written) written.add(r[i]);
+    strides.push_back(r[i].stride);
+  }
+  std::sort(strides.begin(), strides.end());
+  strides.erase(std::unique(strides.begin(), strides.end()), strides.end());
+  if (strides.empty()) strides.push_back((int64_t)1 << 62);
+  std::vector<Box> boxes;
+  for (const int64_t stride : strides) {
+    boxes.clear();
+    for (size_t i = 0; i < n; ++i)
+      if (r[i].single || r[i].stride == stride) add_boxes(r[i], r[0].from, stride, boxes);
+    if (meet(boxes)) return false;
+  }
+  return true;
 }
 
 bool good(const lst_gradient& g) {
@@ -243,9 +346,11 @@ bool apart(int n, const lst_gradient* grads) {
   }
   std::sort(all.begin(), all.end(),
             [](const Region& a, const Region& b) { return a.from < b.from; });
-  for (size_t i = 0; i < all.size(); ++i)
-    for (size_t j = i + 1; j < all.size() && all[j].from < all[i].to; ++j)
-      if ((all[i].written || all[j].written) && overlap(all[i], all[j])) return false;
+  for (size_t i = 0, end; i < all.size(); i = end) {  // groups that reach into each other
+    uintptr_t to = all[i].to;
+    for (end = i + 1; end < all.size() && all[end].from < to; ++end) to = std::max(to, all[end].to);
+    if (end - i > 1 && !apart(&all[i], end - i)) return false;
+  }
   return true;
 }
 

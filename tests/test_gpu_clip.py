@@ -1,5 +1,6 @@
 """lst_clip against oracle.norms: the norm, and every element within its roundings."""
 import ctypes
+import time
 
 import numpy as np
 import pytest
@@ -102,6 +103,64 @@ def test_single_rows_beside_columns(gpu_lib, dtype):
                    (whole[:, 8:40], flat[104:137]), (whole[:, 8:40], flat[40:136])):
         with pytest.raises(lst.LstError):
             lst.lst_clip(others, 1.5)
+
+
+@pytest.mark.gpu
+def test_lists_within_one_matrix(gpu_lib):
+    """Lists drawn from one piece of memory: those are refused in which an element that is written
+    is in two (or whose rows of different strides reach into each other), and no others; of those
+    that are taken every element is right."""
+    rng = np.random.default_rng(7)
+    taken = refused = 0
+    for _ in range(400):
+        memory = torch.randn(1200, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+        used, lists, spans = np.zeros(1200, int), ([], []), []
+        wide = rng.integers(8, 40, 2) if rng.random() < 0.3 else rng.integers(8, 40, 1).repeat(2)
+        shared = False
+        for _ in range(rng.integers(2, 6)):
+            rows = int(rng.choice([1, 1, 2, 7, 20]))
+            cols = int(rng.integers(1, 8 if rows > 1 else 60))
+            apart = rng.random() < 0.3
+            for k in range(2):
+                ld = int(rng.choice(wide))
+                at = int(rng.integers(0, 1200 - (rows - 1) * ld - cols + 1))
+                if k and not apart:
+                    lists[1].append(None)
+                    continue
+                view = torch.as_strided(memory, (rows, cols), (ld, 1), at)
+                lists[k].append(view)
+                place = (at + ld * np.arange(rows)[:, None] + np.arange(cols)).ravel()
+                written = k == 1 or not apart
+                shared |= bool((used[place] >= (1 if written else 2)).any())
+                used[place] |= 2 if written else 1
+                for s in spans if rows > 1 else ():
+                    shared |= (s[2] != ld and at < s[1] and s[0] < place[-1] + 1
+                               and (written or s[3]))
+                if rows > 1:
+                    spans.append((at, int(place[-1]) + 1, ld, written))
+        if shared:
+            refused += 1
+            with pytest.raises(lst.LstError):
+                lst.lst_clip(lists[0], 0.5, out=lists[1])
+            continue
+        taken += 1
+        before = [_np(t) for t in lists[0]]
+        norm = lst.lst_clip(lists[0], 0.5, out=lists[1])
+        _check(before, [t if o is None else o for t, o in zip(*lists)], norm, 0.5)
+    assert taken > 40 and refused > 40
+
+
+def test_many_columns_of_one_matrix_are_compared_quickly():
+    """The list's last matrices share memory: refused, in a time far below that of all pairs
+    (2^31 of them, seconds)."""
+    n = 65_536
+    table = (lst.lst_gradient * n)()
+    for i, g in enumerate(table):  # never read: the call is refused
+        g.data, g.rows, g.cols, g.ld = (1 << 30) + 64 * min(i, n - 2), 500, 16, 16 * n
+    lib, p = lst.load_library(), 1 << 20
+    start = time.process_time()
+    assert lib.lst_clip(n, table, 1.0, p, p, None, None) == lst.LST_EINVAL
+    assert time.process_time() - start < 1.0
 
 
 @pytest.mark.gpu
