@@ -674,12 +674,13 @@ int64_t lst_logprobs_workspace(int32_t m, int32_t D, int32_t top); /* bytes; -1 
  *   grads   (host)    n matrices, 0 <= n <= 65 536, of types of their own, 2^40 elements
  *                     together at most; read before the call returns.
  *   max_norm          at least 0; infinite: nothing is scaled.
- *   norm   (device)   a float, receives n (of the gradients as they came).
+ *   norm   (device)   a float, receives n (of the gradients as they came); infinite also where n
+ *                     is beyond float32's range, and the gradients are scaled all the same.
  * A matrix that is written shares memory with no other of the call, data or out: the call refuses
  * a list in which one does, the same matrix twice among them.  Columns of one wider matrix are
  * apart, and so are single rows and vectors beside them; two matrices of several rows whose
  * strides differ are refused where one begins before the other's end.
- * When n is not finite nothing is scaled, and the status is set to LST_ENONFINITE.
+ * When an element is not finite nothing is scaled, and the status is set to LST_ENONFINITE.
  * The squares are summed in 64 bits, in an order that does not depend on timing.
  */
 typedef struct lst_gradient {

@@ -108,7 +108,7 @@ __device__ inline double tile_squares(const Entry& e, uint32_t tile) {
 }
 
 template <class T>
-__device__ inline void scale_tile(const Entry& e, uint32_t tile, float factor) {
+__device__ inline void scale_tile(const Entry& e, uint32_t tile, float factor, int power) {
   const int64_t group = tile * kGroups + threadIdx.x;
   T v[kItems][8];
 #pragma unroll
@@ -120,7 +120,7 @@ __device__ inline void scale_tile(const Entry& e, uint32_t tile, float factor) {
     const Place at(e, g);
     T* p = (T*)e.out + at.row * e.ldo + at.col;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[j][i] = (T)((float)v[j][i] * factor);
+    for (int i = 0; i < 8; ++i) v[j][i] = (T)__builtin_ldexpf((float)v[j][i] * factor, power);
     if (at.col + 8 <= e.cols) {
       store_vec(p, v[j]);
     } else {
@@ -174,7 +174,10 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(Table t, const double* 
   __shared__ double lds[kThreads / 64];
   const double all = sqrt(total_of(partial, n, lds));
   const bool finite = all < (double)INFINITY;
-  const float factor = finite && all > max_norm ? (float)(max_norm / all) : 1.f;
+  const double ratio = finite && all > max_norm ? max_norm / all : 1.0;
+  // a ratio that is no normal float goes as a fraction and a power of two
+  int power = 0;
+  const float factor = (float)(ratio < 0x1p-126 ? __builtin_frexp(ratio, &power) : ratio);
   if (first && blockIdx.x == 0 && threadIdx.x == 0) {
     *norm = (float)all;
     if (!finite && status) atomicCAS(status, 0, LST_ENONFINITE);
@@ -182,14 +185,14 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(Table t, const double* 
   for (uint32_t i = blockIdx.x; i < t.tiles; i += gridDim.x) {
     const uint32_t tile = t.tiles - 1 - i;
     const Entry& e = t.e[entry_of(t, tile)];
-    if (factor == 1.f && e.out == e.data) continue;
+    if (factor == 1.f && power == 0 && e.out == e.data) continue;
     const uint32_t at = tile - e.first;
     if (e.dtype == LST_F32)
-      scale_tile<float>(e, at, factor);
+      scale_tile<float>(e, at, factor, power);
     else if (e.dtype == LST_BF16)
-      scale_tile<__bf16>(e, at, factor);
+      scale_tile<__bf16>(e, at, factor, power);
     else
-      scale_tile<_Float16>(e, at, factor);
+      scale_tile<_Float16>(e, at, factor, power);
   }
 }
 

@@ -214,6 +214,36 @@ def test_extremes_and_what_is_not_finite(gpu_lib):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES[:2])
+@pytest.mark.parametrize("big,max_norm", [(1e37, 1e-6), (3e38, 1.0), (3e38, 2.0 ** -30),
+                                          (1e30, 2.0 ** -100), (1e38, 1e-100)])
+def test_factors_below_normal_floats(gpu_lib, dtype, big, max_norm):
+    """Gradients so large that max_norm / n is no normal float: each element within its
+    roundings all the same, small ones beside the large ones too."""
+    g = torch.Generator("cuda").manual_seed(5)
+    a = (torch.rand(300, device="cuda", generator=g) * big).to(dtype)
+    b = (torch.randn((9, 17), device="cuda", generator=g) * (big * 2.0 ** -70)).to(dtype)
+    c = torch.randn((5, 8), device="cuda", generator=g).to(dtype)
+    before = [_np(t) for t in (a, b, c)]
+    out = [torch.empty_like(t) for t in (a, b, c)]
+    n = norms.clip(before, max_norm)[0]
+    assert 0 < max_norm / n < 2.0 ** -126
+    for norm, got in ((lst.lst_clip([a, b, c], max_norm, out=out), out),
+                      (lst.lst_clip([a, b, c], max_norm), [a, b, c])):
+        if n > 3.5e38:
+            assert torch.isinf(norm).all()
+            norm = torch.tensor(n, dtype=torch.float64)
+        _check(before, got, norm, max_norm)
+
+
+@pytest.mark.gpu
+def test_a_factor_whose_fraction_rounds_to_one(gpu_lib):
+    t = [torch.full((1,), 2.0 ** 100, device="cuda")]
+    lst.lst_clip(t, (1 - 2.0 ** -40) * 2.0 ** -100)
+    assert float(t[0]) == 2.0 ** -100
+
+
+@pytest.mark.gpu
 def test_repeats_captures_and_streams(gpu_lib):
     tensors = _tensors([(500, 900), (700,), (33, 65)], 5)
     out = [torch.empty_like(t) for t in tensors]
