@@ -635,7 +635,7 @@ int64_t lst_sample_workspace(int32_t m, int32_t D); /* bytes; -1 for a bad size 
  * row:
  *   logits            m x D, 1 <= D <= 2^30.  Entries that are -inf or no number have no
  *                     probability (log p = -inf); where some are +inf, those share all of it.
- *   temperature (device) m values, or NULL for 1.  Above zero and finite.
+ *   temperature (device) m values, or NULL for 1.  Above zero and finite; below 2^-126 as 2^-126.
  *   tokens (device)   m x K ints, 0 <= K <= 1024: -1 is unused.  An index outside [-1, D) sets the
  *                     status LST_EINDEX and counts as unused.
  *   logp   (device)   m x K floats: log p of each token, 0 for an unused one.

@@ -43,9 +43,15 @@ struct Sums {  // relative to m: s = sum e^z, t = sum e^z z / ln 2
   float m, s, t;
 };
 
+// x - m, halved: entries may be further apart than the largest float.  (Halving is exact down to
+// the smallest floats, and 2 c and t take it back: no other bit than without it.)
+__device__ inline float half_of(float x, float m) { return fmaf(x, 0.5f, -0.5f * m); }
+
 // An exponent of two that is never infinite: below 2^-1000 all is zero.  What is no number, and
 // so a masked entry that is none, counts as the smallest.
-__device__ inline float exponent(float x, float m, float c) { return fmaxf((x - m) * c, -1e4f); }
+__device__ inline float exponent(float x, float m, float c) {
+  return fmaxf(half_of(x, m) * (2.f * c), -1e4f);
+}
 
 // c: log2(e) / T.  Eight entries more.
 __device__ inline void add_entries(Sums& a, const float (&x)[8], float largest, float c) {
@@ -165,12 +171,13 @@ struct Args {
   float* largest;   // a batch's rows x segments
 };
 
-// T, or 0 for one that is not above zero and finite.
+// T, or 0 for one that is not above zero and finite.  One below the normal floats counts as the
+// smallest of these, so that twice its rate is a float.
 __device__ inline float temperature_of(const float* temperature, int row) {
   const float t = temperature ? temperature[row] : 1.f;
-  return t > 0.f && t < INFINITY ? t : 0.f;
+  return t > 0.f && t < INFINITY ? fmaxf(t, 0x1p-126f) : 0.f;
 }
-__device__ inline float rate_of(float t) { return t > 0.f ? fminf(kLog2e / t, -kLowest) : 1.f; }
+__device__ inline float rate_of(float t) { return t > 0.f ? kLog2e / t : 1.f; }
 
 // Entries col .. col + 7 of a row, -inf behind the last.
 template <class T>
@@ -517,7 +524,7 @@ __device__ inline void finish_row(const Args& a, int row, const T* x, Sums sums,
   auto log_of = [&](float v) {
     if (!some || !(v > -INFINITY)) return -INFINITY;
     if (sums.m == INFINITY) return v == INFINITY ? -log_s : -INFINITY;
-    return (v - sums.m) / t - log_s;
+    return 2.f * (half_of(v, sums.m) / t) - log_s;
   };
   float* saved = a.saved ? a.saved + (int64_t)row * (a.K + 4) : nullptr;
   if (threadIdx.x == 0) {

@@ -201,6 +201,33 @@ def test_masks_and_what_is_not_finite(gpu_lib, D):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES[:2])
+@pytest.mark.parametrize("D", [2, 60, 9001, 30_000, 200_003])
+def test_entries_further_apart_than_the_largest_float(gpu_lib, dtype, D):
+    """Entries near both ends of the type at temperatures that leave them all a probability: the
+    sums, the tokens' logarithms and the gradient go by the same exponents."""
+    rng = np.random.default_rng(D)
+    x = rng.uniform(-3.3e38, 3.3e38, (5, D))
+    x[:, 0], x[:, 1] = 3.3e38, -3.3e38
+    x[1, D // 2:] = -3.3e38
+    x[2, 1:D // 2 + 1], x[2, D // 2 + 1:] = -3.3e38, 3.3e38
+    x[3, 2:][rng.random(max(0, D - 2)) < 0.5] = -INF
+    x[4, 2:] = -3.2e38
+    x = _dev(x, dtype)
+    t = np.array([1e38, 1e38, 1e38, 3e37, 1e36], np.float32)
+    tokens = np.tile(np.array([1, 0, D - 1, -1]), (5, 1))
+    td, tt = _dev(tokens, torch.int32), _dev(t)
+    # a gradient of ordinary size: it is divided by the temperature
+    g, ge = rng.standard_normal((5, 4)).astype(np.float32) * np.float32(1e33), np.full(
+        5, 1e33, np.float32)
+    got = lst.lst_logprobs(x, td, top=5, temperature=tt, save=True)
+    grad = lst.lst_logprobs_backward(x, td, got[4], _dev(g), _dev(ge), temperature=tt)
+    for i, row in enumerate(_np(x)):
+        _check_row(row, i, tokens[i], float(t[i]), got, 5)
+        _check_grad(row, i, tokens[i], float(t[i]), g[i], float(ge[i]), grad, dtype)
+
+
+@pytest.mark.gpu
 def test_indices_outside_set_the_status(gpu_lib):
     x = _logits(2, 40, torch.float32, masked=0)
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
