@@ -506,7 +506,8 @@ int lst_recur_step(int32_t dtype, int32_t rows, int32_t n_slots, int32_t d, cons
  *   codes, scales (device)  receive y (before it is rounded to the type) in 8 bits, as
  *                   lst_quantize leaves a matrix: input for lst_scores_coded.  Both NULL when
  *                   not wanted; codes 16-byte aligned.
- *   rstd   (device) rows floats, receives q for lst_norm_backward; may be NULL.
+ *   rstd   (device) rows floats, receives q for lst_norm_backward; may be NULL.  Where q is below
+ *                   2^-126 (a root mean square above 2^126) it has fewer digits, at least 22.
  * The squares are summed in 64 bits.
  */
 int lst_norm_forward(int32_t dtype, int64_t rows, int32_t cols, const void* x, int64_t ldx,
@@ -516,7 +517,7 @@ int lst_norm_forward(int32_t dtype, int64_t rows, int32_t cols, const void* x, i
 
 /*
  * lst_norm_backward -- gradients of lst_norm_forward.  sum: its s (x where there was no
- * residual), rstd as it left it.  grad_y and grad_sum (or NULL) are dL/dy and what else of dL/ds
+ * residual; where y took the place of x, what the call left in its sum), rstd as it left it.  grad_y and grad_sum (or NULL) are dL/dy and what else of dL/ds
  * there is; grad_x receives the gradient with respect to x, which is the residual's too, and may
  * be sum, grad_y or grad_sum.  grad_weight (device, cols floats) receives the sums over all rows
  * (zeros for none), added in an order that does not depend on timing.

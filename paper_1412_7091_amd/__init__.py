@@ -777,19 +777,27 @@ def _sum(x, residual, out):
 
 def lst_norm_forward(x, weight, residual=None, *, eps=1e-6, out=None, sum_out=None, rstd=None):
     """(y, s) of the root-mean-square norm: s = x + residual (x itself without one) and
-    y = s weight / rms(s).  rstd: a vector that receives each row's factor."""
+    y = s weight / rms(s).  rstd: a vector that receives each row's factor.
+
+    Where y takes the place of x, without a residual and without rows for s, x is gone: s is None,
+    or, with rstd, rows of its own for the backward pass."""
     import torch
 
     px, ldx = _matrix(x, "x")
     code = _dtype_code(x, "x")
     pr, ldr = _matrix(residual, "residual", x, x.shape)
+    gone = False
     if out is None:
         out = x.new_empty(x.shape)
+    elif residual is None and sum_out is None and x.numel() and out.data_ptr() == px:
+        if rstd is not None:
+            sum_out = x.new_empty(x.shape)
+        gone = rstd is None
     s, ps, lds = _sum(x, residual, sum_out)
     _enqueue("lst_norm_forward", x.device, code, x.shape[0], x.shape[1], px, ldx, pr, ldr,
              _weight(weight, x), float(eps), ps, lds, *_matrix(out, "out", x, x.shape), None, None,
              _vector(rstd, torch.float32, "rstd", x.device, x.shape[0]))
-    return out, s
+    return out, None if gone else s
 
 
 def lst_norm_coded(x, weight, residual=None, *, eps=1e-6, codes=None, scales=None, sum_out=None,
@@ -819,6 +827,8 @@ def lst_norm_backward(s, rstd, weight, grad_y, grad_sum=None, *, out=None, grad_
     """(grad_x, grad_weight) from the forward pass' s and rstd; grad_x is the residual's too."""
     import torch
 
+    if s is None:
+        raise TypeError("s must be what the forward pass normed")
     ps, lds = _matrix(s, "s")
     code = _dtype_code(s, "s")
     (rows, cols), dev = s.shape, s.device
@@ -1254,7 +1264,8 @@ class RMSNorm:
         self.weight, self.eps = weight, float(eps)
 
     def forward(self, x, residual=None, *, out=None, sum_out=None, save=False):
-        """(y, s, rstd); s is x itself without a residual, rstd None unless save."""
+        """(y, s, rstd); s is x itself without a residual, rstd None unless save.  Where y takes the
+        place of x without a residual, s is a copy of x with save, and None without."""
         import torch
 
         rstd = x.new_empty(x.shape[0], dtype=torch.float32) if save else None

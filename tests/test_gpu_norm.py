@@ -185,6 +185,35 @@ def test_strides_in_place_and_what_is_beside(gpu_lib, dtype, cols):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 5), (9, 300), (3, 2049)])
+def test_in_place_without_a_residual(gpu_lib, dtype, rows, cols):
+    """y where x was: the sum that the backward pass reads is x as it was, and none is returned
+    where there is none."""
+    w, (x, _, gy, gs) = _inputs(rows, cols, dtype)
+    layer = lst.RMSNorm(w)
+    want, s, rstd = layer.forward(x, save=True)
+    grads = layer.backward(s, rstd, gy, gs)
+    a = x.clone()
+    y, kept, rstd = layer.forward(a, out=a, save=True)
+    assert y is a and torch.equal(a, want) and torch.equal(kept, x)
+    for g, h in zip(layer.backward(kept, rstd, gy, gs), grads):
+        assert torch.equal(g, h)
+    a, b = x.clone(), torch.empty_like(x)
+    y, kept, _ = layer.forward(a, out=a)
+    assert torch.equal(y, want) and kept is None
+    with pytest.raises(TypeError):
+        layer.backward(kept, rstd, gy)
+    a.copy_(x)
+    y, kept, _ = layer.forward(a, out=a, sum_out=b)
+    assert torch.equal(y, want) and kept is b and torch.equal(b, x)
+    a = x.clone()
+    assert lst.lst_norm_forward(a, w, out=a, rstd=rstd)[1].data_ptr() != a.data_ptr()
+    none = x[:0]
+    assert layer.forward(none, out=none)[1] is none
+
+
+@pytest.mark.gpu
 def test_extremes(gpu_lib):
     """Squares beyond float32's range, rows of zeros, tiny rows, infinities and no numbers."""
     w = torch.ones(40, device="cuda")
