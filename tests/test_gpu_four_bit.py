@@ -141,6 +141,46 @@ def test_rows_of_new_outputs_begin_at_lines(gpu_lib, out):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("out", TYPES[:2])
+@pytest.mark.parametrize("m,D,d,step", [
+    # up to 16 rows of H: 65 536 rows of W a round of waves, with and without words of exponents
+    (1, 140_001, 300, 65_536), (16, 140_001, 512, 65_536), (3, 70_003, 1000, 65_536),
+    (16, 131_073, 40, 65_536),
+    # 131 072 a round, 65 536 above 512 columns; the third round reuses the first one's registers
+    (17, 262_221, 33, 131_072), (40, 262_221, 300, 131_072), (33, 262_145, 450, 131_072),
+    (20, 140_000, 512, 131_072), (30, 400_009, 100, 131_072),
+    (18, 131_149, 700, 65_536), (20, 131_149, 1024, 65_536), (17, 131_073, 520, 65_536),
+    (40, 70_000, 1000, 65_536), (17, 300_001, 896, 65_536),
+    # several parts of H: 10 blocks of a part on an XCD
+    (528, 50_001, 1024, 20_480), (257, 66_000, 1000, 32_768)])
+def test_scores_of_many_rows_of_weights(gpu_lib, m, D, d, step, out):
+    """More rows of W than all waves take at once: rows around the end of each round against the
+    oracle, all of them against calls for parts of W, which one round takes, and what is beside."""
+    g = torch.Generator("cuda").manual_seed(m + D + d)
+    W = torch.randn((D, d), device="cuda", generator=g) / d ** 0.5
+    W *= torch.exp2(torch.randint(-9, 9, (D, 1), device="cuda", generator=g).float())
+    H = torch.randn((m, d), device="cuda", generator=g)
+    layer = lst.FourBitOutputLayer(W)
+    got = layer.scores(H, dtype=out)
+    near = [np.arange(r - 70, r + 70) for r in range(0, D + step, step)] + [np.arange(D - 70, D)]
+    rows = np.unique(np.concatenate(near))
+    rows = torch.from_numpy(rows[(rows >= 0) & (rows < D)]).cuda()
+    part = lst.FourBitOutputLayer(W[:1])
+    part.codes, part.scales = layer.codes[rows], layer.scales[rows]
+    _check_scores(H, part, got[:, rows])
+    for a in range(0, D, 8000):
+        some = slice(a, a + 8000)
+        want = lst.lst_scores_four(H, layer.codes[some], layer.scales[some], dtype=out)
+        assert torch.equal(got[:, some], want), a
+    for wide, at in ((D, 0), (D + 7, 3)):
+        whole = torch.full((m + 2, wide), 5.0, device="cuda", dtype=out)
+        view = whole[1:1 + m, at:at + D]
+        assert torch.equal(layer.scores(H, out=view), got)
+        view.fill_(5.0)
+        assert (whole == 5.0).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("m", [3, 35])
 def test_sums_of_sizes_far_apart(gpu_lib, m):
     """Blocks 2^20 apart that one instruction adds up: what float32 keeps of the smaller stays."""
