@@ -90,6 +90,27 @@ def test_many_rows(gpu_lib, cols):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols", [((1 << 24) + 37, 5), ((1 << 20) + 5, 1030)])
+def test_more_rows_than_a_launch_has_blocks(gpu_lib, rows, cols):
+    """2^20 blocks of 16 rows, or of one: rows of the second turn, and around its begin, are those
+    of a call for them alone."""
+    g = torch.Generator("cuda").manual_seed(cols)
+    x = torch.randn((rows, cols), device="cuda", generator=g, dtype=torch.bfloat16)
+    w = torch.randn(cols, device="cuda", generator=g) + 1
+    layer = lst.RMSNorm(w)
+    some = slice(rows - 300, rows)
+    y, _, rstd = layer.forward(x, save=True)
+    want = layer.forward(x[some], save=True)
+    _check_forward(want[0], x[some], want[2], w, 1e-6, torch.bfloat16)
+    assert torch.equal(y[some], want[0]) and torch.equal(rstd[some], want[2])
+    assert torch.equal(y[:300], layer.forward(x[:300])[0])
+    del y
+    codes, scales, _ = layer.forward_coded(x)
+    want = layer.forward_coded(x[some])
+    assert torch.equal(codes[some], want[0]) and torch.equal(scales[some], want[1])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,cols", SHAPES)
 def test_codes(gpu_lib, dtype, rows, cols):
