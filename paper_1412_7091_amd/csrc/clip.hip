@@ -120,7 +120,11 @@ __device__ inline void scale_tile(const Entry& e, uint32_t tile, float factor, i
     const Place at(e, g);
     T* p = (T*)e.out + at.row * e.ldo + at.col;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[j][i] = (T)__builtin_ldexpf((float)v[j][i] * factor, power);
+    for (int i = 0; i < 8; ++i) {
+      const float f = (float)v[j][i] * factor;
+      // float16's values and a factor that needs a power give zeros without it, too
+      v[j][i] = (T)(std::is_same_v<T, _Float16> ? f : __builtin_ldexpf(f, power));
+    }
     if (at.col + 8 <= e.cols) {
       store_vec(p, v[j]);
     } else {
@@ -192,7 +196,7 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(Table t, const double* 
     else if (e.dtype == LST_BF16)
       scale_tile<__bf16>(e, at, factor, power);
     else
-      scale_tile<_Float16>(e, at, factor, power);
+      scale_tile<_Float16>(e, at, (float)ratio, 0);
   }
 }
 

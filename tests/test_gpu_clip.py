@@ -244,6 +244,18 @@ def test_a_factor_whose_fraction_rounds_to_one(gpu_lib):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("max_norm", [0.0, 1e-30, 1e-6, 2.0 ** -3])
+def test_float16_beside_large_gradients(gpu_lib, max_norm):
+    a = torch.full((70,), 2e38, device="cuda")
+    b = torch.full((5, 33), 60_000.0, device="cuda", dtype=torch.float16)
+    before = [_np(t) for t in (a, b)]
+    lst.lst_clip([a, b], max_norm)
+    _check(before, [a, b], torch.tensor(norms.clip(before, max_norm)[0], dtype=torch.float64),
+           max_norm)
+    assert (b == 0).all()
+
+
+@pytest.mark.gpu
 def test_repeats_captures_and_streams(gpu_lib):
     tensors = _tensors([(500, 900), (700,), (33, 65)], 5)
     out = [torch.empty_like(t) for t in tensors]
