@@ -508,8 +508,9 @@ __global__ __launch_bounds__(512, 1) void held_kernel(const uint8_t* W, const ui
   }
 }
 
-constexpr int kFew = 16;         // rows of H that one launch takes: 17.8 us (16 by 200 000 x
-                                 // 500 codes), with operands first 20.4; one row 15.9 and 19.8
+constexpr int kFew = 16;         // rows of H that one launch takes: a pass of 16 by 200 000 x 500
+                                 // codes 17.1 us, with operands first 19.5; one row 13.3 and 17.6;
+                                 // 16 by 200 000 x 1024 27.8 and 31.1, by 5000 x 500 10.7 and 13.5
 constexpr int kFewBlocks = 512;  // blocks of that launch, two a compute unit
 constexpr int64_t kMostBlocks = (1 << 30) - 64;  // of a matrix: 2^32 threads
 

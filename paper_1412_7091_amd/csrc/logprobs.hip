@@ -18,9 +18,12 @@
 // entries 4.6 us, 16 385 5.6; the 32 likeliest of them 10 and 11).
 //
 // Measured: 128 x 200 000 float32 20.5 us forwards, 5.0 TB/s, 4 more to join, 35 backwards, 5.8
-// TB/s (the logits partly from the cache); 64 x 793 471 bfloat16 27 us, 3.8 TB/s, where each entry
-// costs the vector units 42 clocks a wave, 16 of them the exponential, and 8 to join with the five
-// likeliest.
+// TB/s (the logits partly from the cache); 64 x 793 471 bfloat16 28 us, 3.6 TB/s, and 8 to join
+// with the five likeliest, 54 backwards, 3.7 TB/s.  In 16 bits forwards the vector units work two
+// thirds of the time that the compute units are busy (counted: 15 instructions, 66 clocks, a wave
+// and entry, 51 000 of 76 000 clocks; five of the 15 are the exponent, its power and the two
+// sums).  The rest is waiting: a block reads its four passes at once and sums with nothing under
+// way, and 6208 blocks, where 2048 are resident, are three rounds and a little.
 #include <algorithm>
 
 #include "dtypes.h"
